@@ -11,6 +11,7 @@
 // partials: bf16 on the bf16 path, fp32 on the fp32 path) is what the
 // workspace cap limits.
 #include "moba.h"
+#include "api_common.h"
 #include "bwd_internal.h"
 #include "decode_internal.h"
 #include "moba_internal.h"
@@ -34,108 +35,12 @@ constexpr size_t kAlign = 256;
 constexpr size_t kDefaultWorkspaceLimit = size_t(64) << 30;
 constexpr int kSpinLimit = 1 << 20;  // polls of a dK/dV hand-over flag before a wave gives up
 
-// ------------------------------------------------------------- profiling
-struct PhaseRec {
-  const char* name;
-  hipEvent_t a, b;
-};
-bool g_prof = false;
-std::vector<PhaseRec> g_recs;
-std::mutex g_prof_mu;
-
-struct Phase {
-  hipStream_t st;
-  PhaseRec rec{};
-  bool on = false;
-  Phase(const char* name, hipStream_t s) : st(s) {
-    if (!g_prof || !name) return;
-    rec.name = name;
-    if (hipEventCreate(&rec.a) != hipSuccess) return;
-    if (hipEventCreate(&rec.b) != hipSuccess) { (void)hipEventDestroy(rec.a); return; }
-    (void)hipEventRecord(rec.a, st);
-    on = true;
-  }
-  ~Phase() {
-    if (!on) return;
-    (void)hipEventRecord(rec.b, st);
-    std::lock_guard<std::mutex> lk(g_prof_mu);
-    g_recs.push_back(rec);
-  }
-};
-
-bool env_flag(const char* name) {
-  const char* e = std::getenv(name);
-  return e && e[0] && e[0] != '0';
-}
-
-// Read at every launch, so a process can switch it on and off.
-bool debug_sync() { return env_flag("MOBA_DEBUG_SYNC"); }
-
-#define MOBA_LAUNCH(expr)                                         \
-  do {                                                            \
-    hipError_t e_ = (expr);                                       \
-    if (e_ != hipSuccess) return MOBA_ERR_HIP;                    \
-    if (debug_sync() && hipStreamSynchronize(stream) != hipSuccess) \
-      return MOBA_ERR_HIP;                                        \
-  } while (0)
-
 size_t workspace_limit() {
   const char* e = std::getenv("MOBA_WORKSPACE_LIMIT_BYTES");
   if (!e || !e[0]) return kDefaultWorkspaceLimit;
   char* end = nullptr;
   unsigned long long v = std::strtoull(e, &end, 10);
   return (end && *end == 0) ? (size_t)v : kDefaultWorkspaceLimit;
-}
-
-// ------------------------------------------------------------- validation
-struct View {
-  void* data;
-  int64_t st, sh;  // token and head strides, elements
-  int64_t H;
-};
-
-// Number of elements a descriptor spans (0 if any dimension is empty).
-int64_t numel(const moba_tensor* t) {
-  int64_t n = 1;
-  for (int d = 0; d < t->ndim && d < 4; d++) n *= std::max<int64_t>(t->shape[d], 0);
-  return n;
-}
-
-// A data pointer may be NULL only for an empty tensor.
-bool missing(const moba_tensor* t) { return !t || (!t->data && (t->ndim < 1 || t->ndim > 4 || numel(t) > 0)); }
-
-moba_status check_3d(const moba_tensor* t, int dtype, View* v) {
-  if (missing(t)) return MOBA_ERR_NULL;
-  if (t->dtype != dtype) return MOBA_ERR_DTYPE;
-  if (t->ndim != 3) return MOBA_ERR_SHAPE;
-  if (t->shape[0] < 0 || t->shape[1] < 1) return MOBA_ERR_SHAPE;
-  if (t->shape[2] != kHeadDim) return MOBA_ERR_UNSUPPORTED;
-  if (t->stride[2] != 1 || t->stride[0] < 0 || t->stride[1] < 0) return MOBA_ERR_LAYOUT;
-  // 16-byte vector accesses: base and both strides must keep rows 16-byte aligned
-  const int64_t per16 = dtype == MOBA_BF16 ? 8 : 4;
-  if ((reinterpret_cast<uintptr_t>(t->data) & 15) != 0 || t->stride[0] % per16 != 0 ||
-      t->stride[1] % per16 != 0)
-    return MOBA_ERR_LAYOUT;
-  v->data = t->data;
-  v->st = t->stride[0];
-  v->sh = t->stride[1];
-  v->H = t->shape[1];
-  return MOBA_OK;
-}
-
-moba_status check_contig(const moba_tensor* t, int dtype, int ndim, const int64_t* shape) {
-  if (missing(t)) return MOBA_ERR_NULL;
-  if (t->dtype != dtype) return MOBA_ERR_DTYPE;
-  if (t->ndim != ndim) return MOBA_ERR_SHAPE;
-  for (int d = 0; d < ndim; d++)
-    if (t->shape[d] != shape[d]) return MOBA_ERR_SHAPE;
-  if (numel(t) == 0) return MOBA_OK;  // strides of an empty tensor are irrelevant
-  int64_t expect = 1;
-  for (int d = ndim - 1; d >= 0; d--) {
-    if (t->shape[d] > 1 && t->stride[d] != expect) return MOBA_ERR_LAYOUT;
-    expect *= shape[d];
-  }
-  return MOBA_OK;
 }
 
 // Whether two [T, H, D] views of elements of `el` bytes may share memory.  Views of
@@ -232,8 +137,6 @@ struct Plan {
   std::vector<KeyTile> ktiles;  // key tiles of the dK/dV kernel (kTilesCur plans)
   int64_t hist_per_head = 0;  // routed history selections of one query head, summed over tokens
 };
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // B = 0 means "one block per sequence" (dense attention).
 void build_plan(const std::vector<int32_t>& cu, int Hq, int Hkv, int B, int topk, TileMode mode,
