@@ -66,7 +66,9 @@
 extern "C" {
 #endif
 
-typedef enum { MOBA_F32 = 0, MOBA_BF16 = 1, MOBA_I32 = 2, MOBA_I64 = 3 } moba_dtype;
+/* MOBA_F8E4M3: 8-bit floats, 4 exponent and 3 mantissa bits, largest 448, no infinities
+ * (only in the paged cache) */
+typedef enum { MOBA_F32 = 0, MOBA_BF16 = 1, MOBA_I32 = 2, MOBA_I64 = 3, MOBA_F8E4M3 = 4 } moba_dtype;
 
 typedef struct {
   void* data;        /* host or device pointer, see each argument */
@@ -273,6 +275,129 @@ moba_status moba_select(const moba_tensor* q, const moba_tensor* k, const moba_t
 moba_status moba_route(const moba_tensor* sel, const moba_tensor* cu_seqlens, int32_t block_size,
                        int32_t num_kv_heads, moba_tensor* counts, moba_tensor* offsets,
                        moba_tensor* entries, hipStream_t stream);
+
+/*
+ * Paged 8-bit cache
+ * -----------------
+ * For serving many requests whose lengths change every step.  A pool of N pages holds
+ * P tokens each (page_size: 64, 128, 192 or 256); a request's pages stand in its row of
+ * a block table.  Lengths, tables and the free list live in device memory and no call
+ * reads them back, allocates, or keeps anything between calls, so a step (plan, write, decode)
+ * can be captured into a HIP graph and replayed while the requests grow.  Calls that
+ * share no memory (workspaces included) may overlap on different streams.  None of the
+ * tensors may overlap another one unless its description says so.
+ *
+ *   k       [N, Hkv, P, 128] f8e4m3; the last two dims contiguous
+ *   v       [N, Hkv, 2 P, 64] f8e4m3: value d of token i of the page at
+ *           [.., 128 (i / 64) + d, i % 64], i.e. 64-token tiles [128, 64] with the token
+ *           index innermost; the last two dims contiguous
+ *   k_scale, v_scale [N, Hkv] f32 contiguous: a page's key is k * k_scale, for all P
+ *           tokens of a kv-head
+ *   k_sum   [N, Hkv, 128] f32 contiguous: the sum of the page's keys as they are held
+ * k and v must be 16-byte aligned with page and head strides that are multiples of 16.
+ * The pool's contents need no initialisation: what a page holds past a request's length is
+ * never used, whatever its bits.
+ */
+typedef struct {
+  const moba_tensor* k;
+  const moba_tensor* v;
+  const moba_tensor* k_scale;
+  const moba_tensor* v_scale;
+  const moba_tensor* k_sum;
+} moba_cache;
+
+/*
+ * Block tables and slot maps of a step, from the requests' lengths.
+ *
+ * add      [S] i32: the tokens request s gets in this step (0: none); negative: the
+ *          request ends
+ * lens     [S] i32: tokens it holds; lens_out [S] i32: after the step (may be lens)
+ * table    [S, W] i32, rows contiguous, any row stride: its pages in order; entries of new
+ *          pages are written, all others stay
+ * free_pages [N] i32, num_free [1] i32: the first num_free entries are the free pages;
+ *          num_free_out [1] i32: after the step (may be num_free)
+ * cu_new   [S + 1] i32, output: exclusive sums of max(add, 0), at most T: request s's new
+ *          tokens are rows cu_new[s] .. cu_new[s + 1] - 1 of the step's arrays
+ * slots    [T] i64, output: page * page_size + offset of every new token, -1 for those of
+ *          refused requests and past the last one
+ * refused  [1] i32, output: requests refused
+ *
+ * The pages of ended requests go back first: they are appended to the free list, request
+ * by request, each one's in order, and their lengths become 0.  New pages are then taken
+ * from the list's end, request by request.  A request is refused, as a whole, where its
+ * pages would not fit its table row or its tokens would end past T; or where it needs pages and the
+ * list does not hold those of every request up to it that was not refused for the first
+ * reason.  A refused request keeps its length, pages and free list untouched; the
+ * caller sees it in lens_out, and in slots.
+ * All tensors are contiguous but for the table's row stride.  S <= 4096, S * W and N below
+ * 2^31.  Lengths below 0 or above W * page_size count as 0 and W * page_size, a num_free outside [0, N]
+ * as the nearer end; pages returned beyond N are dropped.
+ */
+moba_status moba_cache_plan(const moba_tensor* add, const moba_tensor* lens, moba_tensor* table,
+                            moba_tensor* free_pages, const moba_tensor* num_free,
+                            int32_t page_size, moba_tensor* lens_out, moba_tensor* num_free_out,
+                            moba_tensor* cu_new, moba_tensor* slots, moba_tensor* refused,
+                            hipStream_t stream);
+
+/*
+ * Writes new keys and values into their slots, in 8 bits.
+ *
+ * k, v [T, Hkv, 128] bf16 or f32 (the same), last dim contiguous, rows 16-byte aligned;
+ * slots [T] i64 contiguous as moba_cache_plan writes them: a token whose slot is negative or not
+ * of the pool is left out.  The tokens of one page must be consecutive rows with ascending slots
+ * (a run), and the call may hold one run per page; two runs of a page race for it (its
+ * contents are then unspecified, no other page's).
+ *
+ * A run at offset o of its page, n tokens:
+ *   e     = the least integer with max |x| <= 448 * 2^e over its finite values x of the
+ *           kv-head (k and v apart), from -100 up, at most 119 (larger values saturate);
+ *           where o > 0 not less than the exponent the page's scale has
+ *   held  = x * 2^-e rounded to the nearest e4m3 (ties to even); NaN for an x that is
+ *           not finite
+ *   tokens before o are rescaled, with one more such rounding, where e grew; tokens from
+ *   o + n on keep their bits and no longer count
+ *   scale = 2^e,  k_sum = the exact sum over tokens 0 .. o + n - 1, rounded once (NaN if
+ *           one of the keys is NaN)
+ * A power of two costs e4m3 no precision, and rescaling by one none above its subnormals.
+ * Writing the same tokens to the same slots again changes nothing; a request may be cut
+ * back (lens) and written on from any offset.
+ */
+moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const moba_tensor* slots,
+                             const moba_cache* cache, hipStream_t stream);
+
+/*
+ * moba_decode over the paged cache: one new query per request, at the last position of
+ * what the request holds.
+ *
+ * q [S, Hq, 128] bf16; table [S, W] i32 (rows contiguous, any row stride), lens [S] i32.
+ * topk == 0: full attention over the lens[s] tokens; block_size is ignored.
+ * topk >= 1: MoBA with blocks of block_size tokens, a multiple of the page size: a past
+ *   block's score for a query head is <q, sum of its pages' k_sum> (its mean but for a
+ *   common factor), computed in 64 bits, NaN counting as the lowest; the topk - 1 highest (equal
+ *   scores: lower block) and the current block are attended.  A topk of at least
+ *   ceil(W * page_size / block_size) attends everything and runs as topk == 0.  At most
+ *   4096 blocks per table row.
+ * out [S, Hq, 128] bf16 (may be q's own memory, with q's strides), lse [Hq, S] f32.
+ * A request with lens[s] <= 0 (an empty place of the batch) gets out 0 and lse -inf;
+ * lens[s] above W * page_size counts as W * page_size.  The tokens of a table entry outside [0, N)
+ * are left out as if masked (their page's k_sum counts as 0).  Hq / Hkv must not exceed 16.
+ * workspace: moba_cache_decode_workspace_bytes of device memory, 16-byte aligned; it needs no
+ * initialisation and nothing is kept in it after the call.  fp32 softmax and sums; the keys, the
+ * queries and the values enter the matrix cores exactly, the weights as two bf16 terms.
+ * Results do not depend on timing; a request's split over work-groups, and with it its
+ * rounding, depends on the lengths of the whole batch.
+ */
+moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
+                              const moba_tensor* table, const moba_tensor* lens,
+                              int32_t block_size, int32_t topk, moba_tensor* out, moba_tensor* lse,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Workspace of a moba_cache_decode call for S requests with tables W pages wide.  Returns 0
+ * for arguments such a call would refuse, or S == 0.  Host-only arithmetic: no HIP call.
+ */
+size_t moba_cache_decode_workspace_bytes(int64_t S, int64_t W, int32_t Hq, int32_t Hkv,
+                                         int32_t page_size, int32_t block_size, int32_t topk);
 
 /*
  * Workspace sizing query: the device workspace bytes moba_forward needs to

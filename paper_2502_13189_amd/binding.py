@@ -8,17 +8,20 @@ raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+import struct
+from typing import NamedTuple
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoba.so")
 
-MOBA_F32, MOBA_BF16, MOBA_I32, MOBA_I64 = 0, 1, 2, 3
+MOBA_F32, MOBA_BF16, MOBA_I32, MOBA_I64, MOBA_F8E4M3 = 0, 1, 2, 3, 4
 _DT = {torch.float32: MOBA_F32, torch.bfloat16: MOBA_BF16, torch.int32: MOBA_I32,
-       torch.int64: MOBA_I64}
+       torch.int64: MOBA_I64, torch.float8_e4m3fn: MOBA_F8E4M3}
 
 STATUS = ["MOBA_OK", "MOBA_ERR_NULL", "MOBA_ERR_DTYPE", "MOBA_ERR_SHAPE", "MOBA_ERR_LAYOUT",
           "MOBA_ERR_BLOCK_SIZE", "MOBA_ERR_TOPK", "MOBA_ERR_SEQLENS", "MOBA_ERR_UNSUPPORTED",
@@ -73,6 +76,16 @@ def load() -> ctypes.CDLL:
         f.argtypes = args
         f.restype = ctypes.c_int
     i64 = ctypes.c_int64
+    for name, args in {
+        "moba_cache_plan": [vp] * 5 + [i32] + [vp] * 6,
+        "moba_cache_write": [vp] * 5,
+        "moba_cache_decode": [vp] * 4 + [i32, i32] + [vp] * 3 + [ctypes.c_size_t, vp],
+    }.items():
+        f = getattr(lib, name)
+        f.argtypes = args
+        f.restype = ctypes.c_int
+    lib.moba_cache_decode_workspace_bytes.restype = ctypes.c_size_t
+    lib.moba_cache_decode_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
     lib.moba_workspace_bytes.restype = ctypes.c_size_t
     lib.moba_workspace_bytes.argtypes = [i64, i32, i32, i32, i64, i32]
     lib.moba_workspace_held_bytes.restype = ctypes.c_size_t
@@ -300,6 +313,182 @@ def route(sel, cu_seqlens, block_size: int, num_kv_heads: int, stream=None):
     _check("moba_route", lib.moba_route(_ref(ds), _ref(dc), int(block_size), int(num_kv_heads),
                                         _ref(dn), _ref(do), _ref(de), _stream(sel, stream)))
     return counts, offsets, entries
+
+
+class PagedCache(NamedTuple):
+    """A pool of N pages of P tokens (64, 128, 192 or 256) in 8 bits, as include/moba.h
+    describes it.  Every tensor may be a slice of a larger pool (a layer's) whose page
+    and head strides are multiples of 16 bytes; scales and sums are contiguous."""
+    k: torch.Tensor        # [N, Hkv, P, 128] float8_e4m3fn
+    v: torch.Tensor        # [N, Hkv, P // 64, 128, 64] float8_e4m3fn, token index innermost
+    k_scale: torch.Tensor  # [N, Hkv] fp32: the page's keys are k * k_scale
+    v_scale: torch.Tensor  # [N, Hkv] fp32
+    k_sum: torch.Tensor    # [N, Hkv, 128] fp32, the sum of the page's keys
+
+
+class CachePlan(NamedTuple):
+    """What cache_plan() returns."""
+    cu_new: torch.Tensor    # [S + 1] int32: request s's new tokens are rows cu_new[s] ..
+    slots: torch.Tensor     # [num_tokens] int64: every new token's slot, -1: none
+    lens: torch.Tensor      # [S] int32: lengths after the step
+    num_free: torch.Tensor  # [1] int32: free pages after the step
+    refused: torch.Tensor   # [1] int32: requests refused
+
+
+# moba_tensor: data, dtype, ndim, shape[4], stride[4]
+_DESC = struct.Struct("=Qii8q")
+_PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())
+
+
+class _Descs:
+    """Descriptors of several tensors of one device in one block of memory; at(i) is the
+    address of the i-th.  (Packed: a step's calls are short, and filling a MobaTensor field by
+    field takes several times as long.)"""
+
+    def __init__(self, tensors):
+        device = tensors[0].device
+        if device.type != "cuda":
+            raise ValueError("the paged cache's tensors live on a GPU")
+        parts = []
+        for t in tensors:
+            if t.device != device:
+                raise ValueError("tensors on %s and on %s" % (device, t.device))
+            shape, stride = tuple(t.shape), t.stride()
+            n = len(shape)
+            if n == 5:  # V pages: the tiles' rows one after the other
+                if stride[3] != shape[4] or (shape[2] > 1 and stride[2] != shape[3] * stride[3]):
+                    raise ValueError("v's last three dims must be contiguous")
+                shape = (shape[0], shape[1], shape[2] * shape[3], shape[4])
+                stride = (stride[0], stride[1], stride[3], stride[4])
+                n = 4
+            elif n > 4:
+                raise ValueError("at most 4 dimensions")
+            dt = _DT.get(t.dtype)
+            if dt is None:
+                raise TypeError("unsupported dtype %s" % t.dtype)
+            parts.append(_DESC.pack(t.data_ptr(), dt, n, *shape, *_PAD[n], *stride, *_PAD[n]))
+        self._buf = ctypes.create_string_buffer(b"".join(parts))
+        self._base = ctypes.addressof(self._buf)
+
+    def at(self, i: int) -> int:
+        return self._base + i * _DESC.size
+
+    def cache(self, i: int):
+        """moba_cache of five tensors from the i-th on."""
+        return (ctypes.c_void_p * 5)(*(self.at(i + j) for j in range(5)))
+
+
+def _call(fn: str, t: torch.Tensor, stream, *args):
+    """Calls fn with the device of t current, on `stream` or that device's current one."""
+    if t.device.index == torch.cuda.current_device():
+        status = getattr(load(), fn)(*args, _stream(t, stream))
+    else:
+        with torch.cuda.device(t.device):
+            status = getattr(load(), fn)(*args, _stream(t, stream))
+    _check(fn, status)
+
+
+def _allocating(stream):
+    """Where a call's own tensors are allocated: for the stream that it runs on, so that
+    memory it drops is not given out again before the call is done with it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
+
+
+def cache_new(num_pages: int, num_kv_heads: int, page_size: int = 64, device="cuda") -> PagedCache:
+    """An empty pool of pages (uninitialised memory: nothing reads what was not written)."""
+    if page_size not in (64, 128, 192, 256):
+        raise ValueError("page_size must be 64, 128, 192 or 256")
+    f8 = dict(dtype=torch.float8_e4m3fn, device=device)
+    f32 = dict(dtype=torch.float32, device=device)
+    n, h = int(num_pages), int(num_kv_heads)
+    return PagedCache(torch.empty((n, h, page_size, 128), **f8),
+                      torch.empty((n, h, page_size // 64, 128, 64), **f8),
+                      torch.empty((n, h), **f32), torch.empty((n, h), **f32),
+                      torch.empty((n, h, 128), **f32))
+
+
+def cache_plan(add, lens, table, free_pages, num_free, page_size: int, num_tokens: int,
+               lens_out=None, num_free_out=None, cu_new=None, slots=None, refused=None,
+               stream=None) -> CachePlan:
+    """Block tables and slot maps of a serving step, on the GPU from the requests' lengths.
+
+    add [S] int32: new tokens per request (0: none, negative: the request ends); lens [S]
+    int32: tokens held; table [S, W] int32 and free_pages [N] int32 are updated in place (the
+    first num_free[0] entries are free); num_tokens: rows of the step's arrays, at least
+    the new tokens'.  Requests that do not fit are refused whole (their slots are -1).
+    lens_out and num_free_out may be lens and num_free themselves: a captured step then
+    carries its state from replay to replay."""
+    S = add.shape[0]
+    if slots is not None and slots.shape[0] != num_tokens:
+        raise ValueError("slots has %d rows, num_tokens is %d" % (slots.shape[0], num_tokens))
+    i32 = dict(dtype=torch.int32, device=add.device)
+    with _allocating(stream):
+        if lens_out is None:
+            lens_out = torch.empty((S,), **i32)
+        if num_free_out is None:
+            num_free_out = torch.empty((1,), **i32)
+        if cu_new is None:
+            cu_new = torch.empty((S + 1,), **i32)
+        if slots is None:
+            slots = torch.empty((int(num_tokens),), dtype=torch.int64, device=add.device)
+        if refused is None:
+            refused = torch.empty((1,), **i32)
+    d = _Descs((add, lens, table, free_pages, num_free, lens_out, num_free_out, cu_new, slots,
+                refused))
+    _call("moba_cache_plan", add, stream, d.at(0), d.at(1), d.at(2), d.at(3), d.at(4),
+          int(page_size), d.at(5), d.at(6), d.at(7), d.at(8), d.at(9))
+    return CachePlan(cu_new, slots, lens_out, num_free_out, refused)
+
+
+def cache_write(k, v, slots, cache: PagedCache, stream=None) -> None:
+    """Quantises new keys and values [T, Hkv, 128] (bf16 or fp32) into their slots [T]
+    int64 (negative: left out), as cache_plan() gives them: a page's tokens are
+    consecutive rows with ascending slots."""
+    d = _Descs((k, v, slots, *cache))
+    c = d.cache(3)
+    _call("moba_cache_write", k, stream, d.at(0), d.at(1), d.at(2), ctypes.addressof(c))
+
+
+def cache_decode_workspace_bytes(num_requests: int, table_width: int, num_q_heads: int,
+                                 num_kv_heads: int, page_size: int, block_size: int,
+                                 topk: int) -> int:
+    """Bytes of cache_decode()'s workspace (0: such a call would be refused)."""
+    return int(load().moba_cache_decode_workspace_bytes(
+        int(num_requests), int(table_width), int(num_q_heads), int(num_kv_heads), int(page_size),
+        int(block_size), int(topk)))
+
+
+def cache_decode(q, cache: PagedCache, table, lens, block_size: int, topk: int, out=None, lse=None,
+                 workspace=None, stream=None):
+    """decode() over a paged 8-bit cache: one new query per request (topk == 0: full
+    attention) at the last position of the lens[s] tokens it holds.  q [S, Hq, 128] bf16,
+    table [S, W] int32, lens [S] int32; block_size is a multiple of the page size.  A request
+    with lens[s] <= 0 gets out 0 and lse -inf.  workspace: uint8, at least
+    cache_decode_workspace_bytes() of it; by default a fresh one per call, so that calls on
+    several streams and captured graphs share nothing.  Returns (out [S, Hq, 128], lse
+    [Hq, S])."""
+    S, Hq = q.shape[0], q.shape[1]
+    if workspace is not None and (workspace.device != q.device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be contiguous and on q's device")
+    with _allocating(stream):
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if lse is None:
+            lse = torch.empty((Hq, S), dtype=torch.float32, device=q.device)
+        if workspace is None:
+            n = cache_decode_workspace_bytes(S, table.shape[1], Hq, cache.k.shape[1],
+                                             cache.k.shape[2], block_size, topk)
+            workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
+    d = _Descs((q, table, lens, out, lse, *cache))
+    c = d.cache(5)
+    _call("moba_cache_decode", q, stream, d.at(0), ctypes.addressof(c), d.at(1), d.at(2),
+          int(block_size), int(topk), d.at(3), d.at(4), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size())
+    return out, lse
 
 
 def workspace_bytes(T: int, num_q_heads: int, num_kv_heads: int, nblk_total: int, topk: int,

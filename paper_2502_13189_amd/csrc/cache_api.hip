@@ -1,0 +1,278 @@
+// Host side of the paged 8-bit cache: argument validation, the layout of the caller's
+// workspace and the launches.  Nothing here allocates, synchronizes or reads device memory.
+#include "api_common.h"
+#include "cache_internal.h"
+#include "decode_internal.h"
+
+#include <cmath>
+#include <type_traits>
+
+using namespace moba;
+
+namespace {
+
+bool page_size_ok(int64_t P) {
+  return P >= kCacheTile && P <= kCacheMaxPage && P % kCacheTile == 0;
+}
+
+// A [shape] tensor of the pool whose last two dims are contiguous, in 16-byte steps.
+moba_status check_pages(const moba_tensor* t, int64_t N, int64_t Hkv, int64_t rows, int64_t cols,
+                        uint8_t** data, int64_t* sp, int64_t* sh) {
+  if (t->dtype != MOBA_F8E4M3) return MOBA_ERR_DTYPE;
+  if (t->ndim != 4 || t->shape[0] != N || t->shape[1] != Hkv || t->shape[2] != rows ||
+      t->shape[3] != cols)
+    return MOBA_ERR_SHAPE;
+  if (t->stride[3] != 1 || t->stride[2] != cols || t->stride[0] < 0 || t->stride[1] < 0 ||
+      t->stride[0] % 16 != 0 || t->stride[1] % 16 != 0 ||
+      (reinterpret_cast<uintptr_t>(t->data) & 15) != 0)
+    return MOBA_ERR_LAYOUT;
+  *data = static_cast<uint8_t*>(t->data);
+  *sp = t->stride[0];
+  *sh = t->stride[1];
+  return MOBA_OK;
+}
+
+moba_status check_cache(const moba_cache* c, CachePool* p) {
+  if (!c || missing(c->k) || missing(c->v) || missing(c->k_scale) || missing(c->v_scale) ||
+      missing(c->k_sum))
+    return MOBA_ERR_NULL;
+  if (c->k->dtype != MOBA_F8E4M3) return MOBA_ERR_DTYPE;
+  if (c->k->ndim != 4 || c->k->shape[0] < 1 || c->k->shape[1] < 1) return MOBA_ERR_SHAPE;
+  const int64_t N = c->k->shape[0], Hkv = c->k->shape[1], P = c->k->shape[2];
+  if (c->k->shape[3] != kHeadDim || !page_size_ok(P)) return MOBA_ERR_UNSUPPORTED;
+  if (N >= (int64_t(1) << 31) || Hkv >= (int64_t(1) << 20)) return MOBA_ERR_UNSUPPORTED;
+  moba_status st;
+  if ((st = check_pages(c->k, N, Hkv, P, kHeadDim, &p->k, &p->k_sp, &p->k_sh)) != MOBA_OK) return st;
+  if ((st = check_pages(c->v, N, Hkv, P / kCacheTile * kHeadDim, kCacheTile, &p->v, &p->v_sp,
+                        &p->v_sh)) != MOBA_OK)
+    return st;
+  const int64_t sums[3] = {N, Hkv, kHeadDim};
+  if ((st = check_contig(c->k_scale, MOBA_F32, 2, sums)) != MOBA_OK) return st;
+  if ((st = check_contig(c->v_scale, MOBA_F32, 2, sums)) != MOBA_OK) return st;
+  if ((st = check_contig(c->k_sum, MOBA_F32, 3, sums)) != MOBA_OK) return st;
+  p->k_scale = static_cast<float*>(c->k_scale->data);
+  p->v_scale = static_cast<float*>(c->v_scale->data);
+  p->k_sum = static_cast<float*>(c->k_sum->data);
+  p->N = (int)N;
+  p->Hkv = (int)Hkv;
+  p->P = (int)P;
+  return MOBA_OK;
+}
+
+// table [S, W] i32, rows contiguous
+moba_status check_table(const moba_tensor* t, int64_t S) {
+  if (t->dtype != MOBA_I32) return MOBA_ERR_DTYPE;
+  if (t->ndim != 2 || t->shape[0] != S || t->shape[1] < 1) return MOBA_ERR_SHAPE;
+  if (S * t->shape[1] >= (int64_t(1) << 31)) return MOBA_ERR_UNSUPPORTED;
+  if (S == 0) return MOBA_OK;  // (strides of an empty tensor are irrelevant)
+  if ((t->shape[1] > 1 && t->stride[1] != 1) || (S > 1 && t->stride[0] < t->shape[1]))
+    return MOBA_ERR_LAYOUT;
+  return MOBA_OK;
+}
+
+struct DecodeShape {
+  int64_t S, W;
+  int Hq, Hkv, P, B, topk;
+  bool full;
+  int nblk, nlist;          // MoBA
+  int shares, gate_shares;
+};
+
+// What a call of these sizes takes; fills the workspace's pointers from `base` (which may
+// be null) and returns its bytes.
+size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
+  size_t off = 0;
+  const auto take = [&](auto** p, int64_t n) {
+    *p = reinterpret_cast<std::remove_reference_t<decltype(*p)>>(base + off);
+    off += ((size_t)n * sizeof(**p) + 15) / 16 * 16;
+  };
+  const int64_t G = d.Hq / d.Hkv, pg = d.full ? d.Hkv : 1;
+  take(&a->part_o, (int64_t)d.shares * 2 * pg * G * kHeadDim);
+  take(&a->part_ml, (int64_t)d.shares * 2 * pg * G);
+  take(&a->join, (int64_t)d.shares * pg);
+  if (!d.full) {
+    take(&a->score, d.topk > 1 ? d.S * d.Hq * d.nblk : 0);
+    take(&a->list, d.S * d.Hkv * d.nlist);
+    take(&a->nsteps, d.S * d.Hkv);
+  }
+  return off;
+}
+
+// Checks the sizes and settles how the call runs.
+moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t P, int32_t block_size,
+                         int32_t topk, DecodeShape* d) {
+  if (S < 0 || W < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return MOBA_ERR_SHAPE;
+  if (!page_size_ok(P) || Hq / Hkv > kDecodeMaxGroup) return MOBA_ERR_UNSUPPORTED;
+  if (topk < 0) return MOBA_ERR_TOPK;
+  if (topk > 0 && (block_size < 1 || block_size % P != 0)) return MOBA_ERR_BLOCK_SIZE;
+  if (Hq >= (int64_t(1) << 20) || W >= (int64_t(1) << 31) || S >= (int64_t(1) << 31) ||
+      S * W >= (int64_t(1) << 31) || S * Hq >= (int64_t(1) << 31))
+    return MOBA_ERR_UNSUPPORTED;
+  d->S = S;
+  d->W = W;
+  d->Hq = (int)Hq;
+  d->Hkv = (int)Hkv;
+  d->P = (int)P;
+  const int64_t nblk = topk > 0 ? ceil_div(W * P, block_size) : 1;
+  d->full = topk == 0 || topk >= nblk;
+  d->B = d->full ? 0 : block_size;
+  d->topk = d->full ? 0 : topk;
+  if (!d->full && nblk > kMaxBlocksPerSeq) return MOBA_ERR_UNSUPPORTED;
+  d->nblk = (int)nblk;
+  d->nlist = d->full ? 0 : (int)std::min<int64_t>(nblk, Hq / Hkv * (topk - 1) + 1);
+  const int64_t steps = S * W * (P / kCacheTile);  // at most, of a kv-head
+  const int64_t each = std::max<int64_t>(1, kCacheWaves / Hkv);
+  d->shares = (int)(d->full ? std::min<int64_t>(each, std::max<int64_t>(steps, 1))
+                            : std::min<int64_t>(kCacheWaves, std::max<int64_t>(steps * Hkv, 1)));
+  d->gate_shares = (int)std::min<int64_t>(each, std::max<int64_t>(S * nblk, 1));
+  return MOBA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+moba_status moba_cache_plan(const moba_tensor* add, const moba_tensor* lens, moba_tensor* table,
+                            moba_tensor* free_pages, const moba_tensor* num_free,
+                            int32_t page_size, moba_tensor* lens_out, moba_tensor* num_free_out,
+                            moba_tensor* cu_new, moba_tensor* slots, moba_tensor* refused,
+                            hipStream_t stream) {
+  if (missing(add) || missing(lens) || missing(table) || missing(free_pages) || missing(num_free) ||
+      missing(lens_out) || missing(num_free_out) || missing(cu_new) || missing(slots) ||
+      missing(refused))
+    return MOBA_ERR_NULL;
+  if (add->dtype != MOBA_I32 || free_pages->dtype != MOBA_I32 || slots->dtype != MOBA_I64)
+    return MOBA_ERR_DTYPE;
+  if (add->ndim != 1 || free_pages->ndim != 1 || slots->ndim != 1 || add->shape[0] < 0 ||
+      free_pages->shape[0] < 0 || slots->shape[0] < 0)
+    return MOBA_ERR_SHAPE;
+  const int64_t S = add->shape[0], N = free_pages->shape[0], T = slots->shape[0];
+  const int64_t one = 1, s1 = S + 1;
+  moba_status st;
+  if ((st = check_contig(add, MOBA_I32, 1, &S)) != MOBA_OK) return st;
+  if ((st = check_contig(lens, MOBA_I32, 1, &S)) != MOBA_OK) return st;
+  if ((st = check_contig(lens_out, MOBA_I32, 1, &S)) != MOBA_OK) return st;
+  if ((st = check_table(table, S)) != MOBA_OK) return st;
+  if ((st = check_contig(free_pages, MOBA_I32, 1, &N)) != MOBA_OK) return st;
+  if ((st = check_contig(num_free, MOBA_I32, 1, &one)) != MOBA_OK) return st;
+  if ((st = check_contig(num_free_out, MOBA_I32, 1, &one)) != MOBA_OK) return st;
+  if ((st = check_contig(cu_new, MOBA_I32, 1, &s1)) != MOBA_OK) return st;
+  if ((st = check_contig(slots, MOBA_I64, 1, &T)) != MOBA_OK) return st;
+  if ((st = check_contig(refused, MOBA_I32, 1, &one)) != MOBA_OK) return st;
+  if (page_size < 1) return MOBA_ERR_BLOCK_SIZE;
+  if (!page_size_ok(page_size) || S > kPlanMaxRequests || N >= (int64_t(1) << 31) ||
+      T >= (int64_t(1) << 31))
+    return MOBA_ERR_UNSUPPORTED;
+  CachePlanArgs a{};
+  a.add = static_cast<const int32_t*>(add->data);
+  a.lens = static_cast<const int32_t*>(lens->data);
+  a.table = static_cast<int32_t*>(table->data);
+  a.t_ss = table->stride[0];
+  a.free_pages = static_cast<int32_t*>(free_pages->data);
+  a.num_free = static_cast<const int32_t*>(num_free->data);
+  a.lens_out = static_cast<int32_t*>(lens_out->data);
+  a.num_free_out = static_cast<int32_t*>(num_free_out->data);
+  a.cu = static_cast<int32_t*>(cu_new->data);
+  a.slots = static_cast<int64_t*>(slots->data);
+  a.refused = static_cast<int32_t*>(refused->data);
+  a.S = (int)S;
+  a.W = (int)table->shape[1];
+  a.N = (int)N;
+  a.P = page_size;
+  a.T = T;
+  Phase ph("cache_plan", stream);
+  MOBA_LAUNCH(launch_cache_plan(a, stream));
+  return MOBA_OK;
+}
+
+moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const moba_tensor* slots,
+                             const moba_cache* cache, hipStream_t stream) {
+  if (missing(k) || missing(v) || missing(slots)) return MOBA_ERR_NULL;
+  CacheWriteArgs a{};
+  moba_status st;
+  if ((st = check_cache(cache, &a.c)) != MOBA_OK) return st;
+  if (k->dtype != MOBA_BF16 && k->dtype != MOBA_F32) return MOBA_ERR_DTYPE;
+  View vk, vv;
+  if ((st = check_3d(k, k->dtype, &vk)) != MOBA_OK) return st;
+  if ((st = check_3d(v, k->dtype, &vv)) != MOBA_OK) return st;
+  const int64_t T = k->shape[0];
+  if (k->shape[1] != a.c.Hkv || v->shape[0] != T || v->shape[1] != a.c.Hkv) return MOBA_ERR_SHAPE;
+  if ((st = check_contig(slots, MOBA_I64, 1, &T)) != MOBA_OK) return st;
+  if (T >= (int64_t(1) << 31) || T * a.c.Hkv >= (int64_t(1) << 32)) return MOBA_ERR_UNSUPPORTED;
+  if (T == 0) return MOBA_OK;
+  a.k = vk.data; a.k_st = vk.st; a.k_sh = vk.sh;
+  a.v = vv.data; a.v_st = vv.st; a.v_sh = vv.sh;
+  a.slots = static_cast<const int64_t*>(slots->data);
+  a.T = T;
+  Phase ph("cache_write", stream);
+  MOBA_LAUNCH(launch_cache_write(k->dtype == MOBA_BF16, a, stream));
+  return MOBA_OK;
+}
+
+size_t moba_cache_decode_workspace_bytes(int64_t S, int64_t W, int32_t Hq, int32_t Hkv,
+                                         int32_t page_size, int32_t block_size, int32_t topk) {
+  DecodeShape d{};
+  if (decode_shape(S, W, Hq, Hkv, page_size, block_size, topk, &d) != MOBA_OK || S == 0) return 0;
+  CacheDecodeArgs a{};
+  return decode_layout(d, nullptr, &a);
+}
+
+moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
+                              const moba_tensor* table, const moba_tensor* lens,
+                              int32_t block_size, int32_t topk, moba_tensor* out, moba_tensor* lse,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (missing(q) || missing(table) || missing(lens) || missing(out) || missing(lse))
+    return MOBA_ERR_NULL;
+  CacheDecodeArgs a{};
+  moba_status st;
+  if ((st = check_cache(cache, &a.c)) != MOBA_OK) return st;
+  View vq, vo;
+  if ((st = check_3d(q, MOBA_BF16, &vq)) != MOBA_OK) return st;
+  if ((st = check_3d(out, MOBA_BF16, &vo)) != MOBA_OK) return st;
+  const int64_t S = q->shape[0], Hq = q->shape[1];
+  if (out->shape[0] != S || out->shape[1] != Hq || Hq % a.c.Hkv != 0) return MOBA_ERR_SHAPE;
+  const int64_t lshape[2] = {Hq, S};
+  if ((st = check_contig(lse, MOBA_F32, 2, lshape)) != MOBA_OK) return st;
+  if ((st = check_table(table, S)) != MOBA_OK) return st;
+  if ((st = check_contig(lens, MOBA_I32, 1, &S)) != MOBA_OK) return st;
+  DecodeShape d{};
+  if ((st = decode_shape(S, table->shape[1], Hq, a.c.Hkv, a.c.P, block_size, topk, &d)) != MOBA_OK)
+    return st;
+  if (S == 0) return MOBA_OK;
+  if (!workspace) return MOBA_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return MOBA_ERR_LAYOUT;
+  if (workspace_bytes < decode_layout(d, static_cast<char*>(workspace), &a))
+    return MOBA_ERR_NO_MEMORY;
+  a.q = static_cast<const __hip_bfloat16*>(vq.data); a.q_ss = vq.st; a.q_sh = vq.sh;
+  a.out = static_cast<__hip_bfloat16*>(vo.data); a.o_ss = vo.st; a.o_sh = vo.sh;
+  a.lse = static_cast<float*>(lse->data);
+  a.table = static_cast<const int32_t*>(table->data);
+  a.t_ss = table->stride[0];
+  a.lens = static_cast<const int32_t*>(lens->data);
+  a.S = (int)S;
+  a.W = (int)d.W;
+  a.Hq = d.Hq;
+  a.G = d.Hq / d.Hkv;
+  a.B = d.B;
+  a.topk = d.topk;
+  a.nblk = d.nblk;
+  a.nlist = d.nlist;
+  a.shares = d.shares;
+  a.gate_shares = d.gate_shares;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)kHeadDim));
+  if (!d.full) {
+    if (d.topk > 1) {
+      Phase ph("cache_gate", stream);
+      MOBA_LAUNCH(launch_cache_gate(a, stream));
+    }
+    Phase ph("cache_select", stream);
+    MOBA_LAUNCH(launch_cache_select(a, stream));
+  }
+  { Phase ph("cache_attend", stream);
+    MOBA_LAUNCH(launch_cache_attend(d.full, a, stream)); }
+  { Phase ph("cache_join", stream);
+    MOBA_LAUNCH(launch_cache_join(d.full, a, stream)); }
+  return MOBA_OK;
+}
+
+}  // extern "C"

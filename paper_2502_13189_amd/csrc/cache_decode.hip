@@ -1,0 +1,611 @@
+// Decode over the paged 8-bit cache: one new query per request, full attention or MoBA.
+//
+// Every attended key and value is one byte per dim, read once per kv-head for all query
+// heads of its group: 256 bytes for at most 4 x 128 x 16 FLOP, so HBM bounds it.
+//
+// Lengths are known on the device alone.  The batch's keys are cut into 64-key steps and the
+// steps, request after request, into equal shares, one wave each, as many as the chip
+// holds; every wave finds its own share from a prefix sum over the lengths.  So a ragged batch, one long
+// request and many short ones all keep the chip evenly busy, and the workspace does not depend on
+// lengths: a share leaves at most two partial rows (the one it enters with and the one it leaves
+// with), which a second launch joins; a row inside one share is finished there.
+//
+//   attend  a step's K and V go from memory to the matrix cores through registers alone.
+//           S^T = K q^T on 16x16x32 MFMAs: a lane has 16 bytes of a key for two operands.
+//           The keys of a step are dealt to the four 16-key operands so that a lane's 16
+//           scores of a head are 16 consecutive tokens, which is what it then needs as the
+//           operand of O^T = V^T P^T, with V's 16 tokens of a dim being one 16-byte load of the
+//           page's token-minor tile.  e4m3 is exact in bf16; the weights enter as a bf16 and
+//           the bf16 of its remainder, the scales through the logits and the weights.
+//   gate    MoBA: a wave adds a block's k_sum rows and takes its scores with the group's
+//           heads, in 64 bits
+//   select  MoBA: a wave finds the (k-1)-th highest score of a head bit by bit; the group's
+//           heads' blocks become one ascending list with a mask of heads for each
+//   join    log-sum-exp merge of split rows
+#include "cache_internal.h"
+
+#include <math.h>
+
+namespace moba {
+namespace {
+
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kRescale = 8.0f;  // a running max may lag by 2^8 before sums are rescaled
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+// Eight e4m3 codes to eight bf16, exactly.
+__device__ __forceinline__ bf16x8_t to_bf16(uint32_t a, uint32_t b) {
+  union {
+    bf16x2_t h[4];
+    bf16x8_t v;
+  } r;
+  r.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
+  r.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+  r.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
+  r.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+  return r.v;
+}
+
+// Tokens request s attends.
+__device__ __forceinline__ int held(const CacheDecodeArgs& a, int s) {
+  return (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.W * a.c.P);
+}
+
+// ------------------------------------------------------------------ shares
+// The rows' units in a sum over all rows: pre[i] units lie before the i-th of the 256
+// groups of `per` rows.
+struct Sums {
+  int64_t pre[kCacheDecodeThreads];
+  int64_t part[kCacheDecodeThreads / 64];
+  int64_t total;
+};
+
+template <typename F>
+__device__ __forceinline__ void sum_rows(Sums& sm, int rows, F units) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (rows + kCacheDecodeThreads - 1) / kCacheDecodeThreads;
+  int64_t mine = 0;
+  for (int i = 0, r = tid * per; i < per && r < rows; i++, r++) mine += units(r);
+  int64_t x = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t o = __shfl_up((long long)x, d, 64);
+    if (lane >= d) x += o;
+  }
+  if (lane == 63) sm.part[wave] = x;
+  __syncthreads();
+  for (int w = 0; w < wave; w++) x += sm.part[w];
+  sm.pre[tid] = x - mine;
+  if (tid == kCacheDecodeThreads - 1) sm.total = x;
+  __syncthreads();
+}
+
+// The row that unit u (< total) belongs to, for a whole wave; base: units before the row.
+template <typename F>
+__device__ __forceinline__ int find_row(const Sums& sm, int rows, int64_t u, F units, int64_t* base) {
+  const int lane = threadIdx.x & 63;
+  const int per = (rows + kCacheDecodeThreads - 1) / kCacheDecodeThreads;
+  int below = 0;  // groups that begin at or before u
+#pragma unroll
+  for (int i = 0; i < kCacheDecodeThreads / 64; i++)
+    below += __popcll(__ballot(sm.pre[64 * i + lane] <= u));
+  const int r0 = (below - 1) * per, r1 = min(r0 + per, rows);
+  int64_t acc = sm.pre[below - 1];
+  for (int r = r0; r < r1; r += 64) {
+    const int64_t n = r + lane < r1 ? units(r + lane) : 0;
+    int64_t x = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t o = __shfl_up((long long)x, d, 64);
+      if (lane >= d) x += o;
+    }
+    const unsigned long long past = __ballot(acc + x > u);
+    if (past) {
+      const int at = __ffsll((long long)past) - 1;
+      *base = acc + __shfl((long long)(x - n), at, 64);
+      return r + at;
+    }
+    acc += __shfl((long long)x, 63, 64);
+  }
+  *base = 0;  // (not reached: u < total)
+  return rows;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// ------------------------------------------------------------------ attend
+// A step: 64 keys of one page.
+struct Step {
+  int64_t page;   // 0 where the table's entry is none of the pool
+  int tile;       // 64-token tile of the page
+  int nk;         // keys attended: the step's first nk
+  uint32_t heads; // of the group, that attend it
+};
+
+struct Tile {
+  u32x4_t k[4][2];  // operand t, dims 64 j + 16 (lane / 16)
+  u32x4_t v[8];     // dim 16 i + lane % 16, tokens 16 (lane / 16) ..
+  float ks, vs;
+};
+
+template <bool MOBA>
+__global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(CacheDecodeArgs a) {
+  __shared__ Sums sums;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const CachePool& c = a.c;
+  const int Hkv = c.Hkv, G = a.G, P = c.P;
+  const int rows = MOBA ? a.S * Hkv : a.S;
+  const auto units = [&](int r) -> int64_t {
+    if constexpr (MOBA) return a.nsteps[r];
+    else return (held(a, r) + kCacheTile - 1) / kCacheTile;
+  };
+  sum_rows(sums, rows, units);
+  const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
+  // rows that attend nothing
+  for (int r = w; r < a.S * Hkv; r += gridDim.x * (kCacheDecodeThreads / 64)) {
+    const int s = r / Hkv, h0 = r % Hkv * G;
+    if (a.lens[s] > 0) continue;
+    for (int h = h0; h < h0 + G; h++) {
+      *reinterpret_cast<uint32_t*>(a.out + s * a.o_ss + h * a.o_sh + 2 * lane) = 0;
+      if (lane == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
+    }
+  }
+  const int share = MOBA ? w : w / Hkv;
+  int g = MOBA ? 0 : w % Hkv;
+  if (share >= a.shares) return;
+  const int pg = MOBA ? 1 : Hkv, pi = MOBA ? 0 : g;  // partials: kv-heads per share, this one
+  const int64_t total = uniform(sums.total);
+  const int64_t per_share = (total + a.shares - 1) / a.shares;
+  const int64_t u_end = min((share + 1) * per_share, total);
+  int64_t u = share * per_share;
+  CacheJoin join = {-1, 0};
+  if (u < u_end) {
+    int64_t base;
+    int r = find_row(sums, rows, u, units, &base);
+    r = __builtin_amdgcn_readfirstlane(r);
+    base = uniform(base);
+    const int hc = lane & 15, quad = lane >> 4;
+    const int spb = MOBA ? a.B / kCacheTile : 0;  // steps per block
+    const int koff = (16 * (hc >> 2) + (hc & 3)) * kHeadDim + 16 * quad;
+    const int voff = hc * kCacheTile + 16 * quad;
+    while (u < u_end) {
+      const int64_t n = uniform(units(r));
+      if (n == 0) {
+        r++;
+        continue;
+      }
+      const int s = MOBA ? r / Hkv : r;
+      if constexpr (MOBA) g = r % Hkv;
+      const int len = held(a, s);
+      const int first = (int)(u - base), last = (int)min(n, u_end - base);
+      const int32_t* row = a.table + s * a.t_ss;
+      const uint32_t* list = MOBA ? a.list + (int64_t)r * a.nlist : nullptr;
+      // B operands: q of head hc, the dims of the K operands
+      bf16x8_t qb[4];
+      {
+        const __hip_bfloat16* qp = a.q + s * a.q_ss + (int64_t)(g * G + min(hc, G - 1)) * a.q_sh;
+#pragma unroll
+        for (int f = 0; f < 4; f++)
+          qb[f] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(
+                                                   qp + 64 * (f >> 1) + 16 * quad + 8 * (f & 1)));
+      }
+      const auto step_at = [&](int x) {
+        Step st;
+        int tok = kCacheTile * x;
+        st.heads = 0xffffu;
+        if constexpr (MOBA) {
+          const int bi = x / spb;
+          const uint32_t e = list[bi];
+          tok = (int)(e & 0xffffu) * a.B + kCacheTile * (x - bi * spb);
+          st.heads = e >> 16;
+        }
+        const int pn = tok / P;
+        const int id = row[pn];
+        const bool ok = (uint32_t)id < (uint32_t)c.N;
+        st.page = ok ? id : 0;
+        st.tile = (tok - pn * P) / kCacheTile;
+        st.nk = ok ? min(kCacheTile, len - tok) : 0;
+        return st;
+      };
+      const auto load = [&](Tile& t, const Step& st) {
+        const uint8_t* kp = c.k + st.page * c.k_sp + g * c.k_sh + st.tile * (kCacheTile * kHeadDim);
+        const uint8_t* vp = c.v + st.page * c.v_sp + g * c.v_sh + st.tile * (kCacheTile * kHeadDim);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int j = 0; j < 2; j++)
+            t.k[i][j] = *reinterpret_cast<const u32x4_t*>(kp + koff + 4 * kHeadDim * i + 64 * j);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+          t.v[i] = *reinterpret_cast<const u32x4_t*>(vp + voff + 16 * kCacheTile * i);
+        t.ks = c.k_scale[st.page * Hkv + g];
+        t.vs = c.v_scale[st.page * Hkv + g];
+      };
+      f32x4_t acc[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) acc[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      float m = -INFINITY, l = 0.0f;
+      const auto fold = [&](Tile& t, const Step& st) {
+        // a lane's scores: head hc, tokens 16 quad + 4 i + e
+        float z[16];
+        const float zs = t.ks * a.scale_log2;
+        const bool mine = !MOBA || ((st.heads >> hc) & 1);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int f = 0; f < 4; f++) {
+            const u32x4_t kw = t.k[i][f >> 1];
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                f & 1 ? to_bf16(kw[2], kw[3]) : to_bf16(kw[0], kw[1]), qb[f], x, 0, 0, 0);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; e++) z[4 * i + e] = x[e] * zs;
+        }
+        if (st.nk < kCacheTile) {
+          const int left = st.nk - 16 * quad;  // of this lane's tokens
+          if (st.nk <= 0) t.vs = 0.0f;  // (no page: its scale may be anything, too)
+#pragma unroll
+          for (int i = 0; i < 16; i++) z[i] = i < left ? z[i] : -INFINITY;
+          // their values may hold anything
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+              const int n = min(max(left - 4 * e, 0), 4);
+              t.v[i][e] &= n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
+            }
+        }
+        if constexpr (MOBA) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) z[i] = mine ? z[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i++) top = fmaxf(top, z[i]);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (__ballot(top > m + kRescale || (m == -INFINITY && top > -INFINITY))) {
+          const float mn = fmaxf(m, top);
+          const float sc = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+          m = mn;
+          l *= sc;
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) acc[i][e] *= sc;
+        }
+        const float mr = m == -INFINITY ? 0.0f : m;
+        // weights times the page's scale, as two bf16 terms
+        u32x4_t hi[2], lo[2];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const float p0 = __builtin_amdgcn_exp2f(z[2 * i] - mr);
+          const float p1 = __builtin_amdgcn_exp2f(z[2 * i + 1] - mr);
+          l += p0 + p1;
+          const float v0 = p0 * t.vs, v1 = p1 * t.vs;
+          const uint32_t h = pack_bf16(v0, v1);
+          hi[i >> 2][i & 3] = h;
+          lo[i >> 2][i & 3] = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+#pragma unroll
+          for (int f = 0; f < 2; f++) {
+            const bf16x8_t vb = to_bf16(t.v[i][2 * f], t.v[i][2 * f + 1]);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, hi[f]),
+                                                             acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, lo[f]),
+                                                             acc[i], 0, 0, 0);
+          }
+        }
+      };
+      for (int x = first; x < last; x++) {
+        const Step st = step_at(x);
+        Tile t;
+        load(t, st);
+        fold(t, st);
+      }
+      l += __shfl_xor(l, 16, 64);
+      l += __shfl_xor(l, 32, 64);
+      // a lane's sums: head hc, dims 16 i + 4 quad + e
+      const bool whole = first == 0 && last == n;
+      if (hc < G) {
+        const int h = g * G + hc;
+        if (whole) {
+          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+          __hip_bfloat16* o = a.out + s * a.o_ss + h * a.o_sh + 4 * quad;
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+            *reinterpret_cast<uint2*>(o + 16 * i) =
+                make_uint2(pack_bf16(acc[i][0] * inv, acc[i][1] * inv),
+                           pack_bf16(acc[i][2] * inv, acc[i][3] * inv));
+          if (quad == 0)
+            a.lse[(int64_t)h * a.S + s] = m == -INFINITY && l == 0.0f ? -INFINITY
+                                              : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        } else {
+          const int64_t at = (((int64_t)share * 2 + (first == 0)) * pg + pi) * G + hc;
+          float* o = a.part_o + at * kHeadDim + 4 * quad;
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+            *reinterpret_cast<f32x4_t*>(o + 16 * i) = acc[i];
+          if (quad == 0) a.part_ml[at] = make_float2(m, l);
+        }
+      }
+      if (first == 0 && last < n)
+        join = {r, (int)((base + n - 1) / per_share - share + 1)};
+      u = base + last;
+      base += n;
+      r++;
+    }
+  }
+  if (lane == 0) a.join[(int64_t)share * pg + pi] = join;
+}
+
+// -------------------------------------------------------------------- join
+// One work-group per (share, kv-head, head of the group) where a split row begins: its
+// partials are slot 1 of that share and slot 0 of those after it.
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheDecodeArgs a, bool full) {
+  __shared__ float wt[kCacheWaves];
+  __shared__ float red[4];
+  __shared__ f32x4_t part[8][kHeadDim / 4];
+  const int G = a.G, tid = threadIdx.x;
+  const int pg = full ? a.c.Hkv : 1;
+  const int hl = blockIdx.x % G;
+  const int64_t at = blockIdx.x / G;
+  const CacheJoin jn = a.join[at];
+  if (jn.row < 0) return;
+  const int share = (int)(at / pg), gi = (int)(at % pg);
+  const auto slot = [&](int i) {
+    return (((int64_t)(share + i) * 2 + (i == 0)) * pg + gi) * G + hl;
+  };
+  float top = -INFINITY;
+  for (int i = tid; i < jn.count; i += 256) top = fmaxf(top, a.part_ml[slot(i)].x);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  const float mr = top == -INFINITY ? 0.0f : top;
+  __syncthreads();
+  float l = 0.0f;
+  for (int i = tid; i < jn.count; i += 256) {
+    const float2 ml = a.part_ml[slot(i)];
+    const float x = __builtin_amdgcn_exp2f(ml.x - mr);
+    wt[i] = x;
+    l = fmaf(x, ml.y, l);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+  if ((tid & 63) == 0) red[tid >> 6] = l;
+  __syncthreads();
+  l = (red[0] + red[1]) + (red[2] + red[3]);
+  const int d4 = tid & 31, grp = tid >> 5;
+  f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int i = grp; i < jn.count; i += 8) {
+    const f32x4_t x = reinterpret_cast<const f32x4_t*>(a.part_o + slot(i) * kHeadDim)[d4];
+    const float y = wt[i];
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = fmaf(y, x[e], o[e]);
+  }
+  part[grp][d4] = o;
+  __syncthreads();
+  if (tid >= kHeadDim / 4) return;
+#pragma unroll
+  for (int i = 1; i < 8; i++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] += part[i][tid][e];
+  const int s = full ? jn.row : jn.row / a.c.Hkv;
+  const int g = full ? gi : jn.row % a.c.Hkv;
+  const int h = g * G + hl;
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  *reinterpret_cast<uint2*>(a.out + s * a.o_ss + h * a.o_sh + 4 * tid) =
+      make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+  if (tid == 0)
+    a.lse[(int64_t)h * a.S + s] =
+        top == -INFINITY && l == 0.0f ? -INFINITY : (mr + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// -------------------------------------------------------------------- gate
+// Past blocks of request s.
+__device__ __forceinline__ int past_blocks(const CacheDecodeArgs& a, int s) {
+  const int len = held(a, s);
+  return len > 0 ? (len - 1) / a.B : 0;
+}
+
+__global__ __launch_bounds__(kCacheDecodeThreads) void cache_gate_kernel(CacheDecodeArgs a) {
+  __shared__ Sums sums;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const CachePool& c = a.c;
+  const int Hkv = c.Hkv, G = a.G;
+  const auto units = [&](int s) -> int64_t { return past_blocks(a, s); };
+  sum_rows(sums, a.S, units);
+  const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
+  const int share = w / Hkv, g = w % Hkv;
+  const int64_t total = uniform(sums.total);
+  const int64_t per_share = (total + a.gate_shares - 1) / a.gate_shares;
+  int64_t u = share * per_share;
+  const int64_t u_end = min(u + per_share, total);
+  if (share >= a.gate_shares || u >= u_end) return;
+  int64_t base;
+  int s = find_row(sums, a.S, u, units, &base);
+  s = __builtin_amdgcn_readfirstlane(s);
+  base = uniform(base);
+  const int per = a.B / c.P;  // pages per block
+  while (u < u_end) {
+    const int64_t n = uniform(units(s));
+    const int last = (int)min(n, u_end - base);
+    for (int j = (int)(u - base); j < last; j++) {
+      double s0 = 0.0, s1 = 0.0;
+      for (int p0 = 0; p0 < per; p0 += 64) {
+        const int np = min(64, per - p0);
+        const int id = a.table[s * a.t_ss + (int64_t)j * per + p0 + min(lane, np - 1)];
+        for (int p = 0; p < np; p += 8) {
+          float2 x[8];
+          bool ok[8];
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            const int page = __builtin_amdgcn_readlane(id, min(p + e, np - 1));
+            ok[e] = p + e < np && (uint32_t)page < (uint32_t)c.N;
+            x[e] = reinterpret_cast<const float2*>(
+                c.k_sum + ((int64_t)(ok[e] ? page : 0) * Hkv + g) * kHeadDim)[lane];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            s0 += ok[e] ? (double)x[e].x : 0.0;
+            s1 += ok[e] ? (double)x[e].y : 0.0;
+          }
+        }
+      }
+      for (int hl = 0; hl < G; hl++) {
+        const int h = g * G + hl;
+        const uint32_t qw = *reinterpret_cast<const uint32_t*>(a.q + s * a.q_ss + h * a.q_sh + 2 * lane);
+        double x = (double)bf16_lo(qw) * s0 + (double)bf16_hi(qw) * s1;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+        if (lane == 0) a.score[((int64_t)s * a.Hq + h) * a.nblk + j] = x;
+      }
+    }
+    u = base + last;
+    base += n;
+    s++;
+  }
+}
+
+// ------------------------------------------------------------------ select
+// A total order of doubles as unsigned integers, NaN with the lowest; never 0.
+__device__ __forceinline__ uint64_t order_of(double x) {
+  const uint64_t b = (uint64_t)__double_as_longlong(x == x ? x + 0.0 : -INFINITY);  // (-0 is 0)
+  return b >> 63 ? ~b : b | (uint64_t(1) << 63);
+}
+
+// One work-group per (request, kv-head); NW: words of 64 blocks.
+template <int NW>
+__global__ __launch_bounds__(256) void cache_select_kernel(CacheDecodeArgs a) {
+  __shared__ unsigned long long kept[16][NW];
+  __shared__ int before[NW + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int G = a.G, Hkv = a.c.Hkv;
+  const int r = blockIdx.x, s = r / Hkv, g = r % Hkv;
+  const int len = held(a, s);
+  if (len == 0) {
+    if (tid == 0) a.nsteps[r] = 0;
+    return;
+  }
+  const int past = (len - 1) / a.B;
+  const int nh = min(a.topk - 1, past);
+  for (int hl = wave; hl < G; hl += 4) {
+    uint64_t key[NW];
+    const double* sc = a.score + ((int64_t)s * a.Hq + g * G + hl) * a.nblk;
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const int j = 64 * x + lane;
+      key[x] = j >= past ? 0 : nh == past ? 1 : order_of(sc[j]);
+    }
+    // the largest bound that at least nh keys reach
+    uint64_t bound = nh == past ? 1 : 0;
+    int reach = nh == past ? nh : 0;  // keys that reach it, where that was counted
+    for (int bit = 63; bit >= 0 && reach != nh && nh > 0; bit--) {
+      const uint64_t cand = bound | (uint64_t(1) << bit);
+      int n = 0;
+#pragma unroll
+      for (int x = 0; x < NW; x++) n += __popcll(__ballot(key[x] >= cand));
+      if (n >= nh) {
+        bound = cand;
+        reach = n;
+      }
+    }
+    // all keys above the bound, and of those that equal it the first ones
+    int above = 0;
+#pragma unroll
+    for (int x = 0; x < NW; x++) above += __popcll(__ballot(key[x] > bound));
+    int ties = nh - above;
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const unsigned long long eq = __ballot(key[x] == bound && key[x] != 0);
+      const bool take = key[x] > bound || (key[x] == bound && key[x] != 0 &&
+                                           __popcll(eq & ((1ull << lane) - 1)) < ties);
+      const unsigned long long m = __ballot(take && nh > 0);
+      ties -= min(ties, (int)__popcll(eq));
+      if (lane == 0) kept[hl][x] = m;
+    }
+  }
+  __syncthreads();
+  if (tid < NW) {
+    unsigned long long any = 0;
+    for (int hl = 0; hl < G; hl++) any |= kept[hl][tid];
+    int n = __popcll(any);
+    int incl = n;
+#pragma unroll
+    for (int d = 1; d < NW; d <<= 1) {
+      const int o = __shfl_up(incl, d, 64);
+      if (lane >= d) incl += o;
+    }
+    before[tid] = incl - n;
+    if (tid == NW - 1) before[NW] = incl;
+  }
+  __syncthreads();
+  const int nu = before[NW];
+  uint32_t* list = a.list + (int64_t)r * a.nlist;
+  for (int x = wave; x < NW; x += 4) {
+    uint32_t heads = 0;
+    for (int hl = 0; hl < G; hl++) heads |= (uint32_t)((kept[hl][x] >> lane) & 1) << hl;
+    const unsigned long long any = __ballot(heads != 0);
+    if (heads) list[before[x] + __popcll(any & ((1ull << lane) - 1))] = (uint32_t)(64 * x + lane) | heads << 16;
+  }
+  if (tid == 0) {
+    list[nu] = (uint32_t)past | 0xffff0000u;
+    a.nsteps[r] = nu * (a.B / kCacheTile) + (len - past * a.B + kCacheTile - 1) / kCacheTile;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_gate(const CacheDecodeArgs& a, hipStream_t st) {
+  const int64_t waves = (int64_t)a.gate_shares * a.c.Hkv;
+  cache_gate_kernel<<<(unsigned)((waves + 3) / 4), kCacheDecodeThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st) {
+  const unsigned groups = (unsigned)(a.S * a.c.Hkv);
+  if (a.nblk <= 256) cache_select_kernel<4><<<groups, 256, 0, st>>>(a);
+  else if (a.nblk <= 1024) cache_select_kernel<16><<<groups, 256, 0, st>>>(a);
+  else cache_select_kernel<kMaxBlocksPerSeq / 64><<<groups, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t st) {
+  const int64_t waves = (int64_t)a.shares * (full ? a.c.Hkv : 1);
+  const unsigned groups = (unsigned)((waves + 3) / 4);
+  if (full) cache_attend_kernel<false><<<groups, kCacheDecodeThreads, 0, st>>>(a);
+  else cache_attend_kernel<true><<<groups, kCacheDecodeThreads, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st) {
+  const int64_t groups = (int64_t)a.shares * (full ? a.c.Hkv : 1) * a.G;
+  cache_join_kernel<<<(unsigned)groups, 256, 0, st>>>(a, full);
+  return hipGetLastError();
+}
+
+}  // namespace moba

@@ -1,0 +1,87 @@
+// Internal declarations of the paged 8-bit cache (plan, write, decode), shared by its host
+// side and its kernels.
+#pragma once
+
+#include "moba_internal.h"
+
+namespace moba {
+
+constexpr int kCacheTile = 64;       // tokens of a V tile, and of a decode step
+constexpr int kCacheMaxPage = 256;   // largest page
+constexpr int kPlanMaxRequests = 4096;
+constexpr int kCacheMinExp = -100, kCacheMaxExp = 119;  // exponents of a page's scale
+
+struct CachePool {
+  uint8_t* k; int64_t k_sp, k_sh;  // [N, Hkv, P, 128], page and head strides in bytes
+  uint8_t* v; int64_t v_sp, v_sh;  // [N, Hkv, P / 64, 128, 64]
+  float* k_scale;                  // [N, Hkv]
+  float* v_scale;
+  float* k_sum;                    // [N, Hkv, 128]
+  int N, Hkv, P;
+};
+
+// ------------------------------------------------------------------ plan
+struct CachePlanArgs {
+  const int32_t* add;
+  const int32_t* lens;
+  int32_t* table; int64_t t_ss;
+  int32_t* free_pages;
+  const int32_t* num_free;
+  int32_t* lens_out;
+  int32_t* num_free_out;
+  int32_t* cu;
+  int64_t* slots;
+  int32_t* refused;
+  int S, W, N, P;
+  int64_t T;
+};
+hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st);
+
+// ----------------------------------------------------------------- write
+struct CacheWriteArgs {
+  const void* k; int64_t k_st, k_sh;  // [T, Hkv, 128], elements
+  const void* v; int64_t v_st, v_sh;
+  const int64_t* slots;
+  int64_t T;
+  CachePool c;
+};
+hipError_t launch_cache_write(bool bf16, const CacheWriteArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- decode
+constexpr int kCacheWaves = 2048;  // attention waves the chip holds: 8 on each of 256 CUs
+constexpr int kCacheDecodeThreads = 256;
+
+// Where a row split over several shares begins: the row (full: request; MoBA: request *
+// Hkv + kv-head; -1: none) and the shares it spans.
+struct CacheJoin {
+  int32_t row, count;
+};
+
+struct CacheDecodeArgs {
+  const __hip_bfloat16* q; int64_t q_ss, q_sh;  // [S, Hq, D]
+  CachePool c;
+  const int32_t* table; int64_t t_ss;
+  const int32_t* lens;
+  int S, W, Hq, G;
+  int B, topk;                                  // MoBA; nblk: blocks a table row holds
+  int nblk;
+  int nlist;                                    // MoBA: list entries per (request, kv-head)
+  __hip_bfloat16* out; int64_t o_ss, o_sh;
+  float* lse;                                   // [Hq, S]
+  float scale_log2;
+  int shares;        // of the batch's 64-key steps; full: of each kv-head
+  int gate_shares;   // of the batch's past blocks, of each kv-head
+  // workspace
+  double* score;     // [S, Hq, nblk] gate scores
+  uint32_t* list;    // [S * Hkv, nlist] blocks attended: index | heads << 16, ascending
+  int32_t* nsteps;   // [S * Hkv] 64-key steps of the list
+  float* part_o;     // [shares, 2, Hkv (MoBA: 1), G, D] unnormalised partials
+  float2* part_ml;   // [shares, 2, Hkv (MoBA: 1), G] their max (log2 domain) and sum
+  CacheJoin* join;   // [shares, Hkv (MoBA: 1)]
+};
+hipError_t launch_cache_gate(const CacheDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st);
+
+}  // namespace moba
