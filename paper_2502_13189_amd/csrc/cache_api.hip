@@ -40,7 +40,9 @@ moba_status check_cache(const moba_cache* c, CachePool* p) {
   if (c->k->ndim != 4 || c->k->shape[0] < 1 || c->k->shape[1] < 1) return MOBA_ERR_SHAPE;
   const int64_t N = c->k->shape[0], Hkv = c->k->shape[1], P = c->k->shape[2];
   if (c->k->shape[3] != kHeadDim || !page_size_ok(P)) return MOBA_ERR_UNSUPPORTED;
-  if (N >= (int64_t(1) << 31) || Hkv >= (int64_t(1) << 20)) return MOBA_ERR_UNSUPPORTED;
+  if (N >= (int64_t(1) << 31) || N * (P / kCacheTile) >= (int64_t(1) << 32) ||
+      Hkv >= (int64_t(1) << 20))
+    return MOBA_ERR_UNSUPPORTED;
   moba_status st;
   if ((st = check_pages(c->k, N, Hkv, P, kHeadDim, &p->k, &p->k_sp, &p->k_sh)) != MOBA_OK) return st;
   if ((st = check_pages(c->v, N, Hkv, P / kCacheTile * kHeadDim, kCacheTile, &p->v, &p->v_sp,
