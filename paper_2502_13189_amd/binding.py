@@ -335,57 +335,56 @@ class CachePlan(NamedTuple):
     refused: torch.Tensor   # [1] int32: requests refused
 
 
-# moba_tensor: data, dtype, ndim, shape[4], stride[4]
-_DESC = struct.Struct("=Qii8q")
 _PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())
+_PACK: dict = {}  # by number of tensors: their moba_tensor descriptors, one after the other
+_DESC_BYTES = ctypes.sizeof(MobaTensor)
 
 
-class _Descs:
-    """Descriptors of several tensors of one device in one block of memory; at(i) is the
-    address of the i-th.  (Packed: a step's calls are short, and filling a MobaTensor field by
-    field takes several times as long.)"""
-
-    def __init__(self, tensors):
-        device = tensors[0].device
-        if device.type != "cuda":
-            raise ValueError("the paged cache's tensors live on a GPU")
-        parts = []
-        for t in tensors:
-            if t.device != device:
-                raise ValueError("tensors on %s and on %s" % (device, t.device))
-            shape, stride = tuple(t.shape), t.stride()
-            n = len(shape)
-            if n == 5:  # V pages: the tiles' rows one after the other
-                if stride[3] != shape[4] or (shape[2] > 1 and stride[2] != shape[3] * stride[3]):
-                    raise ValueError("v's last three dims must be contiguous")
-                shape = (shape[0], shape[1], shape[2] * shape[3], shape[4])
-                stride = (stride[0], stride[1], stride[3], stride[4])
-                n = 4
-            elif n > 4:
-                raise ValueError("at most 4 dimensions")
-            dt = _DT.get(t.dtype)
-            if dt is None:
-                raise TypeError("unsupported dtype %s" % t.dtype)
-            parts.append(_DESC.pack(t.data_ptr(), dt, n, *shape, *_PAD[n], *stride, *_PAD[n]))
-        self._buf = ctypes.create_string_buffer(b"".join(parts))
-        self._base = ctypes.addressof(self._buf)
-
-    def at(self, i: int) -> int:
-        return self._base + i * _DESC.size
-
-    def cache(self, i: int):
-        """moba_cache of five tensors from the i-th on."""
-        return (ctypes.c_void_p * 5)(*(self.at(i + j) for j in range(5)))
+def _descs(tensors):
+    """(memory, address, device): descriptors of tensors of one GPU.  (Packed in one go: a step's
+    calls are short, and a MobaTensor filled field by field takes several times as long.)"""
+    device = tensors[0].get_device()
+    if device < 0:
+        raise ValueError("the paged cache's tensors live on a GPU")
+    fields = []
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError("tensors on several devices")
+        dtype = _DT.get(t.dtype)
+        if dtype is None:
+            raise TypeError("unsupported dtype %s" % t.dtype)
+        shape, stride = t.shape, t.stride()
+        n = len(stride)
+        if n == 5:  # V pages: the rows of a page's tiles one after the other
+            if shape[2] > 1 and stride[2] != shape[3] * stride[3]:
+                raise ValueError("v's last three dims must be contiguous")
+            shape = (shape[0], shape[1], shape[2] * shape[3], shape[4])
+            stride = (stride[0], stride[1], stride[3], stride[4])
+            n = 4
+        elif n > 4:
+            raise ValueError("at most 4 dimensions")
+        pad = _PAD[n]
+        fields += (t.data_ptr(), dtype, n, *shape, *pad, *stride, *pad)
+    pack = _PACK.get(len(tensors))
+    if pack is None:  # data, dtype, ndim, shape[4], stride[4]
+        pack = _PACK[len(tensors)] = struct.Struct("=" + "Qii8q" * len(tensors))
+    memory = ctypes.create_string_buffer(pack.pack(*fields), pack.size)
+    return memory, ctypes.addressof(memory), device
 
 
-def _call(fn: str, t: torch.Tensor, stream, *args):
-    """Calls fn with the device of t current, on `stream` or that device's current one."""
-    if t.device.index == torch.cuda.current_device():
-        status = getattr(load(), fn)(*args, _stream(t, stream))
+def _call(fn: str, device: int, stream, *args):
+    """Calls fn with `device` current, on `stream` or the device's current one."""
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(device)
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
+    if device == torch.cuda.current_device():
+        status = getattr(load(), fn)(*args, int(stream))
     else:
-        with torch.cuda.device(t.device):
-            status = getattr(load(), fn)(*args, _stream(t, stream))
-    _check(fn, status)
+        with torch.cuda.device(device):
+            status = getattr(load(), fn)(*args, int(stream))
+    if status != 0:
+        raise MobaError(fn, status)
 
 
 def _allocating(stream):
@@ -425,22 +424,18 @@ def cache_plan(add, lens, table, free_pages, num_free, page_size: int, num_token
     S = add.shape[0]
     if slots is not None and slots.shape[0] != num_tokens:
         raise ValueError("slots has %d rows, num_tokens is %d" % (slots.shape[0], num_tokens))
-    i32 = dict(dtype=torch.int32, device=add.device)
     with _allocating(stream):
-        if lens_out is None:
-            lens_out = torch.empty((S,), **i32)
-        if num_free_out is None:
-            num_free_out = torch.empty((1,), **i32)
-        if cu_new is None:
-            cu_new = torch.empty((S + 1,), **i32)
+        mine = add.new_empty((2 * S + 3,), dtype=torch.int32).split_with_sizes((S, S + 1, 1, 1))
         if slots is None:
-            slots = torch.empty((int(num_tokens),), dtype=torch.int64, device=add.device)
-        if refused is None:
-            refused = torch.empty((1,), **i32)
-    d = _Descs((add, lens, table, free_pages, num_free, lens_out, num_free_out, cu_new, slots,
-                refused))
-    _call("moba_cache_plan", add, stream, d.at(0), d.at(1), d.at(2), d.at(3), d.at(4),
-          int(page_size), d.at(5), d.at(6), d.at(7), d.at(8), d.at(9))
+            slots = add.new_empty((int(num_tokens),), dtype=torch.int64)
+    lens_out = mine[0] if lens_out is None else lens_out
+    cu_new = mine[1] if cu_new is None else cu_new
+    num_free_out = mine[2] if num_free_out is None else num_free_out
+    refused = mine[3] if refused is None else refused
+    _memory, at, device = _descs((add, lens, table, free_pages, num_free, lens_out, num_free_out,
+                                  cu_new, slots, refused))
+    d = [at + _DESC_BYTES * i for i in range(10)]
+    _call("moba_cache_plan", device, stream, *d[:5], int(page_size), *d[5:])
     return CachePlan(cu_new, slots, lens_out, num_free_out, refused)
 
 
@@ -448,9 +443,10 @@ def cache_write(k, v, slots, cache: PagedCache, stream=None) -> None:
     """Quantises new keys and values [T, Hkv, 128] (bf16 or fp32) into their slots [T]
     int64 (negative: left out), as cache_plan() gives them: a page's tokens are
     consecutive rows with ascending slots."""
-    d = _Descs((k, v, slots, *cache))
-    c = d.cache(3)
-    _call("moba_cache_write", k, stream, d.at(0), d.at(1), d.at(2), ctypes.addressof(c))
+    _memory, at, device = _descs((k, v, slots, *cache))
+    d = [at + _DESC_BYTES * i for i in range(8)]
+    c = (ctypes.c_void_p * 5)(*d[3:])
+    _call("moba_cache_write", device, stream, *d[:3], ctypes.addressof(c))
 
 
 def cache_decode_workspace_bytes(num_requests: int, table_width: int, num_q_heads: int,
@@ -478,16 +474,17 @@ def cache_decode(q, cache: PagedCache, table, lens, block_size: int, topk: int, 
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
-            lse = torch.empty((Hq, S), dtype=torch.float32, device=q.device)
+            lse = q.new_empty((Hq, S), dtype=torch.float32)
         if workspace is None:
-            n = cache_decode_workspace_bytes(S, table.shape[1], Hq, cache.k.shape[1],
-                                             cache.k.shape[2], block_size, topk)
-            workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
-    d = _Descs((q, table, lens, out, lse, *cache))
-    c = d.cache(5)
-    _call("moba_cache_decode", q, stream, d.at(0), ctypes.addressof(c), d.at(1), d.at(2),
-          int(block_size), int(topk), d.at(3), d.at(4), workspace.data_ptr(),
-          workspace.numel() * workspace.element_size())
+            k = cache.k.shape
+            n = load().moba_cache_decode_workspace_bytes(S, table.shape[1], Hq, k[1], k[2],
+                                                         int(block_size), int(topk))
+            workspace = q.new_empty((max(n, 16),), dtype=torch.uint8)
+    _memory, at, device = _descs((q, table, lens, out, lse, *cache))
+    d = [at + _DESC_BYTES * i for i in range(10)]
+    c = (ctypes.c_void_p * 5)(*d[5:])
+    _call("moba_cache_decode", device, stream, d[0], ctypes.addressof(c), d[1], d[2],
+          int(block_size), int(topk), d[3], d[4], workspace.data_ptr(), workspace.nbytes)
     return out, lse
 
 
