@@ -94,7 +94,9 @@ def some_batch(rng, S, W, page, spare):
 @pytest.mark.parametrize("S,W,page,spare,most,slack", [
     (1, 1, 64, 1, 1, 0), (3, 4, 64, 5, 70, 2), (17, 6, 128, 0, 3, 0), (64, 9, 192, 20, 200, 5),
     (65, 3, 64, 200, 2, 1), (300, 5, 256, 100, 400, -50), (1500, 2, 64, 300, 40, 7),
-    (4096, 3, 64, 500, 9, 0), (9, 400, 64, 4000, 9000, 100), (2, 3000, 64, 6000, 150000, -1),
+    (4096, 3, 64, 500, 9, 0), (4096, 3, 64, 700, 90, 0), (4000, 9, 64, 2000, 300, 0), (9, 400, 64, 4000, 9000, 100), (2, 3000, 64, 6000, 150000, -1),
+    (4096, 3, 64, 600, 4, 3), (3000, 2, 64, 100, 1, -5), (70, 5, 192, 9, 4, 9000),
+    (3000, 60, 64, 9000, 1000, 30),
 ])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_plan(S, W, page, spare, most, slack, in_place):
