@@ -108,7 +108,8 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   if (topk < 0) return MOBA_ERR_TOPK;
   if (topk > 0 && (block_size < 1 || block_size % P != 0)) return MOBA_ERR_BLOCK_SIZE;
   if (Hq >= (int64_t(1) << 20) || W >= (int64_t(1) << 31) || S >= (int64_t(1) << 31) ||
-      S * W >= (int64_t(1) << 31) || S * Hq >= (int64_t(1) << 31))
+      S * W >= (int64_t(1) << 31) || S * Hq >= (int64_t(1) << 31) ||
+      S * W * (P / kCacheTile) >= (int64_t(1) << 31) / Hkv)
     return MOBA_ERR_UNSUPPORTED;
   d->S = S;
   d->W = W;
@@ -126,7 +127,8 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   const int64_t each = std::max<int64_t>(1, kCacheWaves / Hkv);
   d->shares = (int)(d->full ? std::min<int64_t>(each, std::max<int64_t>(steps, 1))
                             : std::min<int64_t>(kCacheWaves, std::max<int64_t>(steps * Hkv, 1)));
-  d->gate_shares = (int)std::min<int64_t>(each, std::max<int64_t>(S * nblk, 1));
+  d->gate_shares = (int)std::min<int64_t>(std::max<int64_t>(1, kCacheGateWaves / Hkv),
+                                          std::max<int64_t>(S * nblk, 1));
   return MOBA_OK;
 }
 

@@ -26,6 +26,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace moba {
 namespace {
 
@@ -65,25 +67,31 @@ __device__ __forceinline__ int held(const CacheDecodeArgs& a, int s) {
 
 // ------------------------------------------------------------------ shares
 // The rows' units in a sum over all rows: pre[i] units lie before the i-th of the 256
-// groups of `per` rows.
+// groups of `per` rows.  (The host sees to it that the sum stays below 2^31.)
 struct Sums {
-  int64_t pre[kCacheDecodeThreads];
-  int64_t part[kCacheDecodeThreads / 64];
-  int64_t total;
+  int pre[kCacheDecodeThreads];
+  int part[kCacheDecodeThreads / 64];
+  int total;
 };
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1 lane below in a row of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row 0's last to row 1, 2's to 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31's to rows 2 and 3
+  return x;
+}
 
 template <typename F>
 __device__ __forceinline__ void sum_rows(Sums& sm, int rows, F units) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (rows + kCacheDecodeThreads - 1) / kCacheDecodeThreads;
-  int64_t mine = 0;
+  int mine = 0;
   for (int i = 0, r = tid * per; i < per && r < rows; i++, r++) mine += units(r);
-  int64_t x = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t o = __shfl_up((long long)x, d, 64);
-    if (lane >= d) x += o;
-  }
+  int x = wave_scan(mine);
   if (lane == 63) sm.part[wave] = x;
   __syncthreads();
   for (int w = 0; w < wave; w++) x += sm.part[w];
@@ -94,39 +102,32 @@ __device__ __forceinline__ void sum_rows(Sums& sm, int rows, F units) {
 
 // The row that unit u (< total) belongs to, for a whole wave; base: units before the row.
 template <typename F>
-__device__ __forceinline__ int find_row(const Sums& sm, int rows, int64_t u, F units, int64_t* base) {
+__device__ __forceinline__ int find_row(const Sums& sm, int rows, int u, F units, int* base) {
   const int lane = threadIdx.x & 63;
   const int per = (rows + kCacheDecodeThreads - 1) / kCacheDecodeThreads;
-  int below = 0;  // groups that begin at or before u
+  int below = 0;  // groups that begin at or before u (the last of them is not empty)
 #pragma unroll
   for (int i = 0; i < kCacheDecodeThreads / 64; i++)
     below += __popcll(__ballot(sm.pre[64 * i + lane] <= u));
   const int r0 = (below - 1) * per, r1 = min(r0 + per, rows);
-  int64_t acc = sm.pre[below - 1];
+  int acc = sm.pre[below - 1];
+  if (per == 1) {
+    *base = __builtin_amdgcn_readfirstlane(acc);
+    return r0;
+  }
   for (int r = r0; r < r1; r += 64) {
-    const int64_t n = r + lane < r1 ? units(r + lane) : 0;
-    int64_t x = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t o = __shfl_up((long long)x, d, 64);
-      if (lane >= d) x += o;
-    }
+    const int n = r + lane < r1 ? units(r + lane) : 0;
+    const int x = wave_scan(n);
     const unsigned long long past = __ballot(acc + x > u);
     if (past) {
       const int at = __ffsll((long long)past) - 1;
-      *base = acc + __shfl((long long)(x - n), at, 64);
+      *base = __builtin_amdgcn_readlane(acc + x - n, at);
       return r + at;
     }
-    acc += __shfl((long long)x, 63, 64);
+    acc += __builtin_amdgcn_readlane(x, 63);
   }
   *base = 0;  // (not reached: u < total)
   return rows;
-}
-
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
-  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 // ------------------------------------------------------------------ attend
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
   const CachePool& c = a.c;
   const int Hkv = c.Hkv, G = a.G, P = c.P;
   const int rows = MOBA ? a.S * Hkv : a.S;
-  const auto units = [&](int r) -> int64_t {
+  const auto units = [&](int r) {
     if constexpr (MOBA) return a.nsteps[r];
     else return (held(a, r) + kCacheTile - 1) / kCacheTile;
   };
@@ -171,22 +172,20 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
   int g = MOBA ? 0 : w % Hkv;
   if (share >= a.shares) return;
   const int pg = MOBA ? 1 : Hkv, pi = MOBA ? 0 : g;  // partials: kv-heads per share, this one
-  const int64_t total = uniform(sums.total);
-  const int64_t per_share = (total + a.shares - 1) / a.shares;
-  const int64_t u_end = min((share + 1) * per_share, total);
-  int64_t u = share * per_share;
+  const int total = __builtin_amdgcn_readfirstlane(sums.total);
+  const int per_share = (total + a.shares - 1) / a.shares;
+  int u = (int)min((int64_t)share * per_share, (int64_t)total);
+  const int u_end = (int)min((int64_t)u + per_share, (int64_t)total);
   CacheJoin join = {-1, 0};
   if (u < u_end) {
-    int64_t base;
-    int r = find_row(sums, rows, u, units, &base);
-    r = __builtin_amdgcn_readfirstlane(r);
-    base = uniform(base);
+    int base;
+    int r = __builtin_amdgcn_readfirstlane(find_row(sums, rows, u, units, &base));
     const int hc = lane & 15, quad = lane >> 4;
     const int spb = MOBA ? a.B / kCacheTile : 0;  // steps per block
     const int koff = (16 * (hc >> 2) + (hc & 3)) * kHeadDim + 16 * quad;
     const int voff = hc * kCacheTile + 16 * quad;
     while (u < u_end) {
-      const int64_t n = uniform(units(r));
+      const int n = __builtin_amdgcn_readfirstlane(units(r));
       if (n == 0) {
         r++;
         continue;
@@ -194,7 +193,7 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
       const int s = MOBA ? r / Hkv : r;
       if constexpr (MOBA) g = r % Hkv;
       const int len = held(a, s);
-      const int first = (int)(u - base), last = (int)min(n, u_end - base);
+      const int first = u - base, last = min(n, u_end - base);
       const int32_t* row = a.table + s * a.t_ss;
       const uint32_t* list = MOBA ? a.list + (int64_t)r * a.nlist : nullptr;
       // B operands: q of head hc, the dims of the K operands
@@ -350,7 +349,7 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
         }
       }
       if (first == 0 && last < n)
-        join = {r, (int)((base + n - 1) / per_share - share + 1)};
+        join = {r, (base + n - 1) / per_share - share + 1};
       u = base + last;
       base += n;
       r++;
@@ -360,12 +359,18 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
 }
 
 // -------------------------------------------------------------------- join
-// One work-group per (share, kv-head, head of the group) where a split row begins: its
-// partials are slot 1 of that share and slot 0 of those after it.
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheDecodeArgs a, bool full) {
+// One work-group per (share, kv-head, head of the group); most find no split row that
+// begins in their share.  The row's partials are slot 1 of that share and slot 0 of those
+// after it.  Bound by latency: the share's entry, then partials, maxima and sums together.
+// (As 512-thread work-groups, or with half a wave per short row and a work-group for a long
+// one's heads, a ragged batch of 8 took 9 us, this way 6.)
+constexpr int kJoinThreads = 256;
+constexpr int kJoinGroups = kJoinThreads / (kHeadDim / 4);
+
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheDecodeArgs a, bool full) {
   __shared__ float wt[kCacheWaves];
-  __shared__ float red[4];
-  __shared__ f32x4_t part[8][kHeadDim / 4];
+  __shared__ float red[2][kJoinThreads / 64];
+  __shared__ f32x4_t part[kJoinGroups][kHeadDim / 4];
   const int G = a.G, tid = threadIdx.x;
   const int pg = full ? a.c.Hkv : 1;
   const int hl = blockIdx.x % G;
@@ -376,52 +381,66 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheDecodeArgs a, bool
   const auto slot = [&](int i) {
     return (((int64_t)(share + i) * 2 + (i == 0)) * pg + gi) * G + hl;
   };
-  float top = -INFINITY;
-  for (int i = tid; i < jn.count; i += 256) top = fmaxf(top, a.part_ml[slot(i)].x);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  if ((tid & 63) == 0) red[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  const float mr = top == -INFINITY ? 0.0f : top;
-  __syncthreads();
-  float l = 0.0f;
-  for (int i = tid; i < jn.count; i += 256) {
-    const float2 ml = a.part_ml[slot(i)];
-    const float x = __builtin_amdgcn_exp2f(ml.x - mr);
-    wt[i] = x;
-    l = fmaf(x, ml.y, l);
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
-  if ((tid & 63) == 0) red[tid >> 6] = l;
-  __syncthreads();
-  l = (red[0] + red[1]) + (red[2] + red[3]);
-  const int d4 = tid & 31, grp = tid >> 5;
+  const int d4 = tid & 31, grp = tid >> 5;  // the thread's partials are grp + 8 i
   f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int i = grp; i < jn.count; i += 8) {
-    const f32x4_t x = reinterpret_cast<const f32x4_t*>(a.part_o + slot(i) * kHeadDim)[d4];
-    const float y = wt[i];
+  float top = -INFINITY, l = 0.0f;
+  const auto run = [&](auto ahead) {
+    constexpr int kAhead = decltype(ahead)::value;
+    f32x4_t x[kAhead];
+    const auto fetch = [&](int i0) {
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] = fmaf(y, x[e], o[e]);
-  }
+      for (int e = 0; e < kAhead; e++)
+        x[e] = reinterpret_cast<const f32x4_t*>(
+            a.part_o + slot(min(i0 + kJoinGroups * e, jn.count - 1)) * kHeadDim)[d4];
+    };
+    fetch(grp);  // (in flight while the weights are found)
+    for (int i = tid; i < jn.count; i += kJoinThreads) {
+      wt[i] = a.part_ml[slot(i)].x;
+      top = fmaxf(top, wt[i]);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((tid & 63) == 0) red[0][tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    for (int i = tid; i < jn.count; i += kJoinThreads) {
+      wt[i] = __builtin_amdgcn_exp2f(wt[i] - (top == -INFINITY ? 0.0f : top));
+      l = fmaf(wt[i], a.part_ml[slot(i)].y, l);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) l += __shfl_xor(l, d, 64);
+    if ((tid & 63) == 0) red[1][tid >> 6] = l;
+    __syncthreads();
+    l = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    for (int i0 = grp; i0 < jn.count; i0 += kJoinGroups * kAhead) {
+      if (i0 != grp) fetch(i0);
+#pragma unroll
+      for (int e = 0; e < kAhead; e++) {
+        const int i = i0 + kJoinGroups * e;
+        const float y = wt[min(i, jn.count - 1)];
+#pragma unroll
+        for (int k = 0; k < 4; k++) o[k] = i < jn.count ? fmaf(y, x[e][k], o[k]) : o[k];
+      }
+    }
+  };
+  if (jn.count <= 2 * kJoinGroups) run(std::integral_constant<int, 2>{});
+  else run(std::integral_constant<int, 16>{});
   part[grp][d4] = o;
   __syncthreads();
-  if (tid >= kHeadDim / 4) return;
+  if (grp != 0) return;
 #pragma unroll
-  for (int i = 1; i < 8; i++)
+  for (int i = 1; i < kJoinGroups; i++)
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] += part[i][tid][e];
+    for (int e = 0; e < 4; e++) o[e] += part[i][d4][e];
   const int s = full ? jn.row : jn.row / a.c.Hkv;
   const int g = full ? gi : jn.row % a.c.Hkv;
   const int h = g * G + hl;
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  *reinterpret_cast<uint2*>(a.out + s * a.o_ss + h * a.o_sh + 4 * tid) =
+  *reinterpret_cast<uint2*>(a.out + s * a.o_ss + h * a.o_sh + 4 * d4) =
       make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-  if (tid == 0)
+  if (d4 == 0)
     a.lse[(int64_t)h * a.S + s] =
-        top == -INFINITY && l == 0.0f ? -INFINITY : (mr + __builtin_amdgcn_logf(l)) * kLn2;
+        top == -INFINITY && l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // -------------------------------------------------------------------- gate
@@ -431,58 +450,87 @@ __device__ __forceinline__ int past_blocks(const CacheDecodeArgs& a, int s) {
   return len > 0 ? (len - 1) / a.B : 0;
 }
 
+// x of another lane: of its quad, its 8 or its 16 (CTRL), for two-word values.
+template <int CTRL>
+__device__ __forceinline__ double lane_of(double x) {
+  const uint64_t b = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, false);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+
 __global__ __launch_bounds__(kCacheDecodeThreads) void cache_gate_kernel(CacheDecodeArgs a) {
   __shared__ Sums sums;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const CachePool& c = a.c;
   const int Hkv = c.Hkv, G = a.G;
-  const auto units = [&](int s) -> int64_t { return past_blocks(a, s); };
+  const auto units = [&](int s) { return past_blocks(a, s); };
   sum_rows(sums, a.S, units);
   const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
   const int share = w / Hkv, g = w % Hkv;
-  const int64_t total = uniform(sums.total);
-  const int64_t per_share = (total + a.gate_shares - 1) / a.gate_shares;
-  int64_t u = share * per_share;
-  const int64_t u_end = min(u + per_share, total);
+  const int total = __builtin_amdgcn_readfirstlane(sums.total);
+  const int per_share = (total + a.gate_shares - 1) / a.gate_shares;
+  int u = (int)min((int64_t)share * per_share, (int64_t)total);
+  const int u_end = (int)min((int64_t)u + per_share, (int64_t)total);
   if (share >= a.gate_shares || u >= u_end) return;
-  int64_t base;
-  int s = find_row(sums, a.S, u, units, &base);
-  s = __builtin_amdgcn_readfirstlane(s);
-  base = uniform(base);
+  int base;
+  int s = __builtin_amdgcn_readfirstlane(find_row(sums, a.S, u, units, &base));
   const int per = a.B / c.P;  // pages per block
+  const int half = lane >> 5, d4 = 4 * (lane & 31);  // half a wave per page row, 4 dims a lane
   while (u < u_end) {
-    const int64_t n = uniform(units(s));
-    const int last = (int)min(n, u_end - base);
-    for (int j = (int)(u - base); j < last; j++) {
-      double s0 = 0.0, s1 = 0.0;
+    const int n = __builtin_amdgcn_readfirstlane(units(s));
+    const int last = min(n, u_end - base);
+    for (int j = u - base; j < last; j++) {
+      double sum[4] = {0.0, 0.0, 0.0, 0.0};
       for (int p0 = 0; p0 < per; p0 += 64) {
         const int np = min(64, per - p0);
         const int id = a.table[s * a.t_ss + (int64_t)j * per + p0 + min(lane, np - 1)];
-        for (int p = 0; p < np; p += 8) {
-          float2 x[8];
+        for (int p = 0; p < np; p += 16) {
+          float4 x[8];
           bool ok[8];
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            const int page = __builtin_amdgcn_readlane(id, min(p + e, np - 1));
-            ok[e] = p + e < np && (uint32_t)page < (uint32_t)c.N;
-            x[e] = reinterpret_cast<const float2*>(
-                c.k_sum + ((int64_t)(ok[e] ? page : 0) * Hkv + g) * kHeadDim)[lane];
+            const int at = p + 2 * e;
+            const int page0 = __builtin_amdgcn_readlane(id, min(at, np - 1));
+            const int page1 = __builtin_amdgcn_readlane(id, min(at + 1, np - 1));
+            const int page = half ? page1 : page0;
+            ok[e] = at + half < np && (uint32_t)page < (uint32_t)c.N;
+            x[e] = *reinterpret_cast<const float4*>(
+                c.k_sum + ((int64_t)(ok[e] ? page : 0) * Hkv + g) * kHeadDim + d4);
           }
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            s0 += ok[e] ? (double)x[e].x : 0.0;
-            s1 += ok[e] ? (double)x[e].y : 0.0;
+            sum[0] += ok[e] ? (double)x[e].x : 0.0;
+            sum[1] += ok[e] ? (double)x[e].y : 0.0;
+            sum[2] += ok[e] ? (double)x[e].z : 0.0;
+            sum[3] += ok[e] ? (double)x[e].w : 0.0;
           }
         }
       }
-      for (int hl = 0; hl < G; hl++) {
-        const int h = g * G + hl;
-        const uint32_t qw = *reinterpret_cast<const uint32_t*>(a.q + s * a.q_ss + h * a.q_sh + 2 * lane);
-        double x = (double)bf16_lo(qw) * s0 + (double)bf16_hi(qw) * s1;
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-        if (lane == 0) a.score[((int64_t)s * a.Hq + h) * a.nblk + j] = x;
+      for (int i = 0; i < 4; i++) sum[i] += __shfl_xor(sum[i], 32, 64);
+      // half a wave per head, two heads at a time
+      for (int h0 = 0; h0 < G; h0 += 4) {
+        double x[2];
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int h = g * G + min(h0 + 2 * e + half, G - 1);
+          const uint2 qw = *reinterpret_cast<const uint2*>(a.q + s * a.q_ss + h * a.q_sh + d4);
+          x[e] = (double)bf16_lo(qw.x) * sum[0] + (double)bf16_hi(qw.x) * sum[1] +
+                 (double)bf16_lo(qw.y) * sum[2] + (double)bf16_hi(qw.y) * sum[3];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          x[e] += lane_of<0xb1>(x[e]);  // the neighbour, the other pair, four and eight lanes
+          x[e] += lane_of<0x4e>(x[e]);
+          x[e] += lane_of<0x141>(x[e]);
+          x[e] += lane_of<0x140>(x[e]);
+          x[e] += __shfl_xor(x[e], 16, 64);
+          const int hl = h0 + 2 * e + half;
+          if ((lane & 31) == 0 && hl < G)
+            a.score[((int64_t)s * a.Hq + g * G + hl) * a.nblk + j] = x[e];
+        }
       }
     }
     u = base + last;
@@ -604,7 +652,7 @@ hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t 
 
 hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st) {
   const int64_t groups = (int64_t)a.shares * (full ? a.c.Hkv : 1) * a.G;
-  cache_join_kernel<<<(unsigned)groups, 256, 0, st>>>(a, full);
+  cache_join_kernel<<<(unsigned)groups, kJoinThreads, 0, st>>>(a, full);
   return hipGetLastError();
 }
 

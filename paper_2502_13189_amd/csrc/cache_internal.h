@@ -49,6 +49,7 @@ hipError_t launch_cache_write(bool bf16, const CacheWriteArgs& a, hipStream_t st
 
 // ---------------------------------------------------------------- decode
 constexpr int kCacheWaves = 2048;  // attention waves the chip holds: 8 on each of 256 CUs
+constexpr int kCacheGateWaves = 8192;  // waves of the gate at most (one a block, if they suffice)
 constexpr int kCacheDecodeThreads = 256;
 
 // Where a row split over several shares begins: the row (full: request; MoBA: request *
