@@ -8,10 +8,8 @@ raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
-import struct
 from typing import NamedTuple
 
 import torch
@@ -335,66 +333,41 @@ class CachePlan(NamedTuple):
     refused: torch.Tensor   # [1] int32: requests refused
 
 
-_PAD = ((0, 0, 0, 0), (0, 0, 0), (0, 0), (0,), ())
-_PACK: dict = {}  # by number of tensors: their moba_tensor descriptors, one after the other
-_DESC_BYTES = ctypes.sizeof(MobaTensor)
+_cache_ext = None
 
 
-def _descs(tensors):
-    """(memory, address, device): descriptors of tensors of one GPU.  (Packed in one go: a step's
-    calls are short, and a MobaTensor filled field by field takes several times as long.)"""
-    device = tensors[0].get_device()
+def _cache_module():
+    """The marshalling of the paged cache's calls (csrc/cache_binding.cpp).  Raises if it has
+    not been built."""
+    global _cache_ext
+    if _cache_ext is None:
+        load()
+        try:
+            from . import _cache_binding
+        except ImportError as e:
+            raise RuntimeError("_cache_binding.so does not load; build it with "
+                               "`python -m paper_2502_13189_amd.build`") from e
+        _cache_ext = _cache_binding
+    return _cache_ext
+
+
+def _cache_call(fn: str, t: torch.Tensor, stream, *args):
+    """_cache_binding's fn on `stream` or the current stream of t's device, which is made current.
+    What the call allocates is allocated for that stream, so that memory it drops is not
+    given out again before the call is done with it."""
+    f = getattr(_cache_ext or _cache_module(), fn)
+    device = t.get_device()
     if device < 0:
         raise ValueError("the paged cache's tensors live on a GPU")
-    fields = []
-    for t in tensors:
-        if t.get_device() != device:
-            raise ValueError("tensors on several devices")
-        dtype = _DT.get(t.dtype)
-        if dtype is None:
-            raise TypeError("unsupported dtype %s" % t.dtype)
-        shape, stride = t.shape, t.stride()
-        n = len(stride)
-        if n == 5:  # V pages: the rows of a page's tiles one after the other
-            if shape[2] > 1 and stride[2] != shape[3] * stride[3]:
-                raise ValueError("v's last three dims must be contiguous")
-            shape = (shape[0], shape[1], shape[2] * shape[3], shape[4])
-            stride = (stride[0], stride[1], stride[3], stride[4])
-            n = 4
-        elif n > 4:
-            raise ValueError("at most 4 dimensions")
-        pad = _PAD[n]
-        fields += (t.data_ptr(), dtype, n, *shape, *pad, *stride, *pad)
-    pack = _PACK.get(len(tensors))
-    if pack is None:  # data, dtype, ndim, shape[4], stride[4]
-        pack = _PACK[len(tensors)] = struct.Struct("=" + "Qii8q" * len(tensors))
-    memory = ctypes.create_string_buffer(pack.pack(*fields), pack.size)
-    return memory, ctypes.addressof(memory), device
-
-
-def _call(fn: str, device: int, stream, *args):
-    """Calls fn with `device` current, on `stream` or the device's current one."""
-    if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(device)
-    elif hasattr(stream, "cuda_stream"):
-        stream = stream.cuda_stream
+    if stream is not None:
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=device)
+        with torch.cuda.stream(stream):
+            return f(*args, stream.cuda_stream)
     if device == torch.cuda.current_device():
-        status = getattr(load(), fn)(*args, int(stream))
-    else:
-        with torch.cuda.device(device):
-            status = getattr(load(), fn)(*args, int(stream))
-    if status != 0:
-        raise MobaError(fn, status)
-
-
-def _allocating(stream):
-    """Where a call's own tensors are allocated: for the stream that it runs on, so that
-    memory it drops is not given out again before the call is done with it."""
-    if stream is None:
-        return contextlib.nullcontext()
-    if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream))
-    return torch.cuda.stream(stream)
+        return f(*args, torch._C._cuda_getCurrentRawStream(device))
+    with torch.cuda.device(device):
+        return f(*args, torch._C._cuda_getCurrentRawStream(device))
 
 
 def cache_new(num_pages: int, num_kv_heads: int, page_size: int = 64, device="cuda") -> PagedCache:
@@ -421,32 +394,18 @@ def cache_plan(add, lens, table, free_pages, num_free, page_size: int, num_token
     the new tokens'.  Requests that do not fit are refused whole (their slots are -1).
     lens_out and num_free_out may be lens and num_free themselves: a captured step then
     carries its state from replay to replay."""
-    S = add.shape[0]
-    if slots is not None and slots.shape[0] != num_tokens:
-        raise ValueError("slots has %d rows, num_tokens is %d" % (slots.shape[0], num_tokens))
-    with _allocating(stream):
-        mine = add.new_empty((2 * S + 3,), dtype=torch.int32).split_with_sizes((S, S + 1, 1, 1))
-        if slots is None:
-            slots = add.new_empty((int(num_tokens),), dtype=torch.int64)
-    lens_out = mine[0] if lens_out is None else lens_out
-    cu_new = mine[1] if cu_new is None else cu_new
-    num_free_out = mine[2] if num_free_out is None else num_free_out
-    refused = mine[3] if refused is None else refused
-    _memory, at, device = _descs((add, lens, table, free_pages, num_free, lens_out, num_free_out,
-                                  cu_new, slots, refused))
-    d = [at + _DESC_BYTES * i for i in range(10)]
-    _call("moba_cache_plan", device, stream, *d[:5], int(page_size), *d[5:])
-    return CachePlan(cu_new, slots, lens_out, num_free_out, refused)
+    status, *out = _cache_call("plan", add, stream, add, lens, table, free_pages, num_free, page_size,
+                               num_tokens, lens_out, num_free_out, cu_new, slots, refused)
+    if status:
+        raise MobaError("moba_cache_plan", status)
+    return CachePlan(*out)
 
 
 def cache_write(k, v, slots, cache: PagedCache, stream=None) -> None:
     """Quantises new keys and values [T, Hkv, 128] (bf16 or fp32) into their slots [T]
     int64 (negative: left out), as cache_plan() gives them: a page's tokens are
     consecutive rows with ascending slots."""
-    _memory, at, device = _descs((k, v, slots, *cache))
-    d = [at + _DESC_BYTES * i for i in range(8)]
-    c = (ctypes.c_void_p * 5)(*d[3:])
-    _call("moba_cache_write", device, stream, *d[:3], ctypes.addressof(c))
+    _check("moba_cache_write", _cache_call("write", k, stream, k, v, slots, cache))
 
 
 def cache_decode_workspace_bytes(num_requests: int, table_width: int, num_q_heads: int,
@@ -467,24 +426,10 @@ def cache_decode(q, cache: PagedCache, table, lens, block_size: int, topk: int, 
     cache_decode_workspace_bytes() of it; by default a fresh one per call, so that calls on
     several streams and captured graphs share nothing.  Returns (out [S, Hq, 128], lse
     [Hq, S])."""
-    S, Hq = q.shape[0], q.shape[1]
-    if workspace is not None and (workspace.device != q.device or not workspace.is_contiguous()):
-        raise ValueError("workspace must be contiguous and on q's device")
-    with _allocating(stream):
-        if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        if lse is None:
-            lse = q.new_empty((Hq, S), dtype=torch.float32)
-        if workspace is None:
-            k = cache.k.shape
-            n = load().moba_cache_decode_workspace_bytes(S, table.shape[1], Hq, k[1], k[2],
-                                                         int(block_size), int(topk))
-            workspace = q.new_empty((max(n, 16),), dtype=torch.uint8)
-    _memory, at, device = _descs((q, table, lens, out, lse, *cache))
-    d = [at + _DESC_BYTES * i for i in range(10)]
-    c = (ctypes.c_void_p * 5)(*d[5:])
-    _call("moba_cache_decode", device, stream, d[0], ctypes.addressof(c), d[1], d[2],
-          int(block_size), int(topk), d[3], d[4], workspace.data_ptr(), workspace.nbytes)
+    status, out, lse = _cache_call("decode", q, stream, q, cache, table, lens, block_size, topk, out,
+                                   lse, workspace)
+    if status:
+        raise MobaError("moba_cache_decode", status)
     return out, lse
 
 

@@ -2,8 +2,9 @@
 
     python -m paper_2502_13189_amd.build
 
-Every source under csrc/ is compiled to an object in parallel, then linked
-into paper_2502_13189_amd/libmoba.so.  Packed fp32 instructions are disabled
+Every HIP source under csrc/ is compiled to an object in parallel, then linked
+into paper_2502_13189_amd/libmoba.so; csrc/cache_binding.cpp becomes the Python module
+paper_2502_13189_amd/_cache_binding.so, which calls it.  Packed fp32 instructions are disabled
 for the device code (hipcc's host pass warns that it does not know the
 feature; that warning is expected).
 """
@@ -21,6 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoba.so")
+MODULE = os.path.join(HERE, "_cache_binding.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -46,8 +48,34 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_module() -> None:
+    """The Python module (host code alone), against libmoba.so beside it and torch."""
+    import sysconfig
+
+    import torch
+
+    at = os.path.dirname(torch.__file__)
+    tmp = MODULE + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           "-I" + INCLUDE, "-isystem", "/opt/rocm/include",
+           "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(at, "include"),
+           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           os.path.join(CSRC, "cache_binding.cpp"), "-o", tmp, "-L" + HERE, "-l:libmoba.so",
+           "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(at, "lib"), "-ltorch_python", "-ltorch",
+           "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for cache_binding.cpp:\n" + r.stdout + r.stderr)
+    if r.stderr.strip():
+        sys.stderr.write(r.stderr)
+    os.replace(tmp, MODULE)
+
+
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source and link libmoba.so; returns its path."""
+    """Compile every HIP source, link libmoba.so and build the module that calls it; returns
+    the library's path."""
     os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
@@ -58,6 +86,7 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stdout + r.stderr)
     os.replace(tmp, LIB)
+    _build_module()
     if verbose:
         print("built", LIB)
     return LIB
