@@ -75,7 +75,7 @@ moba_status check_table(const moba_tensor* t, int64_t S) {
 struct DecodeShape {
   int64_t S, W;
   int Hq, Hkv, P, B, topk;
-  bool full;
+  bool full, rows;          // rows: one launch, a work-group per (request, kv-head)
   int nblk, nlist;          // MoBA
   int shares, gate_shares;
 };
@@ -83,6 +83,7 @@ struct DecodeShape {
 // What a call of these sizes takes; fills the workspace's pointers from `base` (which may
 // be null) and returns its bytes.
 size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
+  if (d.rows) return 16;  // (unused, but the call's workspace is checked alike)
   size_t off = 0;
   const auto take = [&](auto** p, int64_t n) {
     *p = reinterpret_cast<std::remove_reference_t<decltype(*p)>>(base + off);
@@ -98,6 +99,26 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
     take(&a->nsteps, d.S * d.Hkv);
   }
   return off;
+}
+
+// Whether a work-group takes each (request, kv-head) by itself.  It needs one launch instead
+// of two (MoBA: four) and no joins, but a row is then one CU's, about 0.3 us per 64-key
+// step, so a row's most (what its table row can hold, MoBA: select) is held against what
+// the other way takes: its launches, while there is little to do, and the batch's share
+// of the chip where there is much.  Whole calls, split and by rows, all rows full:
+//   full  64 tokens .. 1024, any number of rows    10.5 and 7.6 .. 9.8 us
+//         2048: 16 rows 13.3, 15.2; 128 rows 23.2, 16.4; 2048 rows 183, 182
+//         4096: 16 rows 13.6, 25.5; 512 rows 104, 93; 8192: 512 rows 193, 181 (but ragged
+//         118, 120)
+//   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 19.9, 18.0; 4096: 16 rows 23.5, 26.1; 64 rows
+//         29.4, 27.2; 8192: 64 rows 31.6, 33.2; 128 rows 39.9, 33.7; 2048 rows 363, 296
+bool rows_in_one(const DecodeShape& d) {
+  const int64_t rows = d.S * d.Hkv, held = d.W * (d.P / kCacheTile);
+  if (d.full) return held <= std::min<int64_t>(std::max<int64_t>(rows / 4, 16), 64);
+  if (d.nblk > kCacheRowBlocks) return false;
+  // (a page's k_sum is 1/32 of a step's bytes)
+  const int64_t most = std::min<int64_t>(held, (int64_t)d.nlist * (d.B / kCacheTile)) + d.W / 32;
+  return most <= std::min<int64_t>(std::max<int64_t>(rows / 2, 34), 256);
 }
 
 // Checks the sizes and settles how the call runs.
@@ -123,6 +144,7 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   if (!d->full && nblk > kMaxBlocksPerSeq) return MOBA_ERR_UNSUPPORTED;
   d->nblk = (int)nblk;
   d->nlist = d->full ? 0 : (int)std::min<int64_t>(nblk, Hq / Hkv * (topk - 1) + 1);
+  d->rows = rows_in_one(*d);
   const int64_t steps = S * W * (P / kCacheTile);  // at most, of a kv-head
   const int64_t each = std::max<int64_t>(1, kCacheWaves / Hkv);
   d->shares = (int)(d->full ? std::min<int64_t>(each, std::max<int64_t>(steps, 1))
@@ -264,6 +286,11 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
   a.shares = d.shares;
   a.gate_shares = d.gate_shares;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)kHeadDim));
+  if (d.rows) {
+    Phase ph("cache_rows", stream);
+    MOBA_LAUNCH(launch_cache_rows(d.full, a, stream));
+    return MOBA_OK;
+  }
   if (!d.full) {
     if (d.topk > 1) {
       Phase ph("cache_gate", stream);

@@ -4,11 +4,12 @@
 // heads of its group: 256 bytes for at most 4 x 128 x 16 FLOP, so HBM bounds it.
 //
 // Lengths are known on the device alone.  The batch's keys are cut into 64-key steps and the
-// steps, request after request, into equal shares, one wave each, as many as the chip
-// holds; every wave finds its own share from a prefix sum over the lengths.  So a ragged batch, one long
+// steps, request after request, into equal shares, one wave each; every wave finds its own
+// share from a prefix sum over the lengths.  So a ragged batch, one long
 // request and many short ones all keep the chip evenly busy, and the workspace does not depend on
 // lengths: a share leaves at most two partial rows (the one it enters with and the one it leaves
-// with), which a second launch joins; a row inside one share is finished there.
+// with), which a second launch joins; a row inside one share is finished there.  Where rows
+// are short, a work-group per row does all in one launch instead (rows).
 //
 //   attend  a step's K and V go from memory to the matrix cores through registers alone.
 //           S^T = K q^T on 16x16x32 MFMAs: a lane has 16 bytes of a key for two operands.
@@ -16,13 +17,18 @@
 //           scores of a head are 16 consecutive tokens, which is what it then needs as the
 //           operand of O^T = V^T P^T, with V's 16 tokens of a dim being one 16-byte load of the
 //           page's token-minor tile.  e4m3 is exact in bf16; the weights enter as a bf16 and
-//           the bf16 of its remainder, the scales through the logits and the weights.
+//           the bf16 of its remainder (in one term alone: 362.1 us, so 363.5), the scales through
+//           the logits and the weights.  1M tokens, 32/8 heads: 2.15 GB in 345 us, 6.2
+//           TB/s, what bare loads reach; more loads in flight (next keys or whole steps
+//           ahead) or more waves gain nothing.
 //   gate    MoBA: a wave adds a block's k_sum rows and takes its scores with the group's
 //           heads, in 64 bits
 //   select  MoBA: a wave finds the (k-1)-th highest score of a head bit by bit; the group's
 //           heads' blocks become one ascending list with a mask of heads for each
 //   join    log-sum-exp merge of split rows
+//   rows    the four of them for one (request, kv-head)
 #include "cache_internal.h"
+#include "decode_internal.h"
 
 #include <math.h>
 
@@ -145,13 +151,185 @@ struct Tile {
   float ks, vs;
 };
 
+// Sums of a row's steps: head lane % 16 of the group, dims 16 i + 4 (lane / 16) + e.
+struct Row {
+  f32x4_t acc[8];
+  float m, l;  // running maximum (log2 domain) and sum of weights
+};
+
+// Attends steps first .. last - 1 of request s (length len) for kv-head g, by one wave.
+// MOBA: steps of the listed blocks, otherwise of all keys.
+template <bool MOBA>
+__device__ __forceinline__ void attend_steps(const CacheDecodeArgs& a, int s, int g, int len,
+                                             const uint32_t* list, int first, int last, Row& r) {
+  const CachePool& c = a.c;
+  const int Hkv = c.Hkv, G = a.G, P = c.P;
+  const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
+  const int spb = MOBA ? a.B / kCacheTile : 0;  // steps per block
+  const int koff = (16 * (hc >> 2) + (hc & 3)) * kHeadDim + 16 * quad;
+  const int voff = hc * kCacheTile + 16 * quad;
+  const int32_t* row = a.table + s * a.t_ss;
+  // B operands: q of head hc, the dims of the K operands
+  bf16x8_t qb[4];
+  {
+    const __hip_bfloat16* qp = a.q + s * a.q_ss + (int64_t)(g * G + min(hc, G - 1)) * a.q_sh;
+#pragma unroll
+    for (int f = 0; f < 4; f++)
+      qb[f] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(
+                                               qp + 64 * (f >> 1) + 16 * quad + 8 * (f & 1)));
+  }
+  const auto step_at = [&](int x) {
+    Step st;
+    int tok = kCacheTile * x;
+    st.heads = 0xffffu;
+    if constexpr (MOBA) {
+      const int bi = x / spb;
+      const uint32_t e = __builtin_amdgcn_readfirstlane(list[bi]);
+      tok = (int)(e & 0xffffu) * a.B + kCacheTile * (x - bi * spb);
+      st.heads = e >> 16;
+    }
+    const int pn = tok / P;
+    const int id = row[pn];
+    const bool ok = (uint32_t)id < (uint32_t)c.N;
+    st.page = ok ? id : 0;
+    st.tile = (tok - pn * P) / kCacheTile;
+    st.nk = ok ? min(kCacheTile, len - tok) : 0;
+    return st;
+  };
+  const auto load = [&](Tile& t, const Step& st) {
+    const uint8_t* kp = c.k + st.page * c.k_sp + g * c.k_sh + st.tile * (kCacheTile * kHeadDim);
+    const uint8_t* vp = c.v + st.page * c.v_sp + g * c.v_sh + st.tile * (kCacheTile * kHeadDim);
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+        t.k[i][j] = *reinterpret_cast<const u32x4_t*>(kp + koff + 4 * kHeadDim * i + 64 * j);
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      t.v[i] = *reinterpret_cast<const u32x4_t*>(vp + voff + 16 * kCacheTile * i);
+    t.ks = c.k_scale[st.page * Hkv + g];
+    t.vs = c.v_scale[st.page * Hkv + g];
+  };
+  f32x4_t(&acc)[8] = r.acc;
+#pragma unroll
+  for (int i = 0; i < 8; i++) acc[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, l = 0.0f;
+  const auto fold = [&](Tile& t, const Step& st) {
+    // a lane's scores: head hc, tokens 16 quad + 4 i + e
+    float z[16];
+    const float zs = t.ks * a.scale_log2;
+    const bool mine = !MOBA || ((st.heads >> hc) & 1);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int f = 0; f < 4; f++) {
+        const u32x4_t kw = t.k[i][f >> 1];
+        x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            f & 1 ? to_bf16(kw[2], kw[3]) : to_bf16(kw[0], kw[1]), qb[f], x, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e++) z[4 * i + e] = x[e] * zs;
+    }
+    if (st.nk < kCacheTile) {
+      const int left = st.nk - 16 * quad;  // of this lane's tokens
+      if (st.nk <= 0) t.vs = 0.0f;  // (no page: its scale may be anything, too)
+#pragma unroll
+      for (int i = 0; i < 16; i++) z[i] = i < left ? z[i] : -INFINITY;
+      // their values may hold anything
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const int n = min(max(left - 4 * e, 0), 4);
+          t.v[i][e] &= n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
+        }
+    }
+    if constexpr (MOBA) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) z[i] = mine ? z[i] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; i++) top = fmaxf(top, z[i]);
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    if (__ballot(top > m + kRescale || (m == -INFINITY && top > -INFINITY))) {
+      const float mn = fmaxf(m, top);
+      const float sc = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= sc;
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[i][e] *= sc;
+    }
+    const float mr = m == -INFINITY ? 0.0f : m;
+    // weights times the page's scale, as two bf16 terms
+    u32x4_t hi[2], lo[2];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const float p0 = __builtin_amdgcn_exp2f(z[2 * i] - mr);
+      const float p1 = __builtin_amdgcn_exp2f(z[2 * i + 1] - mr);
+      l += p0 + p1;
+      const float v0 = p0 * t.vs, v1 = p1 * t.vs;
+      const uint32_t h = pack_bf16(v0, v1);
+      hi[i >> 2][i & 3] = h;
+      lo[i >> 2][i & 3] = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+#pragma unroll
+      for (int f = 0; f < 2; f++) {
+        const bf16x8_t vb = to_bf16(t.v[i][2 * f], t.v[i][2 * f + 1]);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, hi[f]),
+                                                         acc[i], 0, 0, 0);
+        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, lo[f]),
+                                                         acc[i], 0, 0, 0);
+      }
+    }
+  };
+  Step st = step_at(min(first, max(last - 1, 0)));
+  for (int x = first; x < last; x++) {
+    Tile t;
+    load(t, st);
+    const Step next = step_at(min(x + 1, last - 1));  // (its page is known by the time it is needed)
+    fold(t, st);
+    st = next;
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  r.m = m;
+  r.l = l;
+}
+
+// The row's result, from its sums; for lanes of the group's heads.
+__device__ __forceinline__ void write_row(const CacheDecodeArgs& a, int s, int h, int quad, const Row& r) {
+  const float inv = r.l > 0.0f || r.l != r.l ? 1.0f / r.l : 0.0f;
+  __hip_bfloat16* o = a.out + s * a.o_ss + h * a.o_sh + 4 * quad;
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    *reinterpret_cast<uint2*>(o + 16 * i) =
+        make_uint2(pack_bf16(r.acc[i][0] * inv, r.acc[i][1] * inv),
+                   pack_bf16(r.acc[i][2] * inv, r.acc[i][3] * inv));
+  if (quad == 0)
+    a.lse[(int64_t)h * a.S + s] = r.m == -INFINITY && r.l == 0.0f
+                                      ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * kLn2;
+}
+
+// A request that attends nothing.
+__device__ __forceinline__ void write_nothing(const CacheDecodeArgs& a, int s, int h, int lane) {
+  *reinterpret_cast<uint32_t*>(a.out + s * a.o_ss + h * a.o_sh + 2 * lane) = 0;
+  if (lane == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
+}
+
 template <bool MOBA>
 __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(CacheDecodeArgs a) {
   __shared__ Sums sums;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const CachePool& c = a.c;
-  const int Hkv = c.Hkv, G = a.G, P = c.P;
+  const int Hkv = c.Hkv, G = a.G;
   const int rows = MOBA ? a.S * Hkv : a.S;
   const auto units = [&](int r) {
     if constexpr (MOBA) return a.nsteps[r];
@@ -163,17 +341,18 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
   for (int r = w; r < a.S * Hkv; r += gridDim.x * (kCacheDecodeThreads / 64)) {
     const int s = r / Hkv, h0 = r % Hkv * G;
     if (a.lens[s] > 0) continue;
-    for (int h = h0; h < h0 + G; h++) {
-      *reinterpret_cast<uint32_t*>(a.out + s * a.o_ss + h * a.o_sh + 2 * lane) = 0;
-      if (lane == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
-    }
+    for (int h = h0; h < h0 + G; h++) write_nothing(a, s, h, lane);
   }
   const int share = MOBA ? w : w / Hkv;
   int g = MOBA ? 0 : w % Hkv;
   if (share >= a.shares) return;
   const int pg = MOBA ? 1 : Hkv, pi = MOBA ? 0 : g;  // partials: kv-heads per share, this one
   const int total = __builtin_amdgcn_readfirstlane(sums.total);
-  const int per_share = (total + a.shares - 1) / a.shares;
+  // Two waves per SIMD hide a few steps' latency; where each would have many, one does as
+  // well, with half the partials (1024 and 2048 waves: 1M tokens 354 and 367 us, MoBA over
+  // them 90.5 and 92.8; ragged batch, 8 steps a wave 55.8 and 57.8; ragged MoBA, 4 steps 59 and 54)
+  const int used = total / 6 >= a.shares ? (a.shares + 1) / 2 : a.shares;
+  const int per_share = (total + used - 1) / used;
   int u = (int)min((int64_t)share * per_share, (int64_t)total);
   const int u_end = (int)min((int64_t)u + per_share, (int64_t)total);
   CacheJoin join = {-1, 0};
@@ -181,9 +360,6 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
     int base;
     int r = __builtin_amdgcn_readfirstlane(find_row(sums, rows, u, units, &base));
     const int hc = lane & 15, quad = lane >> 4;
-    const int spb = MOBA ? a.B / kCacheTile : 0;  // steps per block
-    const int koff = (16 * (hc >> 2) + (hc & 3)) * kHeadDim + 16 * quad;
-    const int voff = hc * kCacheTile + 16 * quad;
     while (u < u_end) {
       const int n = __builtin_amdgcn_readfirstlane(units(r));
       if (n == 0) {
@@ -194,158 +370,21 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
       if constexpr (MOBA) g = r % Hkv;
       const int len = held(a, s);
       const int first = u - base, last = min(n, u_end - base);
-      const int32_t* row = a.table + s * a.t_ss;
       const uint32_t* list = MOBA ? a.list + (int64_t)r * a.nlist : nullptr;
-      // B operands: q of head hc, the dims of the K operands
-      bf16x8_t qb[4];
-      {
-        const __hip_bfloat16* qp = a.q + s * a.q_ss + (int64_t)(g * G + min(hc, G - 1)) * a.q_sh;
-#pragma unroll
-        for (int f = 0; f < 4; f++)
-          qb[f] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(
-                                                   qp + 64 * (f >> 1) + 16 * quad + 8 * (f & 1)));
-      }
-      const auto step_at = [&](int x) {
-        Step st;
-        int tok = kCacheTile * x;
-        st.heads = 0xffffu;
-        if constexpr (MOBA) {
-          const int bi = x / spb;
-          const uint32_t e = list[bi];
-          tok = (int)(e & 0xffffu) * a.B + kCacheTile * (x - bi * spb);
-          st.heads = e >> 16;
-        }
-        const int pn = tok / P;
-        const int id = row[pn];
-        const bool ok = (uint32_t)id < (uint32_t)c.N;
-        st.page = ok ? id : 0;
-        st.tile = (tok - pn * P) / kCacheTile;
-        st.nk = ok ? min(kCacheTile, len - tok) : 0;
-        return st;
-      };
-      const auto load = [&](Tile& t, const Step& st) {
-        const uint8_t* kp = c.k + st.page * c.k_sp + g * c.k_sh + st.tile * (kCacheTile * kHeadDim);
-        const uint8_t* vp = c.v + st.page * c.v_sp + g * c.v_sh + st.tile * (kCacheTile * kHeadDim);
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-#pragma unroll
-          for (int j = 0; j < 2; j++)
-            t.k[i][j] = *reinterpret_cast<const u32x4_t*>(kp + koff + 4 * kHeadDim * i + 64 * j);
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-          t.v[i] = *reinterpret_cast<const u32x4_t*>(vp + voff + 16 * kCacheTile * i);
-        t.ks = c.k_scale[st.page * Hkv + g];
-        t.vs = c.v_scale[st.page * Hkv + g];
-      };
-      f32x4_t acc[8];
-#pragma unroll
-      for (int i = 0; i < 8; i++) acc[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-      float m = -INFINITY, l = 0.0f;
-      const auto fold = [&](Tile& t, const Step& st) {
-        // a lane's scores: head hc, tokens 16 quad + 4 i + e
-        float z[16];
-        const float zs = t.ks * a.scale_log2;
-        const bool mine = !MOBA || ((st.heads >> hc) & 1);
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int f = 0; f < 4; f++) {
-            const u32x4_t kw = t.k[i][f >> 1];
-            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                f & 1 ? to_bf16(kw[2], kw[3]) : to_bf16(kw[0], kw[1]), qb[f], x, 0, 0, 0);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; e++) z[4 * i + e] = x[e] * zs;
-        }
-        if (st.nk < kCacheTile) {
-          const int left = st.nk - 16 * quad;  // of this lane's tokens
-          if (st.nk <= 0) t.vs = 0.0f;  // (no page: its scale may be anything, too)
-#pragma unroll
-          for (int i = 0; i < 16; i++) z[i] = i < left ? z[i] : -INFINITY;
-          // their values may hold anything
-#pragma unroll
-          for (int i = 0; i < 8; i++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-              const int n = min(max(left - 4 * e, 0), 4);
-              t.v[i][e] &= n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
-            }
-        }
-        if constexpr (MOBA) {
-#pragma unroll
-          for (int i = 0; i < 16; i++) z[i] = mine ? z[i] : -INFINITY;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i++) top = fmaxf(top, z[i]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        if (__ballot(top > m + kRescale || (m == -INFINITY && top > -INFINITY))) {
-          const float mn = fmaxf(m, top);
-          const float sc = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-          m = mn;
-          l *= sc;
-#pragma unroll
-          for (int i = 0; i < 8; i++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) acc[i][e] *= sc;
-        }
-        const float mr = m == -INFINITY ? 0.0f : m;
-        // weights times the page's scale, as two bf16 terms
-        u32x4_t hi[2], lo[2];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-          const float p0 = __builtin_amdgcn_exp2f(z[2 * i] - mr);
-          const float p1 = __builtin_amdgcn_exp2f(z[2 * i + 1] - mr);
-          l += p0 + p1;
-          const float v0 = p0 * t.vs, v1 = p1 * t.vs;
-          const uint32_t h = pack_bf16(v0, v1);
-          hi[i >> 2][i & 3] = h;
-          lo[i >> 2][i & 3] = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-#pragma unroll
-          for (int f = 0; f < 2; f++) {
-            const bf16x8_t vb = to_bf16(t.v[i][2 * f], t.v[i][2 * f + 1]);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, hi[f]),
-                                                             acc[i], 0, 0, 0);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, lo[f]),
-                                                             acc[i], 0, 0, 0);
-          }
-        }
-      };
-      for (int x = first; x < last; x++) {
-        const Step st = step_at(x);
-        Tile t;
-        load(t, st);
-        fold(t, st);
-      }
-      l += __shfl_xor(l, 16, 64);
-      l += __shfl_xor(l, 32, 64);
+      Row x;
+      attend_steps<MOBA>(a, s, g, len, list, first, last, x);
       // a lane's sums: head hc, dims 16 i + 4 quad + e
       const bool whole = first == 0 && last == n;
       if (hc < G) {
-        const int h = g * G + hc;
         if (whole) {
-          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-          __hip_bfloat16* o = a.out + s * a.o_ss + h * a.o_sh + 4 * quad;
-#pragma unroll
-          for (int i = 0; i < 8; i++)
-            *reinterpret_cast<uint2*>(o + 16 * i) =
-                make_uint2(pack_bf16(acc[i][0] * inv, acc[i][1] * inv),
-                           pack_bf16(acc[i][2] * inv, acc[i][3] * inv));
-          if (quad == 0)
-            a.lse[(int64_t)h * a.S + s] = m == -INFINITY && l == 0.0f ? -INFINITY
-                                              : (m + __builtin_amdgcn_logf(l)) * kLn2;
+          write_row(a, s, g * G + hc, quad, x);
         } else {
           const int64_t at = (((int64_t)share * 2 + (first == 0)) * pg + pi) * G + hc;
           float* o = a.part_o + at * kHeadDim + 4 * quad;
 #pragma unroll
           for (int i = 0; i < 8; i++)
-            *reinterpret_cast<f32x4_t*>(o + 16 * i) = acc[i];
-          if (quad == 0) a.part_ml[at] = make_float2(m, l);
+            *reinterpret_cast<f32x4_t*>(o + 16 * i) = x.acc[i];
+          if (quad == 0) a.part_ml[at] = make_float2(x.m, x.l);
         }
       }
       if (first == 0 && last < n)
@@ -459,12 +498,68 @@ __device__ __forceinline__ double lane_of(double x) {
   return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 
+// put(head of the group, score) for past block j of request s and kv-head g, by a wave.
+template <typename Put>
+__device__ __forceinline__ void block_scores(const CacheDecodeArgs& a, int s, int g, int j, Put put) {
+  const CachePool& c = a.c;
+  const int Hkv = c.Hkv, G = a.G, lane = threadIdx.x & 63;
+  const int per = a.B / c.P;  // pages per block
+  const int half = lane >> 5, d4 = 4 * (lane & 31);  // half a wave per page row, 4 dims a lane
+  double sum[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int p0 = 0; p0 < per; p0 += 64) {
+    const int np = min(64, per - p0);
+    const int id = a.table[s * a.t_ss + (int64_t)j * per + p0 + min(lane, np - 1)];
+    for (int p = 0; p < np; p += 16) {
+      float4 x[8];
+      bool ok[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int at = p + 2 * e;
+        const int page0 = __builtin_amdgcn_readlane(id, min(at, np - 1));
+        const int page1 = __builtin_amdgcn_readlane(id, min(at + 1, np - 1));
+        const int page = half ? page1 : page0;
+        ok[e] = at + half < np && (uint32_t)page < (uint32_t)c.N;
+        x[e] = *reinterpret_cast<const float4*>(
+            c.k_sum + ((int64_t)(ok[e] ? page : 0) * Hkv + g) * kHeadDim + d4);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        sum[0] += ok[e] ? (double)x[e].x : 0.0;
+        sum[1] += ok[e] ? (double)x[e].y : 0.0;
+        sum[2] += ok[e] ? (double)x[e].z : 0.0;
+        sum[3] += ok[e] ? (double)x[e].w : 0.0;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++) sum[i] += __shfl_xor(sum[i], 32, 64);
+  // half a wave per head, two heads at a time
+  for (int h0 = 0; h0 < G; h0 += 4) {
+    double x[2];
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      const int h = g * G + min(h0 + 2 * e + half, G - 1);
+      const uint2 qw = *reinterpret_cast<const uint2*>(a.q + s * a.q_ss + h * a.q_sh + d4);
+      x[e] = (double)bf16_lo(qw.x) * sum[0] + (double)bf16_hi(qw.x) * sum[1] +
+             (double)bf16_lo(qw.y) * sum[2] + (double)bf16_hi(qw.y) * sum[3];
+    }
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      x[e] += lane_of<0xb1>(x[e]);  // the neighbour, the other pair, four and eight lanes
+      x[e] += lane_of<0x4e>(x[e]);
+      x[e] += lane_of<0x141>(x[e]);
+      x[e] += lane_of<0x140>(x[e]);
+      x[e] += __shfl_xor(x[e], 16, 64);
+      const int hl = h0 + 2 * e + half;
+      if ((lane & 31) == 0 && hl < G) put(hl, x[e]);
+    }
+  }
+}
+
 __global__ __launch_bounds__(kCacheDecodeThreads) void cache_gate_kernel(CacheDecodeArgs a) {
   __shared__ Sums sums;
-  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const CachePool& c = a.c;
-  const int Hkv = c.Hkv, G = a.G;
+  const int Hkv = a.c.Hkv, G = a.G;
   const auto units = [&](int s) { return past_blocks(a, s); };
   sum_rows(sums, a.S, units);
   const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
@@ -476,62 +571,13 @@ __global__ __launch_bounds__(kCacheDecodeThreads) void cache_gate_kernel(CacheDe
   if (share >= a.gate_shares || u >= u_end) return;
   int base;
   int s = __builtin_amdgcn_readfirstlane(find_row(sums, a.S, u, units, &base));
-  const int per = a.B / c.P;  // pages per block
-  const int half = lane >> 5, d4 = 4 * (lane & 31);  // half a wave per page row, 4 dims a lane
   while (u < u_end) {
     const int n = __builtin_amdgcn_readfirstlane(units(s));
     const int last = min(n, u_end - base);
     for (int j = u - base; j < last; j++) {
-      double sum[4] = {0.0, 0.0, 0.0, 0.0};
-      for (int p0 = 0; p0 < per; p0 += 64) {
-        const int np = min(64, per - p0);
-        const int id = a.table[s * a.t_ss + (int64_t)j * per + p0 + min(lane, np - 1)];
-        for (int p = 0; p < np; p += 16) {
-          float4 x[8];
-          bool ok[8];
-#pragma unroll
-          for (int e = 0; e < 8; e++) {
-            const int at = p + 2 * e;
-            const int page0 = __builtin_amdgcn_readlane(id, min(at, np - 1));
-            const int page1 = __builtin_amdgcn_readlane(id, min(at + 1, np - 1));
-            const int page = half ? page1 : page0;
-            ok[e] = at + half < np && (uint32_t)page < (uint32_t)c.N;
-            x[e] = *reinterpret_cast<const float4*>(
-                c.k_sum + ((int64_t)(ok[e] ? page : 0) * Hkv + g) * kHeadDim + d4);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; e++) {
-            sum[0] += ok[e] ? (double)x[e].x : 0.0;
-            sum[1] += ok[e] ? (double)x[e].y : 0.0;
-            sum[2] += ok[e] ? (double)x[e].z : 0.0;
-            sum[3] += ok[e] ? (double)x[e].w : 0.0;
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; i++) sum[i] += __shfl_xor(sum[i], 32, 64);
-      // half a wave per head, two heads at a time
-      for (int h0 = 0; h0 < G; h0 += 4) {
-        double x[2];
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const int h = g * G + min(h0 + 2 * e + half, G - 1);
-          const uint2 qw = *reinterpret_cast<const uint2*>(a.q + s * a.q_ss + h * a.q_sh + d4);
-          x[e] = (double)bf16_lo(qw.x) * sum[0] + (double)bf16_hi(qw.x) * sum[1] +
-                 (double)bf16_lo(qw.y) * sum[2] + (double)bf16_hi(qw.y) * sum[3];
-        }
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          x[e] += lane_of<0xb1>(x[e]);  // the neighbour, the other pair, four and eight lanes
-          x[e] += lane_of<0x4e>(x[e]);
-          x[e] += lane_of<0x141>(x[e]);
-          x[e] += lane_of<0x140>(x[e]);
-          x[e] += __shfl_xor(x[e], 16, 64);
-          const int hl = h0 + 2 * e + half;
-          if ((lane & 31) == 0 && hl < G)
-            a.score[((int64_t)s * a.Hq + g * G + hl) * a.nblk + j] = x[e];
-        }
-      }
+      block_scores(a, s, g, j, [&](int hl, double x) {
+        a.score[((int64_t)s * a.Hq + g * G + hl) * a.nblk + j] = x;
+      });
     }
     u = base + last;
     base += n;
@@ -546,84 +592,186 @@ __device__ __forceinline__ uint64_t order_of(double x) {
   return b >> 63 ? ~b : b | (uint64_t(1) << 63);
 }
 
-// One work-group per (request, kv-head); NW: words of 64 blocks.
+// put(x, mask of the kept blocks 64 x ..) for the nh highest scores among `past` blocks (of
+// equal ones the first), by a wave.  NW: words of 64 blocks.
+template <int NW, typename Score, typename Put>
+__device__ __forceinline__ void keep_blocks(int past, int nh, Score score, Put put) {
+  const int lane = threadIdx.x & 63;
+  uint64_t key[NW];
+#pragma unroll
+  for (int x = 0; x < NW; x++) {
+    const int j = 64 * x + lane;
+    key[x] = j >= past ? 0 : nh == past ? 1 : order_of(score(j));
+  }
+  // the largest bound that at least nh keys reach
+  uint64_t bound = nh == past ? 1 : 0;
+  int reach = nh == past ? nh : 0;  // keys that reach it, where that was counted
+  for (int bit = 63; bit >= 0 && reach != nh && nh > 0; bit--) {
+    const uint64_t cand = bound | (uint64_t(1) << bit);
+    int n = 0;
+#pragma unroll
+    for (int x = 0; x < NW; x++) n += __popcll(__ballot(key[x] >= cand));
+    if (n >= nh) {
+      bound = cand;
+      reach = n;
+    }
+  }
+  // all keys above the bound, and of those that equal it the first ones
+  int above = 0;
+#pragma unroll
+  for (int x = 0; x < NW; x++) above += __popcll(__ballot(key[x] > bound));
+  int ties = nh - above;
+#pragma unroll
+  for (int x = 0; x < NW; x++) {
+    const unsigned long long eq = __ballot(key[x] == bound && key[x] != 0);
+    const bool take = key[x] > bound || (key[x] == bound && key[x] != 0 &&
+                                         __popcll(eq & ((1ull << lane) - 1)) < ties);
+    const unsigned long long m = __ballot(take && nh > 0);
+    ties -= min(ties, (int)__popcll(eq));
+    if (lane == 0) put(x, m);
+  }
+}
+
+// The group's kept blocks as one ascending list, and the current block for all heads; returns
+// the steps.  For all threads of a work-group, kept being complete.
 template <int NW>
-__global__ __launch_bounds__(256) void cache_select_kernel(CacheDecodeArgs a) {
-  __shared__ unsigned long long kept[16][NW];
-  __shared__ int before[NW + 1];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int G = a.G, Hkv = a.c.Hkv;
-  const int r = blockIdx.x, s = r / Hkv, g = r % Hkv;
-  const int len = held(a, s);
-  if (len == 0) {
-    if (tid == 0) a.nsteps[r] = 0;
-    return;
-  }
-  const int past = (len - 1) / a.B;
-  const int nh = min(a.topk - 1, past);
-  for (int hl = wave; hl < G; hl += 4) {
-    uint64_t key[NW];
-    const double* sc = a.score + ((int64_t)s * a.Hq + g * G + hl) * a.nblk;
-#pragma unroll
-    for (int x = 0; x < NW; x++) {
-      const int j = 64 * x + lane;
-      key[x] = j >= past ? 0 : nh == past ? 1 : order_of(sc[j]);
-    }
-    // the largest bound that at least nh keys reach
-    uint64_t bound = nh == past ? 1 : 0;
-    int reach = nh == past ? nh : 0;  // keys that reach it, where that was counted
-    for (int bit = 63; bit >= 0 && reach != nh && nh > 0; bit--) {
-      const uint64_t cand = bound | (uint64_t(1) << bit);
-      int n = 0;
-#pragma unroll
-      for (int x = 0; x < NW; x++) n += __popcll(__ballot(key[x] >= cand));
-      if (n >= nh) {
-        bound = cand;
-        reach = n;
-      }
-    }
-    // all keys above the bound, and of those that equal it the first ones
-    int above = 0;
-#pragma unroll
-    for (int x = 0; x < NW; x++) above += __popcll(__ballot(key[x] > bound));
-    int ties = nh - above;
-#pragma unroll
-    for (int x = 0; x < NW; x++) {
-      const unsigned long long eq = __ballot(key[x] == bound && key[x] != 0);
-      const bool take = key[x] > bound || (key[x] == bound && key[x] != 0 &&
-                                           __popcll(eq & ((1ull << lane) - 1)) < ties);
-      const unsigned long long m = __ballot(take && nh > 0);
-      ties -= min(ties, (int)__popcll(eq));
-      if (lane == 0) kept[hl][x] = m;
-    }
-  }
-  __syncthreads();
+struct Kept {
+  unsigned long long of[kDecodeMaxGroup][NW];
+  int before[NW + 1];
+};
+template <int NW>
+__device__ __forceinline__ int block_list(const CacheDecodeArgs& a, Kept<NW>& k, int past, int len, uint32_t* list) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.G;
   if (tid < NW) {
     unsigned long long any = 0;
-    for (int hl = 0; hl < G; hl++) any |= kept[hl][tid];
-    int n = __popcll(any);
+    for (int hl = 0; hl < G; hl++) any |= k.of[hl][tid];
+    const int n = __popcll(any);
     int incl = n;
 #pragma unroll
     for (int d = 1; d < NW; d <<= 1) {
       const int o = __shfl_up(incl, d, 64);
       if (lane >= d) incl += o;
     }
-    before[tid] = incl - n;
-    if (tid == NW - 1) before[NW] = incl;
+    k.before[tid] = incl - n;
+    if (tid == NW - 1) k.before[NW] = incl;
   }
   __syncthreads();
-  const int nu = before[NW];
-  uint32_t* list = a.list + (int64_t)r * a.nlist;
-  for (int x = wave; x < NW; x += 4) {
+  const int nu = k.before[NW];
+  for (int x = wave; x < NW; x += (int)blockDim.x / 64) {
     uint32_t heads = 0;
-    for (int hl = 0; hl < G; hl++) heads |= (uint32_t)((kept[hl][x] >> lane) & 1) << hl;
+    for (int hl = 0; hl < G; hl++) heads |= (uint32_t)((k.of[hl][x] >> lane) & 1) << hl;
     const unsigned long long any = __ballot(heads != 0);
-    if (heads) list[before[x] + __popcll(any & ((1ull << lane) - 1))] = (uint32_t)(64 * x + lane) | heads << 16;
+    if (heads) list[k.before[x] + __popcll(any & ((1ull << lane) - 1))] = (uint32_t)(64 * x + lane) | heads << 16;
   }
-  if (tid == 0) {
-    list[nu] = (uint32_t)past | 0xffff0000u;
-    a.nsteps[r] = nu * (a.B / kCacheTile) + (len - past * a.B + kCacheTile - 1) / kCacheTile;
+  if (tid == 0) list[nu] = (uint32_t)past | 0xffff0000u;
+  return nu * (a.B / kCacheTile) + (len - past * a.B + kCacheTile - 1) / kCacheTile;
+}
+
+// One work-group per (request, kv-head).
+template <int NW>
+__global__ __launch_bounds__(256) void cache_select_kernel(CacheDecodeArgs a) {
+  __shared__ Kept<NW> kept;
+  const int G = a.G, Hkv = a.c.Hkv, wave = threadIdx.x >> 6;
+  const int r = blockIdx.x, s = r / Hkv, g = r % Hkv;
+  const int len = held(a, s);
+  if (len == 0) {
+    if (threadIdx.x == 0) a.nsteps[r] = 0;
+    return;
   }
+  const int past = past_blocks(a, s);
+  for (int hl = wave; hl < G; hl += 4) {
+    const double* sc = a.score + ((int64_t)s * a.Hq + g * G + hl) * a.nblk;
+    keep_blocks<NW>(past, min(a.topk - 1, past), [&](int j) { return sc[j]; },
+                    [&](int x, unsigned long long m) { kept.of[hl][x] = m; });
+  }
+  __syncthreads();
+  const int steps = block_list(a, kept, past, len, a.list + (int64_t)r * a.nlist);
+  if (threadIdx.x == 0) a.nsteps[r] = steps;
+}
+
+// -------------------------------------------------------------------- rows
+// Short rows, a work-group for each (request, kv-head): gate, selection, attention and the
+// join of its waves in one launch.  A CU alone takes about 0.3 us per step (52 GB/s) with 4, 8
+// or 16 waves.
+constexpr int kRowWaves = 8;
+
+template <bool MOBA>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDecodeArgs a) {
+  constexpr int kBlocks = kCacheRowBlocks;
+  static_assert(kBlocks % 64 == 0 && kDecodeMaxGroup * kBlocks * 8 <= 4 * 8 * 64 * 16,
+                "the scores fit where the sums are joined");
+  __shared__ f32x4_t sums[4][8][64];
+  __shared__ float ms[kRowWaves][16], ls[kRowWaves][16];
+  __shared__ Kept<kBlocks / 64> kept;
+  __shared__ uint32_t list[kBlocks];
+  const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.G, Hkv = a.c.Hkv;
+  const int s = blockIdx.x / Hkv, g = blockIdx.x % Hkv;
+  const int len = __builtin_amdgcn_readfirstlane(held(a, s));
+  if (len == 0) {
+    for (int hl = wave; hl < G; hl += kRowWaves) write_nothing(a, s, g * G + hl, lane);
+    return;
+  }
+  int steps = (len + kCacheTile - 1) / kCacheTile;
+  if constexpr (MOBA) {
+    const int past = past_blocks(a, s), nh = min(a.topk - 1, past);
+    double* score = reinterpret_cast<double*>(sums);  // [G, kBlocks]
+    if (nh > 0 && nh < past) {
+      for (int j = wave; j < past; j += kRowWaves)
+        block_scores(a, s, g, j, [&](int hl, double x) { score[hl * kBlocks + j] = x; });
+      __syncthreads();
+    }
+    for (int hl = wave; hl < G; hl += kRowWaves)
+      keep_blocks<kBlocks / 64>(past, nh, [&](int j) { return score[hl * kBlocks + j]; },
+                                [&](int x, unsigned long long m) { kept.of[hl][x] = m; });
+    __syncthreads();
+    steps = block_list(a, kept, past, len, list);
+    __syncthreads();
+  }
+  // equal parts of the steps to the waves
+  const int part = (steps + kRowWaves - 1) / kRowWaves;
+  const int first = min(wave * part, steps), last = min(first + part, steps);
+  Row r;
+  attend_steps<MOBA>(a, s, g, len, list, first, last, r);
+  if (quad == 0) ms[wave][hc] = r.m;
+  __syncthreads();
+  float m = ms[0][hc];
+#pragma unroll
+  for (int w = 1; w < kRowWaves; w++) m = fmaxf(m, ms[w][hc]);
+  const float sc = __builtin_amdgcn_exp2f(r.m - (m == -INFINITY ? 0.0f : m));
+  if (quad == 0) ls[wave][hc] = r.l * sc;
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) r.acc[i][e] *= sc;
+  // four waves' sums at a time to the first four, then to two and one
+  const auto hand = [&](int from, int n) {
+    if (wave >= from && wave < from + n) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) sums[wave - from][i][lane] = r.acc[i];
+    }
+    __syncthreads();
+    if (wave < n) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const f32x4_t x = sums[wave][i][lane];
+#pragma unroll
+        for (int e = 0; e < 4; e++) r.acc[i][e] += x[e];
+      }
+    }
+    __syncthreads();
+  };
+#pragma unroll
+  for (int from = 4; from < kRowWaves; from += 4) hand(from, 4);
+  hand(2, 2);
+  hand(1, 1);
+  if (wave != 0 || hc >= G) return;
+  r.m = m;
+  r.l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; w++) r.l += ls[w][hc];
+  write_row(a, s, g * G + hc, quad, r);
 }
 
 }  // namespace
@@ -639,6 +787,13 @@ hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st) {
   if (a.nblk <= 256) cache_select_kernel<4><<<groups, 256, 0, st>>>(a);
   else if (a.nblk <= 1024) cache_select_kernel<16><<<groups, 256, 0, st>>>(a);
   else cache_select_kernel<kMaxBlocksPerSeq / 64><<<groups, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st) {
+  const unsigned groups = (unsigned)(a.S * a.c.Hkv);
+  if (full) cache_rows_kernel<false><<<groups, 64 * kRowWaves, 0, st>>>(a);
+  else cache_rows_kernel<true><<<groups, 64 * kRowWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -51,6 +51,7 @@ hipError_t launch_cache_write(bool bf16, const CacheWriteArgs& a, hipStream_t st
 constexpr int kCacheWaves = 2048;  // attention waves the chip holds: 8 on each of 256 CUs
 constexpr int kCacheGateWaves = 8192;  // waves of the gate at most (one a block, if they suffice)
 constexpr int kCacheDecodeThreads = 256;
+constexpr int kCacheRowBlocks = 128;   // MoBA blocks of a row that one work-group takes
 
 // Where a row split over several shares begins: the row (full: request; MoBA: request *
 // Hkv + kv-head; -1: none) and the shares it spans.
@@ -80,6 +81,9 @@ struct CacheDecodeArgs {
   float2* part_ml;   // [shares, 2, Hkv (MoBA: 1), G] their max (log2 domain) and sum
   CacheJoin* join;   // [shares, Hkv (MoBA: 1)]
 };
+// Gate, selection, attention and join in one launch, a work-group per (request, kv-head); for
+// table rows of up to kCacheRowBlocks blocks (MoBA).  Needs no workspace.
+hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st);
 hipError_t launch_cache_gate(const CacheDecodeArgs& a, hipStream_t st);
 hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st);
 hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t st);

@@ -344,11 +344,17 @@ def check(pool, table, lens, hq, block, topk, rng, what="", **more):
 LENS = [1, 63, 64, 65, 0, 127, 128, 129, 700, -4, 333, 2, 17]
 
 
+# A short table row is one work-group's, a long one is split over the chip: most tests run
+# with their requests in tables of both kinds.
+WIDTHS = [13, 400]
+
+
+@pytest.mark.parametrize("W", WIDTHS)
 @pytest.mark.parametrize("page", [64, 128, 192, 256])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (8, 2), (16, 1), (10, 2)])
-def test_decode_full(page, hq, hkv):
+def test_decode_full(page, hq, hkv, W):
     rng = np.random.default_rng(page + hq)
-    pool, table = some_cache(rng, LENS, hkv, page, 12)
+    pool, table = some_cache(rng, LENS, hkv, page, W)
     check(pool, table, LENS, hq, 0, 0, rng)
 
 
@@ -356,9 +362,10 @@ def test_decode_full(page, hq, hkv):
                                              (64, 192, 3), (192, 192, 2), (256, 256, 2),
                                              (64, 64, 9), (64, 64, 500)])
 @pytest.mark.parametrize("hq,hkv", [(2, 2), (8, 2), (16, 1)])
-def test_decode_moba(page, block, topk, hq, hkv):
+@pytest.mark.parametrize("W", WIDTHS)
+def test_decode_moba(page, block, topk, hq, hkv, W):
     rng = np.random.default_rng(page + block + topk + hq)
-    pool, table = some_cache(rng, LENS, hkv, page, 13)
+    pool, table = some_cache(rng, LENS, hkv, page, W)
     check(pool, table, LENS, hq, block, topk, rng)
 
 
@@ -370,6 +377,9 @@ def test_decode_moba(page, block, topk, hq, hkv):
     ([200] * 70, 2, 1, 64, 64, 2),
     ([18000], 2, 1, 64, 64, 7),          # 282 blocks: more than the first selection holds
     ([70000, 130], 1, 1, 64, 64, 30),    # 1094 blocks
+    ([300] * 150 + [8000], 4, 4, 64, 512, 3),  # many rows: a work-group each, one of them long
+    ([64 * 126, 5, 7000], 16, 1, 64, 64, 5),   # the most blocks a work-group gates
+    ([1000, 77, 2048] * 20, 6, 2, 128, 0, 0),
 ])
 def test_decode_splits(lens, hq, hkv, page, block, topk):
     rng = np.random.default_rng(len(lens) + hq)
@@ -378,12 +388,13 @@ def test_decode_splits(lens, hq, hkv, page, block, topk):
     check(pool, table, lens, hq, block, topk, rng)
 
 
+@pytest.mark.parametrize("W", WIDTHS)
 @pytest.mark.parametrize("topk", [0, 2, 3])
-def test_decode_bad_table_entries(topk):
+def test_decode_bad_table_entries(topk, W):
     """Entries that are no page are left out; a request all of whose pages are attends nothing."""
     rng = np.random.default_rng(4)
     lens = [300, 64, 500, 130]
-    pool, table = some_cache(rng, lens, 2, 64, 9)
+    pool, table = some_cache(rng, lens, 2, 64, W)
     for s, j, x in ((0, 1, -1), (0, 4, pool.n), (1, 0, 2 ** 31 - 1), (2, 0, -2 ** 31), (2, 7, -1)):
         table[s, j] = x
     check(pool, table, lens, 4, 128, topk, rng)
@@ -397,10 +408,11 @@ def test_decode_lengths_past_the_table():
     check(pool, table, [2 ** 31 - 1, 128], 2, 64, 2, rng)
 
 
-def test_decode_equal_scores_take_the_lower_block():
+@pytest.mark.parametrize("W", WIDTHS)
+def test_decode_equal_scores_take_the_lower_block(W):
     """Every block holds the same keys, so all scores are equal; values tell the blocks apart."""
     rng = np.random.default_rng(8)
-    pool, table = some_cache(rng, [700], 1, 64, 11)
+    pool, table = some_cache(rng, [700], 1, 64, W)
     for j in range(10):
         pool.k[table[0, j]] = pool.k[table[0, 0]]
         pool.k_scale[table[0, j]] = pool.k_scale[table[0, 0]]
@@ -409,20 +421,22 @@ def test_decode_equal_scores_take_the_lower_block():
         check(pool, table, [700], 4, 64, topk, rng, "top-%d" % topk)
 
 
-def test_decode_scores_that_are_no_numbers():
+@pytest.mark.parametrize("W", WIDTHS)
+def test_decode_scores_that_are_no_numbers(W):
     """A block whose key sum is NaN counts as the lowest."""
     rng = np.random.default_rng(9)
-    pool, table = some_cache(rng, [700], 1, 64, 11)
+    pool, table = some_cache(rng, [700], 1, 64, W)
     pool.k_sum[table[0, 3]] = np.nan
     pool.k_sum[table[0, 5], 0, 0] = np.inf
     q, cache, out, _ = check(pool, table, [700], 2, 64, 4, rng)
     assert bool(torch.isfinite(out.float()).all())
 
 
-def test_decode_scales_far_apart():
+@pytest.mark.parametrize("W", WIDTHS)
+def test_decode_scales_far_apart(W):
     """Pages whose scales differ by 2^40, and very large logits."""
     rng = np.random.default_rng(10)
-    pool, table = some_cache(rng, [500, 100], 2, 64, 9)
+    pool, table = some_cache(rng, [500, 100], 2, 64, W)
     pool.v_scale[table[0, 2]] *= 2.0 ** 40
     pool.v_scale[table[0, 3]] *= 2.0 ** -40
     pool.k_scale[table[0, 4]] *= 2.0 ** 4
@@ -431,10 +445,11 @@ def test_decode_scales_far_apart():
     check(pool, table, [500, 100], 4, 0, 0, rng)
 
 
-def test_decode_one_key_far_above():
+@pytest.mark.parametrize("W", [32, 400])
+def test_decode_one_key_far_above(W):
     """A late key far above all others: the running maximum moves."""
     rng = np.random.default_rng(11)
-    pool, table = some_cache(rng, [2000], 1, 64, 33)
+    pool, table = some_cache(rng, [2000], 1, 64, W)
     q = rng.standard_normal((1, 4, ref.D))
     for at, size in ((100, 2.0), (900, 4.0), (1999, 6.0)):
         k = (q[0, at % 4] * size)[None, None]
@@ -445,24 +460,25 @@ def test_decode_one_key_far_above():
     ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("W", WIDTHS)
 @pytest.mark.parametrize("topk", [0, 3])
-def test_decode_layouts(topk):
+def test_decode_layouts(topk, W):
     """Strided q, out in q's own memory, rows of a wider table, a used workspace, twice."""
     rng = np.random.default_rng(12)
     lens = [300, 0, 129, 700]
-    pool, table = some_cache(rng, lens, 2, 64, 12)
+    pool, table = some_cache(rng, lens, 2, 64, W)
     cache = to_gpu(pool)
     big = torch.randn((4, 12, 128), device=DEV).to(torch.bfloat16)
     q = big[:, 2:10]
     keep = big.clone()
-    wide = i32(np.full((4, 20), 2 ** 30))
-    wide[:, 3:15] = i32(table)
-    n = binding.cache_decode_workspace_bytes(4, 12, 8, 2, 64, 64, topk)
+    wide = i32(np.full((4, W + 8), 2 ** 30))
+    wide[:, 3:3 + W] = i32(table)
+    n = binding.cache_decode_workspace_bytes(4, W, 8, 2, 64, 64, topk)
     ws = torch.full((n + 64,), 0xff, dtype=torch.uint8, device=DEV)
     lse = torch.empty((8, 4), device=DEV)
     want = ref.decode(q.double().cpu().numpy(), pool, table, lens, 64, topk)
-    a, la = binding.cache_decode(q, cache, wide[:, 3:15], i32(lens), 64, topk)
-    binding.cache_decode(q, cache, wide[:, 3:15], i32(lens), 64, topk, out=q, lse=lse, workspace=ws[:n])
+    a, la = binding.cache_decode(q, cache, wide[:, 3:3 + W], i32(lens), 64, topk)
+    binding.cache_decode(q, cache, wide[:, 3:3 + W], i32(lens), 64, topk, out=q, lse=lse, workspace=ws[:n])
     torch.cuda.synchronize()
     assert torch.equal(a, q) and torch.equal(la, lse)
     ref.check_decode(q.double().cpu().numpy(), lse.double().cpu().numpy(), want)
@@ -520,12 +536,13 @@ def test_agrees_with_decode_over_a_packed_cache():
         assert float((la - lb).abs().max()) <= 1e-4
 
 
-def test_serving_steps_captured():
+@pytest.mark.parametrize("W", [5, 200])
+def test_serving_steps_captured(W):
     """Plan, write and decode as one captured step, replayed while requests grow, end, enter
     and are refused; eager work and synchronizations between the replays.  Each replay is
     compared with the definitions."""
     rng = np.random.default_rng(15)
-    S, hq, hkv, page, W, N, T = 6, 8, 2, 64, 5, 14, 160
+    S, hq, hkv, page, N, T = 6, 8, 2, 64, 14, 160
     pool = ref.Pool(N, hkv, page)
     cache = to_gpu(pool)
     w_table, w_free, w_lens, n = np.full((S, W), -1), rng.permutation(N), np.zeros(S, int), N
