@@ -377,8 +377,9 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  *   scores: lower block) and the current block are attended.  A topk of at least
  *   ceil(W * page_size / block_size) attends everything and runs as topk == 0.  At most
  *   4096 blocks per table row.
- * S * W pages of page_size / 64 tiles, times Hkv, must be below 2^31.
- * out [S, Hq, 128] bf16 (may be q's own memory, with q's strides), lse [Hq, S] f32.
+ * S * W pages of page_size / 64 tiles, times Hkv, must be below 2^31, S * Hkv below 2^23.
+ * out [S, Hq, 128] bf16 (may be q itself, with its strides; another view of q's memory is
+ * MOBA_ERR_LAYOUT), lse [Hq, S] f32.
  * A request with lens[s] <= 0 (an empty place of the batch) gets out 0 and lse -inf;
  * lens[s] above W * page_size counts as W * page_size.  The tokens of a table entry outside [0, N)
  * are left out as if masked (their page's k_sum counts as 0).  Hq / Hkv must not exceed 16.

@@ -362,6 +362,9 @@ def _cache_call(fn: str, t: torch.Tensor, stream, *args):
     if stream is not None:
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
+        if stream.device_index != device:
+            raise ValueError("the stream is on GPU %d, the tensors on GPU %d"
+                             % (stream.device_index, device))
         with torch.cuda.stream(stream):
             return f(*args, stream.cuda_stream)
     if device == torch.cuda.current_device():

@@ -107,6 +107,18 @@ inline moba_status check_contig(const moba_tensor* t, int dtype, int ndim, const
   return MOBA_OK;
 }
 
+// Whether two [T, H, D] views of elements of `el` bytes may share memory.  Views of
+// one wider buffer (equal token strides) share none if their heads lie apart in it.
+inline bool share_memory(const View& a, const View& b, int64_t T, int64_t el) {
+  const int64_t wa = (a.H - 1) * a.sh + kHeadDim, wb = (b.H - 1) * b.sh + kHeadDim;
+  const int64_t ia = (int64_t)(reinterpret_cast<uintptr_t>(a.data) / el);
+  const int64_t ib = (int64_t)(reinterpret_cast<uintptr_t>(b.data) / el);
+  if (ia + (T - 1) * a.st + wa <= ib || ib + (T - 1) * b.st + wb <= ia) return false;
+  if (a.st != b.st || wa > a.st || wb > a.st) return true;
+  const int64_t d = ((ib - ia) % a.st + a.st) % a.st;  // b's heads from a's, within a token
+  return d < wa || a.st - d < wb;
+}
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace moba

@@ -130,8 +130,8 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   if (topk > 0 && (block_size < 1 || block_size % P != 0)) return MOBA_ERR_BLOCK_SIZE;
   if (Hq >= (int64_t(1) << 20) || W >= (int64_t(1) << 31) || S >= (int64_t(1) << 31) ||
       S * W >= (int64_t(1) << 31) || S * Hq >= (int64_t(1) << 31) ||
-      S * W * (P / kCacheTile) >= (int64_t(1) << 31) / Hkv)
-    return MOBA_ERR_UNSUPPORTED;
+      S * W * (P / kCacheTile) >= (int64_t(1) << 31) / Hkv || S * Hkv >= (int64_t(1) << 23))
+    return MOBA_ERR_UNSUPPORTED;  // (the last: a launch's 2^32 work items)
   d->S = S;
   d->W = W;
   d->Hq = (int)Hq;
@@ -257,6 +257,10 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
   if ((st = check_3d(out, MOBA_BF16, &vo)) != MOBA_OK) return st;
   const int64_t S = q->shape[0], Hq = q->shape[1];
   if (out->shape[0] != S || out->shape[1] != Hq || Hq % a.c.Hkv != 0) return MOBA_ERR_SHAPE;
+  // out may be q (a row of q is read before its result is written), not another view of its memory
+  if (S > 0 && share_memory(vq, vo, S, 2) &&
+      !(vq.data == vo.data && vq.sh == vo.sh && (S == 1 || vq.st == vo.st)))
+    return MOBA_ERR_LAYOUT;
   const int64_t lshape[2] = {Hq, S};
   if ((st = check_contig(lse, MOBA_F32, 2, lshape)) != MOBA_OK) return st;
   if ((st = check_table(table, S)) != MOBA_OK) return st;

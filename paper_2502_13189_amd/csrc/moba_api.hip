@@ -43,18 +43,6 @@ size_t workspace_limit() {
   return (end && *end == 0) ? (size_t)v : kDefaultWorkspaceLimit;
 }
 
-// Whether two [T, H, D] views of elements of `el` bytes may share memory.  Views of
-// one wider buffer (equal token strides) share none if their heads lie apart in it.
-bool share_memory(const View& a, const View& b, int64_t T, int64_t el) {
-  const int64_t wa = (a.H - 1) * a.sh + kHeadDim, wb = (b.H - 1) * b.sh + kHeadDim;
-  const int64_t ia = (int64_t)(reinterpret_cast<uintptr_t>(a.data) / el);
-  const int64_t ib = (int64_t)(reinterpret_cast<uintptr_t>(b.data) / el);
-  if (ia + (T - 1) * a.st + wa <= ib || ib + (T - 1) * b.st + wb <= ia) return false;
-  if (a.st != b.st || wa > a.st || wb > a.st) return true;
-  const int64_t d = ((ib - ia) % a.st + a.st) % a.st;  // b's heads from a's, within a token
-  return d < wa || a.st - d < wb;
-}
-
 // Descriptor-level checks of cu_seqlens (no data access).
 moba_status check_cu_desc(const moba_tensor* cu) {
   if (!cu || !cu->data) return MOBA_ERR_NULL;

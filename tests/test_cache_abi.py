@@ -56,7 +56,7 @@ class Write:
 class Decode:
     def __init__(self, S=3, W=40, Hq=8, H=2, P=128, block=256, topk=3):
         self.t = dict(q=desc([S, Hq, 128]), table=desc([S, W], I32), lens=desc([S], I32),
-                      out=desc([S, Hq, 128]), lse=desc([Hq, S], F32))
+                      out=desc([S, Hq, 128], data=1 << 44), lse=desc([Hq, S], F32))
         self.c = Cache(H=H, P=P)
         self.block, self.topk, self.ws, self.bytes = block, topk, FAKE, 1 << 40
 
@@ -173,6 +173,15 @@ def test_layouts(lib):
     d = Decode()
     d.ws = FAKE + 8
     assert d.call(lib) == "MOBA_ERR_LAYOUT"
+    for off in (256, 8 * 256, -256):  # out over q, shifted by a head, a row, or back
+        d = Decode()
+        d.t["q"].data, d.t["out"].data = FAKE * 16, FAKE * 16 + off
+        assert d.call(lib) == "MOBA_ERR_LAYOUT"
+    d = Decode()  # heads of one wider buffer that do not overlap; the workspace is looked at next
+    for n, off in (("q", 0), ("out", 8 * 256)):
+        d.t[n].data, d.t[n].stride[0] = FAKE * 16 + off, 16 * 128
+    d.bytes = 0
+    assert d.call(lib) == "MOBA_ERR_NO_MEMORY"
 
 
 def test_sizes(lib):
@@ -197,6 +206,8 @@ def test_sizes(lib):
     for block in (0, -128, 64, 129, 192):  # no multiple of the page
         assert Decode(block=block).call(lib) == "MOBA_ERR_BLOCK_SIZE"
     assert Decode(W=4097, block=128).call(lib) == "MOBA_ERR_UNSUPPORTED"  # blocks per row
+    assert Decode(S=1 << 22, W=1).call(lib) == "MOBA_ERR_UNSUPPORTED"  # rows
+    assert Decode(S=1 << 16, W=1 << 14, topk=0).call(lib) == "MOBA_ERR_UNSUPPORTED"  # steps
     d = Decode()
     d.bytes = binding.cache_decode_workspace_bytes(3, 40, 8, 2, 128, 256, 3) - 1
     assert d.call(lib) == "MOBA_ERR_NO_MEMORY"
