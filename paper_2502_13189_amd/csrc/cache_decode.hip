@@ -692,10 +692,8 @@ __global__ __launch_bounds__(256) void cache_select_kernel(CacheDecodeArgs a) {
 // -------------------------------------------------------------------- rows
 // Short rows, a work-group for each (request, kv-head): gate, selection, attention and the
 // join of its waves in one launch.  A CU alone takes about 0.3 us per step (52 GB/s) with 4, 8
-// or 16 waves.
-constexpr int kRowWaves = 8;
-
-template <bool MOBA>
+// or 16 waves (kRowWaves).
+template <bool MOBA, int kRowWaves>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDecodeArgs a) {
   constexpr int kBlocks = kCacheRowBlocks;
   static_assert(kBlocks % 64 == 0 && kDecodeMaxGroup * kBlocks * 8 <= 4 * 8 * 64 * 16,
@@ -792,8 +790,15 @@ hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st) {
 
 hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st) {
   const unsigned groups = (unsigned)(a.S * a.c.Hkv);
-  if (full) cache_rows_kernel<false><<<groups, 64 * kRowWaves, 0, st>>>(a);
-  else cache_rows_kernel<true><<<groups, 64 * kRowWaves, 0, st>>>(a);
+  // Eight waves finish a row sooner (its gate and selection above all); where there are rows
+  // for four work-groups of four waves on every CU, the shorter ones run on past the longer:
+  // 6144 rows of 16 .. 512 tokens 70 -> 49 us, 2048 rows of 16 .. 1024 37 -> 31, MoBA 16 .. 4096 84
+  // -> 80; all rows equal, or up to 4096 tokens with full attention: 2% slower.
+  const bool four = groups >= 512 && (!full || a.W * a.c.P <= 2048);
+  if (full && four) cache_rows_kernel<false, 4><<<groups, 64 * 4, 0, st>>>(a);
+  else if (full) cache_rows_kernel<false, 8><<<groups, 64 * 8, 0, st>>>(a);
+  else if (four) cache_rows_kernel<true, 4><<<groups, 64 * 4, 0, st>>>(a);
+  else cache_rows_kernel<true, 8><<<groups, 64 * 8, 0, st>>>(a);
   return hipGetLastError();
 }
 

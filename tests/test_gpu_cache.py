@@ -380,6 +380,7 @@ def test_decode_moba(page, block, topk, hq, hkv, W):
     ([300] * 150 + [8000], 4, 4, 64, 512, 3),  # many rows: a work-group each, one of them long
     ([64 * 126, 5, 7000], 16, 1, 64, 64, 5),   # the most blocks a work-group gates
     ([1000, 77, 2048] * 20, 6, 2, 128, 0, 0),
+    ([150, 3, 700] * 60, 4, 4, 64, 0, 0),
 ])
 def test_decode_splits(lens, hq, hkv, page, block, topk):
     rng = np.random.default_rng(len(lens) + hq)
