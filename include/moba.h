@@ -84,12 +84,14 @@ typedef enum {
   MOBA_ERR_DTYPE = 2,       /* dtype mismatch or unsupported dtype */
   MOBA_ERR_SHAPE = 3,       /* shapes disagree with each other or with cu_seqlens */
   MOBA_ERR_LAYOUT = 4,      /* last dim not contiguous, or a contiguous tensor required */
-  MOBA_ERR_BLOCK_SIZE = 5,  /* block_size < 1 */
+  MOBA_ERR_BLOCK_SIZE = 5,  /* block_size < 1, or (paged cache) no multiple of the page size */
   MOBA_ERR_TOPK = 6,        /* topk < 1 */
   MOBA_ERR_SEQLENS = 7,     /* cu[0] != 0, decreasing, or cu[S] != T */
   MOBA_ERR_UNSUPPORTED = 8, /* D != 128, Hq/Hkv > 128, > 4096 blocks per sequence,
-                               1 < topk-1 < #blocks with topk > 64, or index overflow */
-  MOBA_ERR_NO_MEMORY = 9,   /* workspace over MOBA_WORKSPACE_LIMIT_BYTES or hipMalloc failed */
+                               1 < topk-1 < #blocks with topk > 64, a page size the paged
+                               cache does not have, or index overflow */
+  MOBA_ERR_NO_MEMORY = 9,   /* workspace over MOBA_WORKSPACE_LIMIT_BYTES, hipMalloc failed, or
+                               a workspace passed in is too small */
   MOBA_ERR_HIP = 10         /* a HIP call or kernel launch failed */
 } moba_status;
 
@@ -377,7 +379,7 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  *   scores: lower block) and the current block are attended.  A topk of at least
  *   ceil(W * page_size / block_size) attends everything and runs as topk == 0.  At most
  *   4096 blocks per table row.
- * S * W pages of page_size / 64 tiles, times Hkv, must be below 2^31, S * Hkv below 2^23.
+ * S * W pages of page_size / 64 tiles, times Hkv, must be below 2^30, S * Hkv below 2^23.
  * out [S, Hq, 128] bf16 (may be q itself, with its strides; another view of q's memory is
  * MOBA_ERR_LAYOUT), lse [Hq, S] f32.
  * A request with lens[s] <= 0 (an empty place of the batch) gets out 0 and lse -inf;

@@ -130,7 +130,7 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   if (topk > 0 && (block_size < 1 || block_size % P != 0)) return MOBA_ERR_BLOCK_SIZE;
   if (Hq >= (int64_t(1) << 20) || W >= (int64_t(1) << 31) || S >= (int64_t(1) << 31) ||
       S * W >= (int64_t(1) << 31) || S * Hq >= (int64_t(1) << 31) ||
-      S * W * (P / kCacheTile) >= (int64_t(1) << 31) / Hkv || S * Hkv >= (int64_t(1) << 23))
+      S * W * (P / kCacheTile) >= (int64_t(1) << 30) / Hkv || S * Hkv >= (int64_t(1) << 23))
     return MOBA_ERR_UNSUPPORTED;  // (the last: a launch's 2^32 work items)
   d->S = S;
   d->W = W;

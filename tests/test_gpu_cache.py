@@ -607,3 +607,98 @@ def test_decode_on_two_streams():
     torch.cuda.synchronize()
     for i, (o, l) in enumerate(got):
         assert torch.equal(o, want[i % 2][0]) and torch.equal(l, want[i % 2][1])
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured decodes of different shapes with one workspace between them, replayed in
+    turn (one stream): each finds nothing of the other's."""
+    rng = np.random.default_rng(17)
+    batches = []
+    for lens, hq, hkv, topk in (([9000, 70, 300], 4, 1, 0), ([5000, 6100], 8, 2, 3)):
+        pool, table = some_cache(rng, lens, hkv, 64, 300)
+        q = torch.randn((len(lens), hq, 128), device=DEV).to(torch.bfloat16)
+        n = binding.cache_decode_workspace_bytes(len(lens), 300, hq, hkv, 64, 64, topk)
+        batches.append([q, to_gpu(pool), i32(table), i32(lens), 64, topk, n])
+    ws = torch.full((max(b[-1] for b in batches),), 0xff, dtype=torch.uint8, device=DEV)
+    want = [binding.cache_decode(*b[:-1]) for b in batches]
+    torch.cuda.synchronize()
+    graphs = []
+    for b in batches:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = binding.cache_decode(*b[:-1], workspace=ws)
+        graphs.append((g, got))
+    for i in (0, 1, 1, 0, 1, 0, 0):
+        g, got = graphs[i]
+        got[0].zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[i][0]) and torch.equal(got[1], want[i][1])
+
+
+def test_steps_on_a_stream_of_their_own():
+    """Every call on a side stream passed in, outputs passed in and left out."""
+    rng = np.random.default_rng(18)
+    lens = [100, 64, 0, 17]
+    T = sum(lens) + 5
+    st = torch.cuda.Stream()
+    k, v = (torch.randn((T, 2, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((4, 4, 128), device=DEV).to(torch.bfloat16)
+    cache = binding.cache_new(9, 2, 64, device=DEV)
+    table, free = i32(np.full((4, 3), -1)), i32(rng.permutation(9))
+    add, zero, nf = i32(lens), i32([0] * 4), i32([9])
+    slots = torch.empty((T,), dtype=torch.int64, device=DEV)
+    torch.cuda.synchronize()
+    p = binding.cache_plan(add, zero, table, free, nf, 64, T, slots=slots, stream=st)
+    binding.cache_write(k, v, p.slots, cache, stream=st.cuda_stream)
+    out, lse = binding.cache_decode(q, cache, table, p.lens, 64, 2, stream=st)
+    st.synchronize()
+    assert p.slots is slots
+    pool = ref.Pool(9, 2, 64)
+    w_table, w_free = np.full((4, 3), -1), free.cpu().numpy().copy()
+    w_slots = ref.plan(lens, [0] * 4, w_table, w_free, 9, 64, T)[1]
+    np.testing.assert_array_equal(slots.cpu(), w_slots)
+    ref.write(k.double().cpu().numpy(), v.double().cpu().numpy(), w_slots, pool)
+    want = ref.decode(q.double().cpu().numpy(), pool, w_table, lens, 64, 2)
+    ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
+
+
+def test_refusals_leave_everything():
+    """What the library or the binding refuses touches nothing."""
+    rng = np.random.default_rng(19)
+    pool, table = some_cache(rng, [100, 30], 2, 64, 4)
+    cache, t, ln = to_gpu(pool), i32(table), i32([100, 30])
+    q = torch.randn((2, 4, 128), device=DEV).to(torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+
+    def refused(name, f, *args, **kw):
+        with pytest.raises(binding.MobaError) as e:
+            f(*args, **kw)
+        assert e.value.name == name
+
+    refused("MOBA_ERR_DTYPE", binding.cache_decode, q.float(), cache, t, ln, 64, 0)
+    refused("MOBA_ERR_BLOCK_SIZE", binding.cache_decode, q, cache, t, ln, 96, 2, out=out)
+    refused("MOBA_ERR_TOPK", binding.cache_decode, q, cache, t, ln, 64, -1, out=out)
+    refused("MOBA_ERR_SHAPE", binding.cache_decode, q, cache, t[:1], ln, 64, 2, out=out)
+    refused("MOBA_ERR_NO_MEMORY", binding.cache_decode, q, cache, t, ln, 64, 2, out=out,
+            workspace=torch.empty((15,), dtype=torch.uint8, device=DEV))
+    refused("MOBA_ERR_LAYOUT", binding.cache_decode, q, cache, t, ln, 64, 2,
+            out=q.new_empty((2, 4, 256))[..., ::2])
+    x = torch.zeros((3, 2, 128), dtype=torch.bfloat16, device=DEV)
+    slots = torch.tensor([0, 1, 2], device=DEV)
+    refused("MOBA_ERR_DTYPE", binding.cache_write, x, x.float(), slots, cache)
+    refused("MOBA_ERR_DTYPE", binding.cache_write, x, x, slots.int(), cache)
+    refused("MOBA_ERR_SHAPE", binding.cache_write, x[:, :1], x[:, :1], slots, cache)
+    refused("MOBA_ERR_UNSUPPORTED", binding.cache_plan, ln, ln, t, ln, ln[:1], 96, 4)
+    for f, args in ((binding.cache_decode, (q, cache, t.cpu(), ln, 64, 0)),
+                    (binding.cache_write, (x, x.cpu(), slots, cache)),
+                    (binding.cache_plan, (ln, ln, t, ln.cpu(), ln[:1], 64, 4))):
+        with pytest.raises(ValueError):
+            f(*args)
+    with pytest.raises(TypeError):
+        binding.cache_write(x.half(), x.half(), slots, cache)
+    with pytest.raises(TypeError):
+        binding.cache_decode(q, cache[:4], t, ln, 64, 0)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+    same_pools(to_host(cache, pool), pool)
