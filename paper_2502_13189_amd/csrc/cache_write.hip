@@ -13,9 +13,14 @@
 // registers (4 tokens x 4 dims of codes) and LDS and leaves in rows of 64 tokens.  The
 // maximum is that of the bit patterns and the rounding the hardware's scaled conversion; the
 // maximum tells where a run has an infinity, a NaN or a value past the largest scale, and
-// such a run is read again and rounded value by value.  117017 tokens of ragged prompts, 8
-// kv-heads, bf16, pages of 128 (724 MB): 156 us, 4.6 TB/s, the rate of a large copy; with the
-// elements held, measured and rounded as floats, one by one, 347 us.
+// such a run is read again and rounded value by value.  A run of one token, a request's in a
+// decode step, is one wave's, several in a work-group side by side.
+//
+// Measured: 117017 tokens of ragged prompts, 8 kv-heads, bf16, pages of 128 (724 MB): 150
+// us, 4.8 TB/s, the rate of a large copy (with the elements held, measured and rounded as
+// floats, one by one, 347).  One token for each of 62 requests: 6 us; of 1024: 28 (as whole
+// work-groups' runs 40), with pages of 256 28 too (196).  A wave per tile, V turned over in
+// registers alone, was slower but for pages of 256.
 #include "cache_internal.h"
 
 #include <math.h>
@@ -147,6 +152,12 @@ __device__ __forceinline__ uint32_t odd_codes(const Eight<T>& x, int i, float in
   return pack_f8(y[0], y[1], y[2], y[3]);
 }
 
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float by) {
+  float f[4];
+  unpack_f8(w, f);
+  return pack_f8(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
+}
+
 // Four words of four bytes, turned over.
 __device__ __forceinline__ void turn(const uint32_t* c, uint32_t* r) {
   const uint32_t t0 = __builtin_amdgcn_perm(c[1], c[0], 0x05010400u);
@@ -159,11 +170,134 @@ __device__ __forceinline__ void turn(const uint32_t* c, uint32_t* r) {
   r[3] = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
 }
 
-// One work-group per window of `window` tokens (at most a page's) and kv-head: the runs
-// that begin in it, one after the other.  TILES: the page's 64-token tiles.
+// A run of one token (a request's in a decode step), by one wave: lanes 0 .. 7 have its key's
+// 16 dims each, lanes 8 .. 15 its value's; eight lanes each read an older key for the sum.
 template <typename T, int TILES>
-__global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) == 2 ? 6 : 4) void cache_write_kernel(
-    CacheWriteArgs a, int window, uint32_t first) {
+__device__ __forceinline__ void write_single(const CacheWriteArgs& a, int64_t t, int64_t slot, int h) {
+  const CachePool& c = a.c;
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // (opaque, as in the kernel below)
+  const uint32_t page = (uint32_t)(slot >> 6) / TILES;
+  const int o = (int)(slot - (int64_t)page * (TILES * kCacheTile));
+  const int64_t ph = (int64_t)page * c.Hkv + h;
+  uint8_t* kp = c.k + page * c.k_sp + h * c.k_sh;
+  uint8_t* vp = c.v + page * c.v_sp + h * c.v_sh;
+  const int d16 = 16 * (lane & 7), row = lane >> 3;
+  const bool value = lane & 8;  // (for lanes below 16)
+  Eight<T> x[2];
+  x[0].clear();
+  x[1].clear();
+  if (lane < 16) {
+    const T* at = value ? static_cast<const T*>(a.v) + t * a.v_st + h * a.v_sh
+                        : static_cast<const T*>(a.k) + t * a.k_st + h * a.k_sh;
+    x[0].load(at + d16);
+    x[1].load(at + d16 + 8);
+  }
+  const float ks0 = o > 0 ? c.k_scale[ph] : 0.0f, vs0 = o > 0 ? c.v_scale[ph] : 0.0f;
+  // older keys, eight rows a load, half a tile in flight
+  uint4 old[4];
+  const auto older = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int p = p0 + 8 * i + row;
+      old[i] = make_uint4(0, 0, 0, 0);
+      if (p < o) old[i] = *reinterpret_cast<const uint4*>(kp + p * kHeadDim + d16);
+    }
+  };
+  older(0);
+  uint32_t m = fine_top(x[1], fine_top(x[0], 0));
+#pragma unroll
+  for (int i = 1; i < 8; i *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, i, 64));
+  const uint32_t km = __builtin_amdgcn_readlane(m, 0), vm = __builtin_amdgcn_readlane(m, 8);
+  const int ke = max(o > 0 ? held_exp(ks0) : kCacheMinExp, scale_exp(km));
+  const int ve = max(o > 0 ? held_exp(vs0) : kCacheMinExp, scale_exp(vm));
+  const bool kold = o > 0 && ks0 != exp2_int(ke), vold = o > 0 && vs0 != exp2_int(ve);
+  const float kre = ks0 * exp2_int(-ke), vre = vs0 * exp2_int(-ve);
+  const float inv = exp2_int(value ? -ve : -ke);
+  const uint32_t code[4] = {odd_codes(x[0], 0, inv), odd_codes(x[0], 1, inv), odd_codes(x[1], 0, inv),
+                            odd_codes(x[1], 1, inv)};
+  // Sums of codes, multiples of 2^-9: exact in fp32 over up to 64 tokens, and a lane has at
+  // most 33; over the lanes as integers.  NaN where one is NaN.
+  static_assert(kCacheMaxPage / 8 + 1 <= 64, "a lane's sums are exact");
+  float f[16];
+#pragma unroll
+  for (int d = 0; d < 16; d++) f[d] = 0.0f;
+  const auto add = [&](uint32_t w, int e) {
+    float g[4];
+    unpack_f8(w, g);
+#pragma unroll
+    for (int d = 0; d < 4; d++) f[4 * e + d] += g[d];
+  };
+#pragma unroll 1
+  for (int p0 = 0; p0 < o; p0 += kCacheTile / 2) {
+    if (p0 > 0) older(p0);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int p = p0 + 8 * i + row;
+      uint32_t w[4] = {old[i].x, old[i].y, old[i].z, old[i].w};
+      if (kold) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) w[e] = rescaled(w[e], kre);
+        if (p < o) *reinterpret_cast<uint4*>(kp + p * kHeadDim + d16) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e++) add(w[e], e);
+      __builtin_amdgcn_sched_barrier(0);  // (rows side by side would need all registers)
+    }
+  }
+  if (lane < 8) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) add(code[e], e);
+    *reinterpret_cast<uint4*>(kp + o * kHeadDim + d16) = make_uint4(code[0], code[1], code[2], code[3]);
+  }
+#pragma unroll
+  for (int d = 0; d < 16; d++) {
+    int sum = f[d] == f[d] ? (int)(f[d] * 512.0f) : 1 << 27;  // (a page's sums stay within 2^26)
+#pragma unroll
+    for (int i = 8; i < 64; i *= 2) sum += __shfl_xor(sum, i, 64);
+    f[d] = sum > 1 << 26 ? NAN : (float)sum * exp2_int(ke - 9);
+  }
+  if (lane < 8) {
+    float4* out = reinterpret_cast<float4*>(c.k_sum + ph * kHeadDim + d16);
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
+  }
+  if (vold) {  // the older values, 16 tokens of a dim at a time
+#pragma unroll 1
+    for (int i = lane; i < (o + kCacheTile - 1) / kCacheTile * (kHeadDim * 4); i += 64) {
+      const int p = i / (kHeadDim * 4) * kCacheTile + 16 * (i & 3);  // place of its first token
+      uint4* at = reinterpret_cast<uint4*>(vp + 16 * i);
+      const uint4 was = *at;
+      uint32_t w[4] = {was.x, was.y, was.z, was.w};
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int n = o - p - 4 * e;  // older tokens from this word on
+        const uint32_t keep = n >= 4 ? 0u : n <= 0 ? ~0u : ~0u << (8 * n);
+        w[e] = (w[e] & keep) | (rescaled(w[e], vre) & ~keep);
+      }
+      *at = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __threadfence_block();  // (the new value's bytes, written next, lie in the same words)
+  }
+  if (lane >= 8 && lane < 16) {
+    uint8_t* at = vp + (o / kCacheTile) * (kCacheTile * kHeadDim) + d16 * kCacheTile + o % kCacheTile;
+#pragma unroll
+    for (int d = 0; d < 16; d++) at[d * kCacheTile] = (uint8_t)(code[d / 4] >> (8 * (d & 3)));
+  }
+  if (lane == 0) {
+    c.k_scale[ph] = exp2_int(ke);
+    c.v_scale[ph] = exp2_int(ve);
+  }
+}
+
+// One work-group per window of `window` tokens (at most a page's) and kv-head: the runs
+// that begin in it, with SINGLES those of one token a wave each first, then one after the
+// other.  TILES: the page's 64-token tiles.
+// (Waves per SIMD: where the next more would spill much; three tiles need six for two
+// work-groups.)
+template <typename T, int TILES, bool SINGLES>
+__global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) != 2 ? 4 : SINGLES && TILES != 3 ? 5 : 6) void
+cache_write_kernel(CacheWriteArgs a, int window, uint32_t first) {
   constexpr int P = TILES * kCacheTile;
   __shared__ uint32_t vt[TILES][kHeadDim * kVRow];
   __shared__ int ksum[kHeadDim];
@@ -196,9 +330,24 @@ __global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) == 2 ? 6 : 4) void c
     }
   }
   __syncthreads();
-  unsigned long long left = begins[0];
+  // rows that begin a run and that none follows
+  const auto singles = [&](int word) {
+    return SINGLES ? begins[word] & ~(follows[word] >> 1 | follows[word + 1] << 63) : 0;
+  };
+  if constexpr (SINGLES) {
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int nth = 0;
+    for (int word = 0; word < TILES; word++) {
+      for (unsigned long long w = singles(word); w; w &= w - 1, nth++) {
+        if (nth % (kTileThreads / 64 * TILES) != wave) continue;
+        const int i = 64 * word + __ffsll((long long)w) - 1;
+        write_single<T, TILES>(a, w0 + i, slot_at[i], h);
+      }
+    }
+  }
+  unsigned long long left = begins[0] & ~singles(0);
   for (int word = 0;;) {
-    while (left == 0 && ++word < TILES) left = begins[word];
+    while (left == 0 && ++word < TILES) left = begins[word] & ~singles(word);
     if (left == 0) break;
     // (opaque, so that what follows from it is computed here: kept across the loop it takes
     // half of the registers)
@@ -316,10 +465,8 @@ __global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) == 2 ? 6 : 4) void c
       const int r = p0 + i - o;
       float f[8];
       if (r < 0 && kold) {
-        unpack_f8(kc[i].x, f);
-        unpack_f8(kc[i].y, f + 4);
-        kc[i].x = pack_f8(f[0] * kre, f[1] * kre, f[2] * kre, f[3] * kre);
-        kc[i].y = pack_f8(f[4] * kre, f[5] * kre, f[6] * kre, f[7] * kre);
+        kc[i].x = rescaled(kc[i].x, kre);
+        kc[i].y = rescaled(kc[i].y, kre);
       }
       if (r < n && (r >= 0 || kold))
         *reinterpret_cast<uint2*>(kp + (p0 + i) * kHeadDim + c8) = kc[i];
@@ -351,10 +498,9 @@ __global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) == 2 ? 6 : 4) void c
       const uint32_t keep = o - p0 >= 4 ? 0u : 0xffffffffu << (8 * (o - p0));  // new tokens' bytes
 #pragma unroll
       for (int d = 0; d < 8; d++) {
-        float f[4];
-        unpack_f8(*reinterpret_cast<const uint32_t*>(vp + tile * kCacheTile * kHeadDim +
-                                                     (c8 + d) * kCacheTile + x4), f);
-        vw[d] = (vw[d] & keep) | (pack_f8(f[0] * vre, f[1] * vre, f[2] * vre, f[3] * vre) & ~keep);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(vp + tile * kCacheTile * kHeadDim +
+                                                              (c8 + d) * kCacheTile + x4);
+        vw[d] = (vw[d] & keep) | (rescaled(w, vre) & ~keep);
       }
     }
 #pragma unroll
@@ -385,28 +531,37 @@ __global__ __launch_bounds__(kTileThreads* TILES, sizeof(T) == 2 ? 6 : 4) void c
   }
 }
 
-template <typename T>
-hipError_t launch(const CacheWriteArgs& a, int window, int64_t groups, hipStream_t st) {
-  const int tiles = a.c.P / kCacheTile, threads = kTileThreads * tiles;
+template <typename T, int TILES>
+hipError_t launch(const CacheWriteArgs& a, hipStream_t st) {
+  // A work-group takes the runs that begin in its window: of four tokens for each of the
+  // page's tiles (its waves) where every row may be a run of its own (a decode step), up to a
+  // page's where there are rows enough to fill the chip either way.  There the rows are
+  // prompts', and the kernel without the path of single tokens needs fewer registers:
+  // 117017 tokens of prompts take 149 us with it and 157 with the other.
+  constexpr int P = TILES * kCacheTile, threads = kTileThreads * TILES;
+  int window = 4 * TILES;
+  while (2 * window <= P && a.T * a.c.Hkv * TILES / (2 * window) >= 4096) window *= 2;
+  const int64_t groups = (a.T + window - 1) / window * a.c.Hkv;
   return launch_pieces(groups, threads, [&](uint32_t first, unsigned n) {
-    if (tiles == 1) cache_write_kernel<T, 1><<<n, threads, 0, st>>>(a, window, first);
-    else if (tiles == 2) cache_write_kernel<T, 2><<<n, threads, 0, st>>>(a, window, first);
-    else if (tiles == 3) cache_write_kernel<T, 3><<<n, threads, 0, st>>>(a, window, first);
-    else cache_write_kernel<T, 4><<<n, threads, 0, st>>>(a, window, first);
+    if (2 * window <= P) cache_write_kernel<T, TILES, true><<<n, threads, 0, st>>>(a, window, first);
+    else cache_write_kernel<T, TILES, false><<<n, threads, 0, st>>>(a, window, first);
   });
+}
+
+template <typename T>
+hipError_t launch(const CacheWriteArgs& a, hipStream_t st) {
+  const int tiles = a.c.P / kCacheTile;
+  return tiles == 1   ? launch<T, 1>(a, st)
+         : tiles == 2 ? launch<T, 2>(a, st)
+         : tiles == 3 ? launch<T, 3>(a, st)
+                      : launch<T, 4>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_cache_write(bool bf16, const CacheWriteArgs& a, hipStream_t st) {
   if (a.T <= 0) return hipSuccess;
-  // A work-group takes the runs that begin in its window one after the other: a window of
-  // one token where every row may be a run of its own (a decode step), up to a page's
-  // tokens where there are rows enough to fill the chip either way.
-  int window = 1;
-  while (2 * window <= a.c.P && a.T * a.c.Hkv / (2 * window) >= 4096) window *= 2;
-  const int64_t groups = (a.T + window - 1) / window * a.c.Hkv;
-  return bf16 ? launch<__hip_bfloat16>(a, window, groups, st) : launch<float>(a, window, groups, st);
+  return bf16 ? launch<__hip_bfloat16>(a, st) : launch<float>(a, st);
 }
 
 }  // namespace moba

@@ -235,6 +235,26 @@ def test_write_token_by_token():
         same_pools(to_host(cache, pool), pool)
 
 
+@pytest.mark.parametrize("page", [64, 128, 192, 256])
+def test_write_single_tokens(page):
+    """A decode step's tokens: one for each of many pages, at every kind of offset, with sizes
+    that make older tokens keep their scale or lose it; older and new keys with NaN; runs of
+    two and more, and rows that are left out, between them."""
+    rng = np.random.default_rng(page)
+    for spans, dtype in (([(int(o), 1) for o in rng.integers(0, page, 60)], torch.bfloat16),
+                         ([(o, 1) for o in (0, 1, 7, 8, 31, 32, 33, 62, 63, page - 1)], torch.float32),
+                         ([(int(o), int(min(n, page - o))) for o, n in zip(
+                             rng.integers(0, page, 90), rng.choice([1, 1, 1, 2, 5, 64], 90))], torch.bfloat16)):
+        pool = filled(ref.Pool(len(spans) + 2, 3, page), 5)
+        pool.k[3, :, 2, 5] = pool.k[7, 1, page - 1, 9] = 0x7f
+        slots = runs(pool, rng, spans)
+
+        def edit(k, v):
+            k *= torch.from_numpy(2.0 ** rng.integers(-8, 9, (len(k), 1, 1))).to(DEV, dtype)
+            k[1, 0, 3], v[2, 2, 100], v[4] = float("nan"), float("inf"), 0.0
+        check_write(pool, slots, dtype, page + 2, edit=edit)
+
+
 def test_write_extremes():
     """Zeros, subnormals, the type's largest values, infinities and NaN."""
     def edit(k, v):
@@ -282,6 +302,41 @@ def test_write_many_rows_in_no_order(dtype):
     slots = runs(pool, rng, [spans[i] for i in order])
     slots[0:0] = [700 * 64, 1 << 40, -(1 << 40)]  # (between runs: a page has one run per call)
     check_write(pool, slots, dtype, 11, strided=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("page", [64, 128, 192, 256])
+def test_write_windows_of_a_page(page, dtype):
+    """Rows and heads enough that a work-group takes a page's rows: whole pages, prompts cut
+    anywhere, single tokens.  A page's bits do not depend on what else a call writes, so they
+    are those of calls of a few hundred rows each, which the tests above hold to the definition."""
+    rng, hkv = np.random.default_rng(page), 16
+    spans = [(0, page)] * (13000 // page) + [(int(o), int(rng.integers(1, page + 1 - o)))
+                                             for o in rng.integers(0, page, 60)]
+    spans += [(int(o), 1) for o in rng.integers(0, page, 300)]
+    spans = [spans[i] for i in rng.permutation(len(spans))] + [(0, page)] * (4000 // page)
+    spans += [(int(o), 1) for o in rng.integers(0, page, 300)]
+    slots, cuts = [], [0]
+    for (o, n), p in zip(spans, rng.permutation(len(spans) + 1)):
+        slots += [int(p) * page + o + i for i in range(n)] + [-1] * int(rng.integers(0, 2))
+        if len(slots) - cuts[-1] > 500:
+            cuts.append(len(slots))
+    assert len(slots) * hkv / 64 >= 4096
+    gen = torch.Generator(device=DEV).manual_seed(page)
+    one = binding.cache_new(len(spans) + 1, hkv, page, device=DEV)
+    for x in one:  # (codes of any kind but NaN)
+        x.copy_(torch.randn(x.shape, generator=gen, device=DEV).to(x.dtype))
+    one.k_scale.copy_(2.0 ** torch.randint(-12, 1, one.k_scale.shape, generator=gen, device=DEV))
+    one.v_scale.copy_(2.0 ** torch.randint(-12, 1, one.k_scale.shape, generator=gen, device=DEV))
+    many = binding.PagedCache(*(x.clone() for x in one))
+    k, v = (torch.randn((len(slots), hkv, 128), generator=gen, device=DEV).to(dtype) for _ in range(2))
+    k[3, 10, 3], v[70, 15, 100], v[-2, 5, 5] = float("nan"), float("inf"), -float("inf")
+    slots = torch.tensor(slots, device=DEV)
+    binding.cache_write(k, v, slots, one)
+    for lo, hi in zip(cuts, cuts[1:] + [len(slots)]):
+        binding.cache_write(k[lo:hi], v[lo:hi], slots[lo:hi], many)
+    for x, y in zip(one, many):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
 def test_write_into_a_layer_of_a_larger_pool():
