@@ -389,7 +389,7 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  * initialisation and nothing is kept in it after the call.  fp32 softmax and sums; the keys, the
  * queries and the values enter the matrix cores exactly, the weights as two bf16 terms.
  * Results do not depend on timing; a request's split over work-groups, and with it its
- * rounding, depends on the lengths of the whole batch.
+ * rounding, depends on the whole batch.
  */
 moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
                               const moba_tensor* table, const moba_tensor* lens,

@@ -76,7 +76,8 @@ struct DecodeShape {
   int64_t S, W;
   int Hq, Hkv, P, B, topk;
   bool full, rows;          // rows: one launch, a work-group per (request, kv-head)
-  int nblk, nlist;          // MoBA
+  int nblk, parts;          // MoBA
+  int64_t most;             // 64-key steps of a row at most
   int shares, gate_shares;
 };
 
@@ -89,20 +90,17 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
     *p = reinterpret_cast<std::remove_reference_t<decltype(*p)>>(base + off);
     off += ((size_t)n * sizeof(**p) + 15) / 16 * 16;
   };
-  const int64_t G = d.Hq / d.Hkv, pg = d.full ? d.Hkv : 1;
-  take(&a->part_o, (int64_t)d.shares * 2 * pg * G * kHeadDim);
-  take(&a->part_ml, (int64_t)d.shares * 2 * pg * G);
-  take(&a->join, (int64_t)d.shares * pg);
-  if (!d.full) {
-    take(&a->score, d.topk > 1 ? d.S * d.Hq * d.nblk : 0);
-    take(&a->list, d.S * d.Hkv * d.nlist);
-    take(&a->nsteps, d.S * d.Hkv);
-  }
+  const int64_t G = d.Hq / d.Hkv;
+  const int64_t partials = d.full ? (int64_t)d.shares * 2 * d.Hkv : d.parts > 1 ? d.S * d.Hkv * d.parts : 0;
+  take(&a->part_o, partials * G * kHeadDim);
+  take(&a->part_ml, partials * G);
+  if (d.full) take(&a->join, (int64_t)d.shares * d.Hkv);
+  else take(&a->score, d.topk > 1 ? d.S * d.Hq * d.nblk : 0);
   return off;
 }
 
 // Whether a work-group takes each (request, kv-head) by itself.  It needs one launch instead
-// of two (MoBA: four) and no joins, but a row is then one CU's, about 0.3 us per 64-key
+// of two (MoBA: three) and no joins, but a row is then one CU's, about 0.3 us per 64-key
 // step, so a row's most (what its table row can hold, MoBA: select) is held against what
 // the other way takes: its launches, while there is little to do, and the batch's share
 // of the chip where there is much.  Whole calls, split and by rows, all rows full:
@@ -110,15 +108,25 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
 //         2048: 16 rows 13.3, 15.2; 128 rows 23.2, 16.4; 2048 rows 183, 182
 //         4096: 16 rows 13.6, 25.5; 512 rows 104, 93; 8192: 512 rows 193, 181 (but ragged
 //         118, 120)
-//   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 19.9, 18.0; 4096: 16 rows 23.5, 26.1; 64 rows
-//         29.4, 27.2; 8192: 64 rows 31.6, 33.2; 128 rows 39.9, 33.7; 2048 rows 363, 296
+//   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 16.0, 18.0 (ragged 12.2, 8.1), 64 rows 19.3,
+//         19.6; 4096: 128 rows 29.9, 28.7, 2048 rows 271, 253; 8192: 128 rows 33.6, 33.8 (ragged
+//         23.3, 27.3), 512 rows 94, 90
 bool rows_in_one(const DecodeShape& d) {
   const int64_t rows = d.S * d.Hkv, held = d.W * (d.P / kCacheTile);
   if (d.full) return held <= std::min<int64_t>(std::max<int64_t>(rows / 4, 16), 64);
   if (d.nblk > kCacheRowBlocks) return false;
   // (a page's k_sum is 1/32 of a step's bytes)
-  const int64_t most = std::min<int64_t>(held, (int64_t)d.nlist * (d.B / kCacheTile)) + d.W / 32;
-  return most <= std::min<int64_t>(std::max<int64_t>(rows / 2, 34), 256);
+  return d.most + d.W / 32 <= std::min<int64_t>(std::max<int64_t>(rows / 3, 34), 256);
+}
+
+// MoBA: work-groups for a (request, kv-head), whose waves have a step or more.  (256, 512, 768,
+// 1024 work-groups: 8 ragged requests 44.2, 44.1, 47.1, 49.3 us, 32 x 65536 tokens 180, 184, 187,
+// 187, ragged 91, 64, 70, 61.  At most 64, 256, 1024 steps: 64 ragged requests of up to 32768
+// tokens 77, 88, 89 us, all full 196, 189, 190.)
+int parts_of(int64_t rows, int64_t most) {
+  if (rows == 0 || rows >= int64_t(1) << 19) return 1;  // (as far as the grids go)
+  const int64_t n = std::max(ceil_div(kCachePartGroups, rows), ceil_div(most, kCachePartSteps));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({n, ceil_div(most, 4), kCacheWaves}));
 }
 
 // Checks the sizes and settles how the call runs.
@@ -143,12 +151,13 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t Hq, int64_t Hkv, int64_t 
   d->topk = d->full ? 0 : topk;
   if (!d->full && nblk > kMaxBlocksPerSeq) return MOBA_ERR_UNSUPPORTED;
   d->nblk = (int)nblk;
-  d->nlist = d->full ? 0 : (int)std::min<int64_t>(nblk, Hq / Hkv * (topk - 1) + 1);
+  d->most = W * (P / kCacheTile);
+  if (!d->full)  // (a kv-head's heads may choose different blocks)
+    d->most = std::min<int64_t>(d->most, std::min<int64_t>(nblk, Hq / Hkv * (topk - 1) + 1) * (block_size / kCacheTile));
   d->rows = rows_in_one(*d);
   const int64_t steps = S * W * (P / kCacheTile);  // at most, of a kv-head
-  const int64_t each = std::max<int64_t>(1, kCacheWaves / Hkv);
-  d->shares = (int)(d->full ? std::min<int64_t>(each, std::max<int64_t>(steps, 1))
-                            : std::min<int64_t>(kCacheWaves, std::max<int64_t>(steps * Hkv, 1)));
+  d->shares = (int)std::min<int64_t>(std::max<int64_t>(1, kCacheWaves / Hkv), std::max<int64_t>(steps, 1));
+  d->parts = d->full ? 0 : parts_of(S * Hkv, d->most);
   d->gate_shares = (int)std::min<int64_t>(std::max<int64_t>(1, kCacheGateWaves / Hkv),
                                           std::max<int64_t>(S * nblk, 1));
   return MOBA_OK;
@@ -286,7 +295,7 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
   a.B = d.B;
   a.topk = d.topk;
   a.nblk = d.nblk;
-  a.nlist = d.nlist;
+  a.parts = d.parts;
   a.shares = d.shares;
   a.gate_shares = d.gate_shares;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)kHeadDim));
@@ -295,18 +304,19 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
     MOBA_LAUNCH(launch_cache_rows(d.full, a, stream));
     return MOBA_OK;
   }
-  if (!d.full) {
-    if (d.topk > 1) {
-      Phase ph("cache_gate", stream);
-      MOBA_LAUNCH(launch_cache_gate(a, stream));
-    }
-    Phase ph("cache_select", stream);
-    MOBA_LAUNCH(launch_cache_select(a, stream));
+  if (!d.full && d.topk > 1) {
+    Phase ph("cache_gate", stream);
+    MOBA_LAUNCH(launch_cache_gate(a, stream));
   }
-  { Phase ph("cache_attend", stream);
-    MOBA_LAUNCH(launch_cache_attend(d.full, a, stream)); }
-  { Phase ph("cache_join", stream);
-    MOBA_LAUNCH(launch_cache_join(d.full, a, stream)); }
+  {
+    Phase ph("cache_attend", stream);
+    if (d.full) MOBA_LAUNCH(launch_cache_attend(a, stream));
+    else MOBA_LAUNCH(launch_cache_parts(a, stream));
+  }
+  if (d.full || d.parts > 1) {
+    Phase ph("cache_join", stream);
+    MOBA_LAUNCH(launch_cache_join(d.full, a, stream));
+  }
   return MOBA_OK;
 }
 

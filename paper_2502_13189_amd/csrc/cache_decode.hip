@@ -3,13 +3,15 @@
 // Every attended key and value is one byte per dim, read once per kv-head for all query
 // heads of its group: 256 bytes for at most 4 x 128 x 16 FLOP, so HBM bounds it.
 //
-// Lengths are known on the device alone.  The batch's keys are cut into 64-key steps and the
-// steps, request after request, into equal shares, one wave each; every wave finds its own
-// share from a prefix sum over the lengths.  So a ragged batch, one long
+// Lengths are known on the device alone.  For full attention the batch's keys are cut into
+// 64-key steps and the steps, request after request, into equal shares, one wave each; every wave
+// finds its own share from a prefix sum over the lengths.  So a ragged batch, one long
 // request and many short ones all keep the chip evenly busy, and the workspace does not depend on
 // lengths: a share leaves at most two partial rows (the one it enters with and the one it leaves
-// with), which a second launch joins; a row inside one share is finished there.  Where rows
-// are short, a work-group per row does all in one launch instead (rows).
+// with), which a second launch joins; a row inside one share is finished there.  A MoBA row
+// has no more steps than its heads choose blocks, so rows differ little and each gets as
+// many work-groups as the other (parts).  Where rows are short, a work-group per row does all
+// in one launch instead (rows).
 //
 //   attend  a step's K and V go from memory to the matrix cores through registers alone.
 //           S^T = K q^T on 16x16x32 MFMAs: a lane has 16 bytes of a key for two operands.
@@ -23,10 +25,11 @@
 //           ahead) or more waves gain nothing.
 //   gate    MoBA: a wave adds a block's k_sum rows and takes its scores with the group's
 //           heads, in 64 bits
-//   select  MoBA: a wave finds the (k-1)-th highest score of a head bit by bit; the group's
-//           heads' blocks become one ascending list with a mask of heads for each
+//   parts   MoBA: a wave finds the (k-1)-th highest score of a head bit by bit; the group's
+//           heads' blocks become one ascending list with a mask of heads for each, and the
+//           work-group attends its part of their steps
 //   join    log-sum-exp merge of split rows
-//   rows    the four of them for one (request, kv-head)
+//   rows    all of it for one (request, kv-head)
 #include "cache_internal.h"
 #include "decode_internal.h"
 
@@ -323,19 +326,13 @@ __device__ __forceinline__ void write_nothing(const CacheDecodeArgs& a, int s, i
   if (lane == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
 }
 
-template <bool MOBA>
 __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(CacheDecodeArgs a) {
   __shared__ Sums sums;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const CachePool& c = a.c;
-  const int Hkv = c.Hkv, G = a.G;
-  const int rows = MOBA ? a.S * Hkv : a.S;
-  const auto units = [&](int r) {
-    if constexpr (MOBA) return a.nsteps[r];
-    else return (held(a, r) + kCacheTile - 1) / kCacheTile;
-  };
-  sum_rows(sums, rows, units);
+  const int Hkv = a.c.Hkv, G = a.G;
+  const auto units = [&](int s) { return (held(a, s) + kCacheTile - 1) / kCacheTile; };
+  sum_rows(sums, a.S, units);
   const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
   // rows that attend nothing
   for (int r = w; r < a.S * Hkv; r += gridDim.x * (kCacheDecodeThreads / 64)) {
@@ -343,14 +340,12 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
     if (a.lens[s] > 0) continue;
     for (int h = h0; h < h0 + G; h++) write_nothing(a, s, h, lane);
   }
-  const int share = MOBA ? w : w / Hkv;
-  int g = MOBA ? 0 : w % Hkv;
+  const int share = w / Hkv, g = w % Hkv;
   if (share >= a.shares) return;
-  const int pg = MOBA ? 1 : Hkv, pi = MOBA ? 0 : g;  // partials: kv-heads per share, this one
   const int total = __builtin_amdgcn_readfirstlane(sums.total);
   // Two waves per SIMD hide a few steps' latency; where each would have many, one does as
-  // well, with half the partials (1024 and 2048 waves: 1M tokens 354 and 367 us, MoBA over
-  // them 90.5 and 92.8; ragged batch, 8 steps a wave 55.8 and 57.8; ragged MoBA, 4 steps 59 and 54)
+  // well, with half the partials (1024 and 2048 waves: 1M tokens 354 and 367 us, ragged
+  // batch, 8 steps a wave, 55.8 and 57.8)
   const int used = total / 6 >= a.shares ? (a.shares + 1) / 2 : a.shares;
   const int per_share = (total + used - 1) / used;
   int u = (int)min((int64_t)share * per_share, (int64_t)total);
@@ -358,28 +353,24 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
   CacheJoin join = {-1, 0};
   if (u < u_end) {
     int base;
-    int r = __builtin_amdgcn_readfirstlane(find_row(sums, rows, u, units, &base));
+    int s = __builtin_amdgcn_readfirstlane(find_row(sums, a.S, u, units, &base));
     const int hc = lane & 15, quad = lane >> 4;
     while (u < u_end) {
-      const int n = __builtin_amdgcn_readfirstlane(units(r));
+      const int n = __builtin_amdgcn_readfirstlane(units(s));
       if (n == 0) {
-        r++;
+        s++;
         continue;
       }
-      const int s = MOBA ? r / Hkv : r;
-      if constexpr (MOBA) g = r % Hkv;
-      const int len = held(a, s);
       const int first = u - base, last = min(n, u_end - base);
-      const uint32_t* list = MOBA ? a.list + (int64_t)r * a.nlist : nullptr;
       Row x;
-      attend_steps<MOBA>(a, s, g, len, list, first, last, x);
+      attend_steps<false>(a, s, g, held(a, s), nullptr, first, last, x);
       // a lane's sums: head hc, dims 16 i + 4 quad + e
       const bool whole = first == 0 && last == n;
       if (hc < G) {
         if (whole) {
           write_row(a, s, g * G + hc, quad, x);
         } else {
-          const int64_t at = (((int64_t)share * 2 + (first == 0)) * pg + pi) * G + hc;
+          const int64_t at = (((int64_t)share * 2 + (first == 0)) * Hkv + g) * G + hc;
           float* o = a.part_o + at * kHeadDim + 4 * quad;
 #pragma unroll
           for (int i = 0; i < 8; i++)
@@ -388,18 +379,18 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
         }
       }
       if (first == 0 && last < n)
-        join = {r, (base + n - 1) / per_share - share + 1};
+        join = {s, (base + n - 1) / per_share - share + 1};
       u = base + last;
       base += n;
-      r++;
+      s++;
     }
   }
-  if (lane == 0) a.join[(int64_t)share * pg + pi] = join;
+  if (lane == 0) a.join[(int64_t)share * Hkv + g] = join;
 }
 
 // -------------------------------------------------------------------- join
-// One work-group per (share, kv-head, head of the group); most find no split row that
-// begins in their share.  The row's partials are slot 1 of that share and slot 0 of those
+// One work-group per head: full, of a (share, kv-head), most of which find no split row that begins
+// in their share, and its partials are slot 1 of that share and slot 0 of those
 // after it.  Bound by latency: the share's entry, then partials, maxima and sums together.
 // (As 512-thread work-groups, or with half a wave per short row and a work-group for a long
 // one's heads, a ragged batch of 8 took 9 us, this way 6.)
@@ -411,14 +402,16 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheDecodeArg
   __shared__ float red[2][kJoinThreads / 64];
   __shared__ f32x4_t part[kJoinGroups][kHeadDim / 4];
   const int G = a.G, tid = threadIdx.x;
-  const int pg = full ? a.c.Hkv : 1;
-  const int hl = blockIdx.x % G;
+  const int Hkv = a.c.Hkv, hl = blockIdx.x % G;
   const int64_t at = blockIdx.x / G;
-  const CacheJoin jn = a.join[at];
-  if (jn.row < 0) return;
-  const int share = (int)(at / pg), gi = (int)(at % pg);
+  const int first = (int)(at / Hkv), g = (int)(at % Hkv);  // share or request
+  CacheJoin jn = {first, a.parts};
+  if (full) jn = a.join[at];
+  else if (a.lens[first] <= 0) return;
+  const int s = jn.row;
+  if (s < 0) return;
   const auto slot = [&](int i) {
-    return (((int64_t)(share + i) * 2 + (i == 0)) * pg + gi) * G + hl;
+    return (full ? ((int64_t)(first + i) * 2 + (i == 0)) * Hkv + g : at * a.parts + i) * G + hl;
   };
   const int d4 = tid & 31, grp = tid >> 5;  // the thread's partials are grp + 8 i
   f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -471,8 +464,6 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheDecodeArg
   for (int i = 1; i < kJoinGroups; i++)
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] += part[i][d4][e];
-  const int s = full ? jn.row : jn.row / a.c.Hkv;
-  const int g = full ? gi : jn.row % a.c.Hkv;
   const int h = g * G + hl;
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   *reinterpret_cast<uint2*>(a.out + s * a.o_ss + h * a.o_sh + 4 * d4) =
@@ -601,7 +592,7 @@ __device__ __forceinline__ void keep_blocks(int past, int nh, Score score, Put p
 #pragma unroll
   for (int x = 0; x < NW; x++) {
     const int j = 64 * x + lane;
-    key[x] = j >= past ? 0 : nh == past ? 1 : order_of(score(j));
+    key[x] = j >= past ? 0 : nh == 0 || nh == past ? 1 : order_of(score(j));  // (else there are none)
   }
   // the largest bound that at least nh keys reach
   uint64_t bound = nh == past ? 1 : 0;
@@ -667,39 +658,65 @@ __device__ __forceinline__ int block_list(const CacheDecodeArgs& a, Kept<NW>& k,
   return nu * (a.B / kCacheTile) + (len - past * a.B + kCacheTile - 1) / kCacheTile;
 }
 
-// One work-group per (request, kv-head).
-template <int NW>
-__global__ __launch_bounds__(256) void cache_select_kernel(CacheDecodeArgs a) {
-  __shared__ Kept<NW> kept;
-  const int G = a.G, Hkv = a.c.Hkv, wave = threadIdx.x >> 6;
-  const int r = blockIdx.x, s = r / Hkv, g = r % Hkv;
-  const int len = held(a, s);
-  if (len == 0) {
-    if (threadIdx.x == 0) a.nsteps[r] = 0;
-    return;
-  }
-  const int past = past_blocks(a, s);
-  for (int hl = wave; hl < G; hl += 4) {
-    const double* sc = a.score + ((int64_t)s * a.Hq + g * G + hl) * a.nblk;
-    keep_blocks<NW>(past, min(a.topk - 1, past), [&](int j) { return sc[j]; },
-                    [&](int x, unsigned long long m) { kept.of[hl][x] = m; });
-  }
-  __syncthreads();
-  const int steps = block_list(a, kept, past, len, a.list + (int64_t)r * a.nlist);
-  if (threadIdx.x == 0) a.nsteps[r] = steps;
-}
-
 // -------------------------------------------------------------------- rows
 // Short rows, a work-group for each (request, kv-head): gate, selection, attention and the
 // join of its waves in one launch.  A CU alone takes about 0.3 us per step (52 GB/s) with 4, 8
 // or 16 waves (kRowWaves).
+template <int WAVES>
+struct WaveSums {
+  f32x4_t of[4][8][64];
+  float m[WAVES][16], l[WAVES][16];
+};
+
+// The work-group's sums of a row in its first wave, from its waves'.
+template <int WAVES>
+__device__ __forceinline__ void add_waves(WaveSums<WAVES>& sm, Row& r) {
+  const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (quad == 0) sm.m[wave][hc] = r.m;
+  __syncthreads();
+  float m = sm.m[0][hc];
+#pragma unroll
+  for (int w = 1; w < WAVES; w++) m = fmaxf(m, sm.m[w][hc]);
+  const float sc = __builtin_amdgcn_exp2f(r.m - (m == -INFINITY ? 0.0f : m));
+  if (quad == 0) sm.l[wave][hc] = r.l * sc;
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+#pragma unroll
+    for (int e = 0; e < 4; e++) r.acc[i][e] *= sc;
+  // four waves' sums at a time to the first four, then to two and one
+  const auto hand = [&](int from, int n) {
+    if (wave >= from && wave < from + n) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) sm.of[wave - from][i][lane] = r.acc[i];
+    }
+    __syncthreads();
+    if (wave < n) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const f32x4_t x = sm.of[wave][i][lane];
+#pragma unroll
+        for (int e = 0; e < 4; e++) r.acc[i][e] += x[e];
+      }
+    }
+    __syncthreads();
+  };
+#pragma unroll
+  for (int from = 4; from < WAVES; from += 4) hand(from, 4);
+  hand(2, 2);
+  hand(1, 1);
+  r.m = m;
+  r.l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < WAVES; w++) r.l += sm.l[w][hc];
+}
+
 template <bool MOBA, int kRowWaves>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDecodeArgs a) {
   constexpr int kBlocks = kCacheRowBlocks;
   static_assert(kBlocks % 64 == 0 && kDecodeMaxGroup * kBlocks * 8 <= 4 * 8 * 64 * 16,
                 "the scores fit where the sums are joined");
-  __shared__ f32x4_t sums[4][8][64];
-  __shared__ float ms[kRowWaves][16], ls[kRowWaves][16];
+  __shared__ WaveSums<kRowWaves> sums;
   __shared__ Kept<kBlocks / 64> kept;
   __shared__ uint32_t list[kBlocks];
   const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
@@ -714,7 +731,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDeco
   int steps = (len + kCacheTile - 1) / kCacheTile;
   if constexpr (MOBA) {
     const int past = past_blocks(a, s), nh = min(a.topk - 1, past);
-    double* score = reinterpret_cast<double*>(sums);  // [G, kBlocks]
+    double* score = reinterpret_cast<double*>(sums.of);  // [G, kBlocks]
     if (nh > 0 && nh < past) {
       for (int j = wave; j < past; j += kRowWaves)
         block_scores(a, s, g, j, [&](int hl, double x) { score[hl * kBlocks + j] = x; });
@@ -732,44 +749,67 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDeco
   const int first = min(wave * part, steps), last = min(first + part, steps);
   Row r;
   attend_steps<MOBA>(a, s, g, len, list, first, last, r);
-  if (quad == 0) ms[wave][hc] = r.m;
-  __syncthreads();
-  float m = ms[0][hc];
-#pragma unroll
-  for (int w = 1; w < kRowWaves; w++) m = fmaxf(m, ms[w][hc]);
-  const float sc = __builtin_amdgcn_exp2f(r.m - (m == -INFINITY ? 0.0f : m));
-  if (quad == 0) ls[wave][hc] = r.l * sc;
-#pragma unroll
-  for (int i = 0; i < 8; i++)
-#pragma unroll
-    for (int e = 0; e < 4; e++) r.acc[i][e] *= sc;
-  // four waves' sums at a time to the first four, then to two and one
-  const auto hand = [&](int from, int n) {
-    if (wave >= from && wave < from + n) {
-#pragma unroll
-      for (int i = 0; i < 8; i++) sums[wave - from][i][lane] = r.acc[i];
+  add_waves(sums, r);
+  if (wave == 0 && hc < G) write_row(a, s, g * G + hc, quad, r);
+}
+
+// ------------------------------------------------------------------- parts
+// MoBA, past a gate launch: a.parts work-groups for each (request, kv-head), each of which
+// selects the row's blocks (the same for all of them) and attends its part of their steps.
+// Selection in a launch of its own before shares of equal steps, and this: 8 ragged requests
+// (130K tokens, blocks of 1024, top-4) 54.5 and 44.1 us, 4 x 4096 tokens 26.5 and 18.8, 1M
+// tokens 90.6 and 89.8; slower where a request has thousands of blocks (4096 blocks of 64,
+// top-40: 113 and 125).  NW: words of 64 blocks.
+constexpr int kPartWaves = 4;
+
+template <int NW>
+__global__ __launch_bounds__(64 * kPartWaves, 2) void cache_parts_kernel(CacheDecodeArgs a) {
+  __shared__ WaveSums<kPartWaves> sums;
+  __shared__ Kept<NW> kept;
+  __shared__ uint32_t list[64 * NW];
+  const int lane = threadIdx.x & 63, hc = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.G, Hkv = a.c.Hkv;
+  const int r = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+  const int s = r / Hkv, g = r % Hkv;
+  const int len = __builtin_amdgcn_readfirstlane(held(a, s));
+  if (len == 0) {  // (the join leaves such a row)
+    for (int hl = wave; hl < G && part == 0; hl += kPartWaves) write_nothing(a, s, g * G + hl, lane);
+    return;
+  }
+  const int past = past_blocks(a, s), nh = min(a.topk - 1, past), spb = a.B / kCacheTile;
+  // the steps are no more than if no two heads chose the same block
+  const int64_t most = (int64_t)min((int64_t)G * nh, (int64_t)past) * spb + spb;
+  Row x;
+  int first = 0, last = 0;
+  if (part * kPartWaves < most) {
+    for (int hl = wave; hl < G; hl += kPartWaves) {
+      const double* sc = a.score + ((int64_t)s * a.Hq + g * G + hl) * a.nblk;
+      keep_blocks<NW>(past, nh, [&](int j) { return sc[j]; },
+                      [&](int w, unsigned long long m) { kept.of[hl][w] = m; });
     }
     __syncthreads();
-    if (wave < n) {
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const f32x4_t x = sums[wave][i][lane];
-#pragma unroll
-        for (int e = 0; e < 4; e++) r.acc[i][e] += x[e];
-      }
-    }
+    const int steps = block_list(a, kept, past, len, list);
     __syncthreads();
-  };
-#pragma unroll
-  for (int from = 4; from < kRowWaves; from += 4) hand(from, 4);
-  hand(2, 2);
-  hand(1, 1);
+    const int each = (steps + a.parts * kPartWaves - 1) / (a.parts * kPartWaves);
+    first = (int)min((int64_t)(part * kPartWaves + wave) * each, (int64_t)steps);
+    last = min(first + each, steps);
+  } else {
+    if (threadIdx.x == 0) list[0] = (uint32_t)past;  // (an empty part looks at it, too)
+    __syncthreads();
+  }
+  attend_steps<true>(a, s, g, len, list, first, last, x);
+  add_waves(sums, x);
   if (wave != 0 || hc >= G) return;
-  r.m = m;
-  r.l = 0.0f;
+  if (a.parts == 1) {
+    write_row(a, s, g * G + hc, quad, x);
+    return;
+  }
+  const int64_t at = (int64_t)blockIdx.x * G + hc;
+  float* o = a.part_o + at * kHeadDim + 4 * quad;
 #pragma unroll
-  for (int w = 0; w < kRowWaves; w++) r.l += ls[w][hc];
-  write_row(a, s, g * G + hc, quad, r);
+  for (int i = 0; i < 8; i++) *reinterpret_cast<f32x4_t*>(o + 16 * i) = x.acc[i];
+  if (quad == 0) a.part_ml[at] = make_float2(x.m, x.l);
 }
 
 }  // namespace
@@ -780,11 +820,11 @@ hipError_t launch_cache_gate(const CacheDecodeArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st) {
-  const unsigned groups = (unsigned)(a.S * a.c.Hkv);
-  if (a.nblk <= 256) cache_select_kernel<4><<<groups, 256, 0, st>>>(a);
-  else if (a.nblk <= 1024) cache_select_kernel<16><<<groups, 256, 0, st>>>(a);
-  else cache_select_kernel<kMaxBlocksPerSeq / 64><<<groups, 256, 0, st>>>(a);
+hipError_t launch_cache_parts(const CacheDecodeArgs& a, hipStream_t st) {
+  const unsigned groups = (unsigned)(a.S * a.c.Hkv * a.parts);
+  if (a.nblk <= 256) cache_parts_kernel<4><<<groups, 64 * kPartWaves, 0, st>>>(a);
+  else if (a.nblk <= 1024) cache_parts_kernel<16><<<groups, 64 * kPartWaves, 0, st>>>(a);
+  else cache_parts_kernel<kMaxBlocksPerSeq / 64><<<groups, 64 * kPartWaves, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -802,16 +842,14 @@ hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st
   return hipGetLastError();
 }
 
-hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t st) {
-  const int64_t waves = (int64_t)a.shares * (full ? a.c.Hkv : 1);
-  const unsigned groups = (unsigned)((waves + 3) / 4);
-  if (full) cache_attend_kernel<false><<<groups, kCacheDecodeThreads, 0, st>>>(a);
-  else cache_attend_kernel<true><<<groups, kCacheDecodeThreads, 0, st>>>(a);
+hipError_t launch_cache_attend(const CacheDecodeArgs& a, hipStream_t st) {
+  const int64_t waves = (int64_t)a.shares * a.c.Hkv;
+  cache_attend_kernel<<<(unsigned)((waves + 3) / 4), kCacheDecodeThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st) {
-  const int64_t groups = (int64_t)a.shares * (full ? a.c.Hkv : 1) * a.G;
+  const int64_t groups = (int64_t)(full ? a.shares : a.S) * a.Hq;
   cache_join_kernel<<<(unsigned)groups, kJoinThreads, 0, st>>>(a, full);
   return hipGetLastError();
 }

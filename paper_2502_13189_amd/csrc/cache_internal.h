@@ -50,11 +50,12 @@ hipError_t launch_cache_write(bool bf16, const CacheWriteArgs& a, hipStream_t st
 // ---------------------------------------------------------------- decode
 constexpr int kCacheWaves = 2048;  // attention waves the chip holds: 8 on each of 256 CUs
 constexpr int kCacheGateWaves = 8192;  // waves of the gate at most (one a block, if they suffice)
+constexpr int64_t kCachePartGroups = 512;  // MoBA: work-groups that split rows fill, two on a CU
+constexpr int64_t kCachePartSteps = 256;   // and the most steps of one, however many rows
 constexpr int kCacheDecodeThreads = 256;
 constexpr int kCacheRowBlocks = 128;   // MoBA blocks of a row that one work-group takes
 
-// Where a row split over several shares begins: the row (full: request; MoBA: request *
-// Hkv + kv-head; -1: none) and the shares it spans.
+// Where a row split over several shares begins: the request (-1: none) and the shares it spans.
 struct CacheJoin {
   int32_t row, count;
 };
@@ -67,26 +68,24 @@ struct CacheDecodeArgs {
   int S, W, Hq, G;
   int B, topk;                                  // MoBA; nblk: blocks a table row holds
   int nblk;
-  int nlist;                                    // MoBA: list entries per (request, kv-head)
+  int parts;                                    // MoBA: work-groups for a (request, kv-head)
   __hip_bfloat16* out; int64_t o_ss, o_sh;
   float* lse;                                   // [Hq, S]
   float scale_log2;
-  int shares;        // of the batch's 64-key steps; full: of each kv-head
+  int shares;        // full: of the batch's 64-key steps, of each kv-head
   int gate_shares;   // of the batch's past blocks, of each kv-head
   // workspace
   double* score;     // [S, Hq, nblk] gate scores
-  uint32_t* list;    // [S * Hkv, nlist] blocks attended: index | heads << 16, ascending
-  int32_t* nsteps;   // [S * Hkv] 64-key steps of the list
-  float* part_o;     // [shares, 2, Hkv (MoBA: 1), G, D] unnormalised partials
-  float2* part_ml;   // [shares, 2, Hkv (MoBA: 1), G] their max (log2 domain) and sum
-  CacheJoin* join;   // [shares, Hkv (MoBA: 1)]
+  float* part_o;     // full [shares, 2, Hkv, G, D], MoBA [S, Hkv, parts, G, D]: unnormalised partials
+  float2* part_ml;   // [..., G] their max (log2 domain) and sum
+  CacheJoin* join;   // full [shares, Hkv]
 };
 // Gate, selection, attention and join in one launch, a work-group per (request, kv-head); for
 // table rows of up to kCacheRowBlocks blocks (MoBA).  Needs no workspace.
 hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st);
 hipError_t launch_cache_gate(const CacheDecodeArgs& a, hipStream_t st);
-hipError_t launch_cache_select(const CacheDecodeArgs& a, hipStream_t st);
-hipError_t launch_cache_attend(bool full, const CacheDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_parts(const CacheDecodeArgs& a, hipStream_t st);
+hipError_t launch_cache_attend(const CacheDecodeArgs& a, hipStream_t st);
 hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st);
 
 }  // namespace moba

@@ -444,6 +444,20 @@ def test_decode_splits(lens, hq, hkv, page, block, topk):
     check(pool, table, lens, hq, block, topk, rng)
 
 
+@pytest.mark.parametrize("lens,hq,hkv,page,block,topk", [
+    ([300, 64, 1] * 50 + [9000], 4, 4, 64, 64, 3),   # a work-group for each of 604 rows, unjoined
+    ([300, 0, 5000, -1] * 20, 12, 4, 64, 64, 9),     # two work-groups a row, some of them idle
+    ([12345, 3, 0, 7000], 16, 1, 128, 1024, 6),      # many, of long blocks
+    ([20000, 19999], 4, 1, 64, 2048, 1),             # the current block alone: no gate
+    ([16500], 3, 1, 64, 64, 257),                    # all past blocks but one
+])
+def test_decode_parts(lens, hq, hkv, page, block, topk):
+    rng = np.random.default_rng(len(lens) + topk)
+    W = max(-(-max(lens) // page) + 2, 131)
+    pool, table = some_cache(rng, lens, hkv, page, W)
+    check(pool, table, lens, hq, block, topk, rng)
+
+
 @pytest.mark.parametrize("W", WIDTHS)
 @pytest.mark.parametrize("topk", [0, 2, 3])
 def test_decode_bad_table_entries(topk, W):
