@@ -5,17 +5,20 @@
 // from three prefix sums over the requests (new tokens, pages given back, pages needed), done by
 // one work-group: the whole step of a decode batch is a few hundred integers, bound by the
 // latency of one launch and its chain of dependent loads (add and lens, the free list, the
-// table).  The slots of a long prompt are the only bytes in quantity (8 per token): past
-// kPlanOwnTokens of them a second launch writes them over the whole chip.
+// table).  The slots of a long prompt are the only bytes in quantity (8 per token, and 4 per
+// page): past kPlanOwnTokens of them a second launch writes them over the whole chip, and, past
+// kPlanOwnPages, the tables' new pages, where its work-groups have a thread for every request.
 //
 // Measured: 64 requests, one token each, two ending: 5.0 us (a launch that does nothing takes
-// about 3); 1M tokens of 8 prompts into 16384 pages: 12.4 us and 6.1 us for their slots.
+// about 3); 1M tokens of 8 prompts into 16384 pages: 5.9 us, and 8.6 for their slots and
+// pages (with the pages in the first launch, 12.4 and 6.1).
 #include "cache_internal.h"
 
 namespace moba {
 namespace {
 
 constexpr int kPlanOwnTokens = 8192;
+constexpr int kPlanOwnPages = 65536;  // tokens, up to which the first launch takes their pages
 constexpr int kPlanPer = 4;         // requests per thread at most, of kPlanThreads
 constexpr int kPlanThreads = kPlanMaxRequests / kPlanPer;
 constexpr int kLightTokens = 4;     // at most, of every request: none of them searches (a
@@ -110,8 +113,10 @@ __device__ __forceinline__ void each_item(const int32_t* pre, int S, uint32_t n,
 }
 
 // own_slots: this launch writes slots; otherwise only the one of each request's first
-// token (where cache_slots_kernel finds whether the request was refused).
-__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs a, bool own_slots) {
+// token (where cache_slots_kernel finds whether the request was refused).  own_pages: it
+// writes the new pages into the tables.
+__global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs a, bool own_slots,
+                                                                  bool own_pages) {
   extern __shared__ int32_t lds[];
   __shared__ int64_t part[3][kPlanThreads / 64];
   __shared__ int64_t totals[3];  // pages given back, pages taken, new tokens
@@ -238,10 +243,11 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs 
     const int page = j < h ? a.table[s * a.t_ss + j] : a.free_pages[avail - 1 - (pre[s] + (int64_t)(j - h))];
     return (int64_t)page * P + (pos - j * P);
   };
-  each_item(pre, S, (uint32_t)take, [&](uint32_t i, int) { return a.free_pages[avail - 1 - i]; },
-            [&](uint32_t i, int s, int32_t page) {
-              a.table[s * a.t_ss + held(s) + (i - pre[s])] = page;
-            });
+  if (own_pages)
+    each_item(pre, S, (uint32_t)take, [&](uint32_t i, int) { return a.free_pages[avail - 1 - i]; },
+              [&](uint32_t i, int s, int32_t page) {
+                a.table[s * a.t_ss + held(s) + (i - pre[s])] = page;
+              });
   if (own_slots) {
     for (int64_t x0 = tid; x0 < a.T; x0 += 8 * nt) {
       uint32_t at[8];
@@ -265,12 +271,33 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs 
 }
 
 // The slots of every token.  cache_plan_kernel left each request's first one (written again
-// here, with the same value): -1 where the request was refused.
+// here, with the same value): -1 where the request was refused.  PAGES (S <= kSlotThreads): and
+// the new pages of the tables, from the free list, by the page's first token; where a
+// request's begin on the list follows from the lengths.
+template <bool PAGES>
 __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs a) {
-  const int lane = threadIdx.x & 63;
+  __shared__ int64_t part[kPlanThreads / 64];
+  __shared__ int32_t before[kSlotThreads];  // pages that earlier requests take
+  __shared__ int64_t taken;
+  const int lane = threadIdx.x & 63, P = a.P;
   const int64_t w0 = ((int64_t)blockIdx.x * kSlotThreads + (threadIdx.x & ~63)) * kSlotPer;  // the wave's
-  if (w0 >= a.T) return;
   const int64_t all = a.cu[a.S];
+  int64_t top = 0;  // pages on the free list before any was taken
+  if constexpr (PAGES) {
+    const int r = threadIdx.x;
+    int64_t need = 0;
+    if (r < a.S) {
+      const int c = a.cu[r];
+      const uint32_t now = (uint32_t)a.lens_out[r], tok = (uint32_t)max(a.add[r], 0);
+      if (c < a.cu[r + 1] && a.slots[c] >= 0) need = pages_of(now, P) - pages_of(now - tok, P);
+    }
+    const int64_t upto = group_scan(need, part);
+    before[r] = (int32_t)(upto - need);
+    if (r == kSlotThreads - 1) taken = upto;
+    __syncthreads();
+    top = *a.num_free_out + taken;
+  }
+  if (w0 >= a.T) return;
   // the requests of the wave's first and last token, 64 candidates at a time
   int lo = 0, hi = 0;
   for (int width = a.S; width > 1;) {
@@ -281,28 +308,39 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
     hi += step * (max((int)__popcll(__ballot(c1 <= w0 + 64 * kSlotPer - 1)), 1) - 1);
     width = step;
   }
+  // the slot of position pos of a granted request s that held h pages; its page for the table
+  const auto slot_of = [&](int s, uint32_t pos, uint32_t h) {
+    const uint32_t j = page_of(pos, P);
+    int32_t* at = a.table + s * a.t_ss + j;
+    int32_t page;
+    if (PAGES && j >= h) {
+      page = a.free_pages[top - 1 - (before[s] + (int64_t)(j - h))];
+      if (pos == j * P) *at = page;
+    } else {
+      page = *at;
+    }
+    return (int64_t)page * P + (pos - j * P);
+  };
   if (lo == hi && w0 + 64 * kSlotPer <= all) {  // one request's, as in a long prompt
     const int r = __builtin_amdgcn_readfirstlane(lo), begin = a.cu[r];
     const bool ok = a.slots[begin] >= 0;
-    const uint32_t pos0 = (uint32_t)(a.lens_out[r] - a.add[r] + (int)(w0 - begin)) + lane;
-    const int32_t* row = a.table + r * a.t_ss;
+    const uint32_t old = (uint32_t)(a.lens_out[r] - a.add[r]);
+    const uint32_t pos0 = old + (uint32_t)(w0 - begin) + lane, h = pages_of(old, P);
     int64_t slot[kSlotPer];
 #pragma unroll
-    for (int i = 0; i < kSlotPer; i++) {
-      const uint32_t pos = pos0 + 64 * i, j = page_of(pos, a.P);
-      slot[i] = ok ? (int64_t)row[j] * a.P + (pos - j * a.P) : -1;
-    }
+    for (int i = 0; i < kSlotPer; i++) slot[i] = ok ? slot_of(r, pos0 + 64 * i, h) : -1;
 #pragma unroll
     for (int i = 0; i < kSlotPer; i++) a.slots[w0 + 64 * i + lane] = slot[i];
     return;
   }
   const int64_t x0 = w0 + lane * kSlotPer;
   int s = lo, c0 = 0;
-  for (int top = hi; s < top;) {  // among them, this thread's first
-    const int mid = (s + top + 1) >> 1;
-    if (a.cu[mid] <= x0) s = mid; else top = mid - 1;
+  for (int last = hi; s < last;) {  // among them, this thread's first
+    const int mid = (s + last + 1) >> 1;
+    if (a.cu[mid] <= x0) s = mid; else last = mid - 1;
   }
   int64_t end = -1, old = 0;  // where request s ends; its length before the step
+  uint32_t h = 0;
   bool granted = false;
   int64_t slot[kSlotPer];
 #pragma unroll
@@ -316,11 +354,9 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
         end = a.cu[s + 1];
         granted = a.slots[c0] >= 0;
         old = (int64_t)a.lens_out[s] - a.add[s];
+        if (granted) h = pages_of((uint32_t)old, P);
       }
-      if (granted) {
-        const uint32_t pos = (uint32_t)(old + (x - c0)), j = page_of(pos, a.P);
-        slot[i] = (int64_t)a.table[s * a.t_ss + j] * a.P + (pos - j * a.P);
-      }
+      if (granted) slot[i] = slot_of(s, (uint32_t)(old + (x - c0)), h);
     }
   }
   if (x0 + kSlotPer <= a.T) {
@@ -338,14 +374,19 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
 
 hipError_t launch_cache_plan(const CachePlanArgs& a, hipStream_t st) {
   const bool own = a.T <= kPlanOwnTokens;
+  // New pages from one work-group, and from the second launch (whole calls): 10000 tokens
+  // in 8 requests 11.5, 13.2 us, 32768 12.3, 12.4, 524288 14.1, 12.9; in 200 requests 10000 16.0,
+  // 17.8, 131072 20.1, 16.8; 2M in 256 43, 20.
+  const bool pages = a.T <= kPlanOwnPages || a.S > kSlotThreads;
   // threads for the requests, and for the pages and slots to write (64 tokens in 8 requests:
   // 4.9 us with 64 threads, 8.2 with 1024)
-  const int nt = a.S <= 64 && a.T <= 256 ? 64 : a.S <= 256 && a.T <= 16384 ? 256 : kPlanThreads;
-  cache_plan_kernel<<<1, nt, 3 * sizeof(int32_t) * (size_t)a.S, st>>>(a, own);
+  const int nt = a.S <= 64 && a.T <= 256 ? 64 : a.S <= 256 && (!pages || a.T <= 16384) ? 256 : kPlanThreads;
+  cache_plan_kernel<<<1, nt, 3 * sizeof(int32_t) * (size_t)a.S, st>>>(a, own, pages);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || own) return e;
-  const int64_t groups = (a.T + kSlotThreads * kSlotPer - 1) / (kSlotThreads * kSlotPer);
-  cache_slots_kernel<<<(unsigned)groups, kSlotThreads, 0, st>>>(a);
+  const unsigned groups = (unsigned)((a.T + kSlotThreads * kSlotPer - 1) / (kSlotThreads * kSlotPer));
+  if (pages) cache_slots_kernel<false><<<groups, kSlotThreads, 0, st>>>(a);
+  else cache_slots_kernel<true><<<groups, kSlotThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 

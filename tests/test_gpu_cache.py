@@ -110,6 +110,29 @@ def test_plan(S, W, page, spare, most, slack, in_place):
         check_plan(add, lens, table, free, n, page, T, in_place, wide=seed * 3)
 
 
+@pytest.mark.parametrize("S,W,page,spare,most,slack", [
+    (256, 40, 64, 3000, 600, 11), (257, 40, 64, 3000, 600, 0), (200, 9, 192, 100, 200, -300),
+    (256, 70, 128, 9000, 4, 70000), (100, 300, 64, 8000, 9000, 5), (1, 2000, 64, 2000, 100000, 1),
+    (30, 200, 256, 500, 20000, 700), (200, 80, 192, 1000, 900, -5000), (9, 90, 64, 300, 5000, 60000),
+])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plan_of_long_steps(S, W, page, spare, most, slack, in_place):
+    """Steps of more tokens than one work-group writes; requests that end and are refused among
+    them, and such as begin on a page's last token."""
+    for seed in range(2):
+        rng = np.random.default_rng(seed + 10 * S + W)
+        lens, table, free, n = some_batch(rng, S, W // 2, page, spare)
+        table = np.concatenate([table, rng.integers(-5, n, (S, W - W // 2))], 1)
+        lens[lens % page == 1] -= 1
+        add = rng.integers(most // 2, most + 1, S)
+        add[rng.random(S) < 0.1] = 0
+        add[rng.random(S) < 0.2] = -1
+        add[0] = most
+        T = int(np.maximum(add, 0).sum()) + slack
+        assert T > 8192
+        check_plan(add, lens, table, free, n, page, T, in_place, wide=seed)
+
+
 def test_plan_of_nothing():
     check_plan([], [], np.zeros((0, 3), int), np.arange(5), 4, 64, 3)
     check_plan([0, 0], [5, 0], np.zeros((2, 3), int), np.arange(5), 4, 64, 0)
