@@ -25,6 +25,7 @@
 
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 namespace moba {
@@ -534,16 +535,20 @@ cache_write_kernel(CacheWriteArgs a, int window, uint32_t first) {
 template <typename T, int TILES>
 hipError_t launch(const CacheWriteArgs& a, hipStream_t st) {
   // A work-group takes the runs that begin in its window: of four tokens for each of the
-  // page's tiles (its waves) where every row may be a run of its own (a decode step), up to a
-  // page's where there are rows enough to fill the chip either way.  There the rows are
-  // prompts', and the kernel without the path of single tokens needs fewer registers:
-  // 117017 tokens of prompts take 149 us with it and 157 with the other.
+  // page's tiles (its waves) where every row may be a run of its own (a decode step), and of as
+  // many times that, up to a page, as lets the chip hold all work-groups at once (about
+  // 1024 tiles' worth; with four times as many, and half of them): 10000 tokens of one prompt,
+  // pages of 128, 2 kv-heads 10.3 us (37.3, 10.6), 8 kv-heads 19.1 (38.2, 19.0), 64 x 16 tokens 11.2
+  // (18.1, 14.8), one token each of 1024 requests, pages of 256, 27.5 (28.2, 34.2); 1024 x 40
+  // tokens, pages of 128, 2 kv-heads 58.0 (43.5, 57.4).
+  // Where rows are many they are prompts', and the kernel without the path of single tokens
+  // needs fewer registers: 117017 tokens of prompts take 149 us with it and 157 with the other.
   constexpr int P = TILES * kCacheTile, threads = kTileThreads * TILES;
-  int window = 4 * TILES;
-  while (2 * window <= P && a.T * a.c.Hkv * TILES / (2 * window) >= 4096) window *= 2;
+  const int64_t rows = a.T * a.c.Hkv;
+  const int window = (int)std::min<int64_t>(4 * TILES * ((rows + 4095) / 4096), P);
   const int64_t groups = (a.T + window - 1) / window * a.c.Hkv;
   return launch_pieces(groups, threads, [&](uint32_t first, unsigned n) {
-    if (2 * window <= P) cache_write_kernel<T, TILES, true><<<n, threads, 0, st>>>(a, window, first);
+    if (rows < 64 * 4096) cache_write_kernel<T, TILES, true><<<n, threads, 0, st>>>(a, window, first);
     else cache_write_kernel<T, TILES, false><<<n, threads, 0, st>>>(a, window, first);
   });
 }
