@@ -481,6 +481,14 @@ def test_decode_parts(lens, hq, hkv, page, block, topk):
     check(pool, table, lens, hq, block, topk, rng)
 
 
+@pytest.mark.parametrize("lens", [[2049], [2112, 1], [4096], [4097], [1000, 0, 1100], [64] * 33, [64] * 32])
+def test_decode_share_of_two_steps(lens):
+    """32 kv-heads have 64 shares each: up to 32 steps, up to 64 and more."""
+    rng = np.random.default_rng(sum(lens))
+    pool, table = some_cache(rng, lens, 32, 64, 80)
+    check(pool, table, lens, 64, 0, 0, rng)
+
+
 @pytest.mark.parametrize("W", WIDTHS)
 @pytest.mark.parametrize("topk", [0, 2, 3])
 def test_decode_bad_table_entries(topk, W):
