@@ -587,7 +587,9 @@ __device__ __forceinline__ uint64_t order_of(double x) {
 }
 
 // put(x, mask of the kept blocks 64 x ..) for the nh highest scores among `past` blocks (of
-// equal ones the first), by a wave.  NW: words of 64 blocks.
+// equal ones the first), by a wave.  NW: words of 64 blocks.  (Searching 64 bits at once, from the
+// first bit on, whole calls: 1049 blocks, top-8, 3 heads to a kv-head 55.0 us, this way 32.9; 2048
+// blocks, 16 heads 186, 105; up to 256 blocks the same.)
 template <int NW, typename Score, typename Put>
 __device__ __forceinline__ void keep_blocks(int past, int nh, Score score, Put put) {
   const int lane = threadIdx.x & 63;
@@ -597,11 +599,51 @@ __device__ __forceinline__ void keep_blocks(int past, int nh, Score score, Put p
     const int j = 64 * x + lane;
     key[x] = j >= past ? 0 : nh == 0 || nh == past ? 1 : order_of(score(j));  // (else there are none)
   }
-  // the largest bound that at least nh keys reach
+  // the largest bound that at least nh keys reach, its upper word first
+  const auto upper = [&](int x) { return (uint32_t)(key[x] >> 32); };
+  const auto reaching = [&](uint32_t c) {  // keys whose upper word reaches c
+    int n = 0;
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      if constexpr (NW < 16) n += __popcll(__ballot(upper(x) >= c));
+      else n += upper(x) >= c;
+    }
+    return NW < 16 ? n : __builtin_amdgcn_readlane(wave_scan(n), 63);
+  };
+  uint32_t high = 0;
   uint64_t bound = nh == past ? 1 : 0;
   int reach = nh == past ? nh : 0;  // keys that reach it, where that was counted
-  for (int bit = 63; bit >= 0 && reach != nh && nh > 0; bit--) {
-    const uint64_t cand = bound | (uint64_t(1) << bit);
+  const bool search = nh > 0 && nh < past;
+  int bit = 31;
+  if (NW >= 16 && search && nh <= 64) {
+    // the lanes' highest: nh of them reach the nh-th, so it bounds from below; what it has in
+    // common with the highest of all needs no search
+    uint32_t most = 0, least = 0, top = 0;
+#pragma unroll
+    for (int x = 0; x < NW; x++) most = max(most, upper(x));
+#pragma unroll 1
+    for (int b = 31; b >= 0; b--) {
+      const uint32_t m = 1u << b;
+      if (__popcll(__ballot(most >= (least | m))) >= nh) least |= m;
+      if (__ballot(most >= (top | m))) top |= m;
+    }
+    const uint32_t differ = least ^ top;
+    bit = differ ? 31 - __clz(differ) : -1;
+    high = bit < 31 ? least >> (bit + 1) << (bit + 1) : 0;
+  }
+#pragma unroll 1
+  for (; bit >= 0 && search && reach != nh; bit--) {
+    const uint32_t cand = high | 1u << bit;
+    const int n = reaching(cand);
+    if (n >= nh) {
+      high = cand;
+      reach = n;
+    }
+  }
+  if (search) bound = (uint64_t)high << 32;
+#pragma unroll 1
+  for (bit = 31; bit >= 0 && search && reach != nh; bit--) {
+    const uint64_t cand = bound | (uint64_t)1 << bit;
     int n = 0;
 #pragma unroll
     for (int x = 0; x < NW; x++) n += __popcll(__ballot(key[x] >= cand));
@@ -761,8 +803,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDeco
 // selects the row's blocks (the same for all of them) and attends its part of their steps.
 // Selection in a launch of its own before shares of equal steps, and this: 8 ragged requests
 // (130K tokens, blocks of 1024, top-4) 54.5 and 44.1 us, 4 x 4096 tokens 26.5 and 18.8, 1M
-// tokens 90.6 and 89.8; slower where a request has thousands of blocks (4096 blocks of 64,
-// top-40: 113 and 125).  NW: words of 64 blocks.
+// tokens 90.6 and 88.6, 4096 blocks of 64, top-40, 113 and 106.  NW: words of 64 blocks.
 constexpr int kPartWaves = 4;
 
 template <int NW>
@@ -827,6 +868,7 @@ hipError_t launch_cache_parts(const CacheDecodeArgs& a, hipStream_t st) {
   const unsigned groups = (unsigned)(a.S * a.c.Hkv * a.parts);
   if (a.nblk <= 256) cache_parts_kernel<4><<<groups, 64 * kPartWaves, 0, st>>>(a);
   else if (a.nblk <= 1024) cache_parts_kernel<16><<<groups, 64 * kPartWaves, 0, st>>>(a);
+  else if (a.nblk <= 2048) cache_parts_kernel<32><<<groups, 64 * kPartWaves, 0, st>>>(a);
   else cache_parts_kernel<kMaxBlocksPerSeq / 64><<<groups, 64 * kPartWaves, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -481,6 +481,23 @@ def test_decode_parts(lens, hq, hkv, page, block, topk):
     check(pool, table, lens, hq, block, topk, rng)
 
 
+@pytest.mark.parametrize("W", [257, 1025, 2049, 4096])
+@pytest.mark.parametrize("topk", [1, 2, 33, 65, 66, 70])
+def test_decode_selection(topk, W):
+    """Wide tables, few and many blocks chosen, pages with equal sums and with NaN among them,
+    sums that differ in their last bits alone or by many powers of two."""
+    rng = np.random.default_rng(topk)
+    lens = [5000, 63, 4200, 4200]
+    pool, table = some_cache(rng, lens, 2, 64, W)
+    for j in range(3, 30):  # (equal scores, as another page's)
+        pool.k_sum[table[0, j]] = pool.k_sum[table[0, 2]]
+    pool.k_sum[table[0, 40]] = np.nan
+    for j in range(60):
+        pool.k_sum[table[2, j]] = pool.k_sum[table[2, 0]] * np.float32(1 + (j * 7 % 60) * 2.0 ** -22)
+        pool.k_sum[table[3, j]] *= np.float32(2.0 ** ((j * 13) % 60 - 30))
+    check(pool, table, lens, 4, 64, topk, rng)
+
+
 @pytest.mark.parametrize("lens", [[2049], [2112, 1], [4096], [4097], [1000, 0, 1100], [64] * 33, [64] * 32])
 def test_decode_share_of_two_steps(lens):
     """32 kv-heads have 64 shares each: up to 32 steps, up to 64 and more."""
