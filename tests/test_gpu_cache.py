@@ -139,6 +139,14 @@ def test_plan_of_nothing():
     check_plan([1, 1], [63, 64], np.array([[4, 0], [3, 0]]), np.zeros(0, int), 0, 64, 2)
 
 
+def test_plan_of_nothing_in_long_steps():
+    """No requests, none that gets a token, and none that is granted one, with slots for many."""
+    for T in (9000, 70000):
+        check_plan([], [], np.zeros((0, 3), int), np.arange(5), 4, 64, T)
+        check_plan([0, -1, 0], [5, 64, 0], np.array([[1, 9], [3, 9], [9, 9]]), np.arange(5), 3, 64, T)
+        check_plan([200, 20000], [5, 0], np.array([[1, 9], [9, 9]]), np.arange(5), 3, 64, T)
+
+
 def test_plan_returns_then_takes():
     """The pages of a request that ends are what the next one gets; a request that asks for
     too much on its own does not starve the ones after it, one that finds the list short
