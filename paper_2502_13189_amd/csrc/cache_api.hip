@@ -94,7 +94,7 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
   const int64_t partials = d.full ? (int64_t)d.shares * 2 * d.Hkv : d.parts > 1 ? d.S * d.Hkv * d.parts : 0;
   take(&a->part_o, partials * G * kHeadDim);
   take(&a->part_ml, partials * G);
-  if (d.full) take(&a->join, (int64_t)d.shares * d.Hkv);
+  if (d.full) take(&a->join, std::min<int64_t>(d.S, d.shares) * d.Hkv);
   else take(&a->score, d.topk > 1 ? d.S * d.Hq * d.nblk : 0);
   return off;
 }
@@ -104,10 +104,9 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
 // step, so a row's most (what its table row can hold, MoBA: select) is held against what
 // the other way takes: its launches, while there is little to do, and the batch's share
 // of the chip where there is much.  Whole calls, split and by rows, all rows full:
-//   full  64 tokens .. 1024, any number of rows    10.5 and 7.6 .. 9.8 us
-//         2048: 16 rows 13.3, 15.2; 128 rows 23.2, 16.4; 2048 rows 183, 182
-//         4096: 16 rows 13.6, 25.5; 512 rows 104, 93; 8192: 512 rows 193, 181 (but ragged
-//         118, 120)
+//   full  64 tokens .. 1024, up to 128 rows        10.5 .. 13.3 and 7.6 .. 10.5 us
+//         2048: 16 rows 12.2, 15.2; 128 rows 18.4, 16.4 (ragged 12.7, 13.7); 2048 rows 188, 183
+//         4096: 16 rows 13.4, 25.5; 512 rows 98, 93 (ragged 28, 34); 8192: 512 rows 184, 181
 //   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 16.0, 18.0 (ragged 12.2, 8.1), 64 rows 19.3,
 //         19.6; 4096: 128 rows 29.9, 28.7, 2048 rows 271, 253; 8192: 128 rows 33.6, 33.8 (ragged
 //         23.3, 27.3), 512 rows 94, 90
@@ -297,6 +296,7 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
   a.nblk = d.nblk;
   a.parts = d.parts;
   a.shares = d.shares;
+  a.join_rows = d.S <= d.shares;
   a.gate_shares = d.gate_shares;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)kHeadDim));
   if (d.rows) {

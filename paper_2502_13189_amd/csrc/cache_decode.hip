@@ -339,6 +339,7 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
     const int s = r / Hkv, h0 = r % Hkv * G;
     if (a.lens[s] > 0) continue;
     for (int h = h0; h < h0 + G; h++) write_nothing(a, s, h, lane);
+    if (lane == 0 && a.join_rows) a.join[r] = {-1, 0};
   }
   const int share = w / Hkv, g = w % Hkv;
   if (share >= a.shares) return;
@@ -381,20 +382,25 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
           if (quad == 0) a.part_ml[at] = make_float2(x.m, x.l);
         }
       }
-      if (first == 0 && last < n)
-        join = {s, (base + n - 1) / per_share - share + 1};
+      if (first == 0) {
+        join = {-1, 0};
+        if (last < n) join = {a.join_rows ? share : s, (base + n - 1) / per_share - share + 1};
+        if (lane == 0 && a.join_rows) a.join[(int64_t)s * Hkv + g] = join;
+      }
       u = base + last;
       base += n;
       s++;
     }
   }
-  if (lane == 0) a.join[(int64_t)share * Hkv + g] = join;
+  if (lane == 0 && !a.join_rows) a.join[(int64_t)share * Hkv + g] = join;
 }
 
 // -------------------------------------------------------------------- join
-// One work-group per head: full, of a (share, kv-head), most of which find no split row that begins
-// in their share, and its partials are slot 1 of that share and slot 0 of those
-// after it.  Bound by latency: the share's entry, then partials, maxima and sums together.
+// One work-group per head of a request, or of a share where requests are more (join_rows: with
+// those of every share always, 2048 times 16 heads, 18 requests of 10496 tokens, 16/1 heads,
+// took 33.8 us instead of 21.2); it may find that nothing is split.  Full: the partials are
+// slot 1 of the row's first share and slot 0 of those after it.  Bound by latency: the
+// entry, then partials, maxima and sums together.
 // (As 512-thread work-groups, or with half a wave per short row and a work-group for a long
 // one's heads, a ragged batch of 8 took 9 us, this way 6.)
 constexpr int kJoinThreads = 256;
@@ -407,12 +413,13 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheDecodeArg
   const int G = a.G, tid = threadIdx.x;
   const int Hkv = a.c.Hkv, hl = blockIdx.x % G;
   const int64_t at = blockIdx.x / G;
-  const int first = (int)(at / Hkv), g = (int)(at % Hkv);  // share or request
-  CacheJoin jn = {first, a.parts};
+  const int i = (int)(at / Hkv), g = (int)(at % Hkv);  // request or share
+  CacheJoin jn = {i, a.parts};
   if (full) jn = a.join[at];
-  else if (a.lens[first] <= 0) return;
-  const int s = jn.row;
-  if (s < 0) return;
+  else if (a.lens[i] <= 0) return;
+  if (jn.at < 0) return;
+  const bool of_row = !full || a.join_rows;
+  const int s = of_row ? i : jn.at, first = of_row ? jn.at : i;
   const auto slot = [&](int i) {
     return (full ? ((int64_t)(first + i) * 2 + (i == 0)) * Hkv + g : at * a.parts + i) * G + hl;
   };
@@ -894,7 +901,7 @@ hipError_t launch_cache_attend(const CacheDecodeArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_cache_join(bool full, const CacheDecodeArgs& a, hipStream_t st) {
-  const int64_t groups = (int64_t)(full ? a.shares : a.S) * a.Hq;
+  const int64_t groups = (int64_t)(full && !a.join_rows ? a.shares : a.S) * a.Hq;
   cache_join_kernel<<<(unsigned)groups, kJoinThreads, 0, st>>>(a, full);
   return hipGetLastError();
 }

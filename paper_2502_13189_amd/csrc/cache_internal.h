@@ -55,9 +55,11 @@ constexpr int64_t kCachePartSteps = 256;   // and the most steps of one, however
 constexpr int kCacheDecodeThreads = 256;
 constexpr int kCacheRowBlocks = 128;   // MoBA blocks of a row that one work-group takes
 
-// Where a row split over several shares begins: the request (-1: none) and the shares it spans.
+// A row split over several shares.  Of a request's entry: the share it begins in, of a share's
+// (where requests are more than shares): the request that begins in it; -1: none; and the shares
+// it spans.
 struct CacheJoin {
-  int32_t row, count;
+  int32_t at, count;
 };
 
 struct CacheDecodeArgs {
@@ -73,12 +75,13 @@ struct CacheDecodeArgs {
   float* lse;                                   // [Hq, S]
   float scale_log2;
   int shares;        // full: of the batch's 64-key steps, of each kv-head
+  bool join_rows;    // full: an entry of join for every request, not for every share
   int gate_shares;   // of the batch's past blocks, of each kv-head
   // workspace
   double* score;     // [S, Hq, nblk] gate scores
   float* part_o;     // full [shares, 2, Hkv, G, D], MoBA [S, Hkv, parts, G, D]: unnormalised partials
   float2* part_ml;   // [..., G] their max (log2 domain) and sum
-  CacheJoin* join;   // full [shares, Hkv]
+  CacheJoin* join;   // full [S (join_rows) or shares, Hkv]
 };
 // Gate, selection, attention and join in one launch, a work-group per (request, kv-head); for
 // table rows of up to kCacheRowBlocks blocks (MoBA).  Needs no workspace.

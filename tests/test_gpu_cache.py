@@ -489,6 +489,15 @@ def test_decode_parts(lens, hq, hkv, page, block, topk):
     check(pool, table, lens, hq, block, topk, rng)
 
 
+@pytest.mark.parametrize("lens", [[300, 0, 1, 900, 64] * 13, [100] * 64, [300, 0, 1, 900] * 16,
+                                  [0] * 70 + [2000], [0] * 63 + [2000]])
+def test_decode_more_requests_than_shares(lens):
+    """32 kv-heads have 64 shares each, for up to 64 requests and for more."""
+    rng = np.random.default_rng(len(lens))
+    pool, table = some_cache(rng, lens, 32, 64, 80)
+    check(pool, table, lens, 32, 0, 0, rng)
+
+
 @pytest.mark.parametrize("W", [257, 1025, 2049, 4096])
 @pytest.mark.parametrize("topk", [1, 2, 33, 65, 66, 70])
 def test_decode_selection(topk, W):
