@@ -387,7 +387,7 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  * are left out as if masked (their page's k_sum counts as 0).  Hq / Hkv must not exceed 16.
  * workspace: moba_cache_decode_workspace_bytes of device memory, 16-byte aligned; it needs no
  * initialisation and nothing is kept in it after the call.  fp32 softmax and sums; the keys, the
- * queries and the values enter the matrix cores exactly, the weights as two bf16 terms.
+ * queries, the values and the weights (as three bf16 terms) enter the matrix cores exactly.
  * Results do not depend on timing; a request's split over work-groups, and with it its
  * rounding, depends on the whole batch.
  */

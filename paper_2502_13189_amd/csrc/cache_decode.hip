@@ -18,9 +18,10 @@
 //           The keys of a step are dealt to the four 16-key operands so that a lane's 16
 //           scores of a head are 16 consecutive tokens, which is what it then needs as the
 //           operand of O^T = V^T P^T, with V's 16 tokens of a dim being one 16-byte load of the
-//           page's token-minor tile.  e4m3 is exact in bf16; the weights enter as a bf16 and
-//           the bf16 of its remainder (in one term alone: 362.1 us, so 363.5), the scales through
-//           the logits and the weights.  1M tokens, 32/8 heads: 2.15 GB in 345 us, 6.2
+//           page's token-minor tile.  e4m3 is exact in bf16; the weights enter as three
+//           bf16 terms, which hold their 24 bits (in two, 17 bits, whole calls over 1M tokens take
+//           355.4 us, so 355.8; a ragged batch 46.0 and 47.2), the scales through the logits and the
+//           weights.  1M tokens, 32/8 heads: 2.15 GB in 345 us, 6.2
 //           TB/s, what bare loads reach; more loads in flight (next keys or whole steps
 //           ahead) or more waves gain nothing.
 //   gate    MoBA: a wave adds a block's k_sum rows and takes its scores with the group's
@@ -268,27 +269,37 @@ __device__ __forceinline__ void attend_steps(const CacheDecodeArgs& a, int s, in
         for (int e = 0; e < 4; e++) acc[i][e] *= sc;
     }
     const float mr = m == -INFINITY ? 0.0f : m;
-    // weights times the page's scale, as two bf16 terms
-    u32x4_t hi[2], lo[2];
+    // weights times the page's scale, as three bf16 terms: all 24 bits
+    u32x4_t w[3][2];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const float p0 = __builtin_amdgcn_exp2f(z[2 * i] - mr);
       const float p1 = __builtin_amdgcn_exp2f(z[2 * i + 1] - mr);
       l += p0 + p1;
-      const float v0 = p0 * t.vs, v1 = p1 * t.vs;
-      const uint32_t h = pack_bf16(v0, v1);
-      hi[i >> 2][i & 3] = h;
-      lo[i >> 2][i & 3] = pack_bf16(v0 - bf16_lo(h), v1 - bf16_hi(h));
-    }
+      float v0 = p0 * t.vs, v1 = p1 * t.vs;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
+      for (int n = 0; n < 3; n++) {
+        const uint32_t x = pack_bf16(v0, v1);
+        w[n][i >> 2][i & 3] = x;
+        v0 -= bf16_lo(x);
+        v1 -= bf16_hi(x);
+      }
+    }
+    // (two sums side by side: a product waits for the one before it in its own sum.  Ragged batch
+    // 48.9 us one after the other, 47.2 so)
+#pragma unroll
+    for (int i0 = 0; i0 < 8; i0 += 2) {
 #pragma unroll
       for (int f = 0; f < 2; f++) {
-        const bf16x8_t vb = to_bf16(t.v[i][2 * f], t.v[i][2 * f + 1]);
-        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, hi[f]),
-                                                         acc[i], 0, 0, 0);
-        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, __builtin_bit_cast(bf16x8_t, lo[f]),
-                                                         acc[i], 0, 0, 0);
+        bf16x8_t vb[2];
+#pragma unroll
+        for (int i = 0; i < 2; i++) vb[i] = to_bf16(t.v[i0 + i][2 * f], t.v[i0 + i][2 * f + 1]);
+#pragma unroll
+        for (int n = 0; n < 3; n++)
+#pragma unroll
+          for (int i = 0; i < 2; i++)
+            acc[i0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                vb[i], __builtin_bit_cast(bf16x8_t, w[n][f]), acc[i0 + i], 0, 0, 0);
       }
     }
   };
@@ -763,8 +774,10 @@ __device__ __forceinline__ void add_waves(WaveSums<WAVES>& sm, Row& r) {
   for (int w = 0; w < WAVES; w++) r.l += sm.l[w][hc];
 }
 
+// (Waves per SIMD: two work-groups of eight waves on a CU take the 128 registers that they
+// would go past; 192 ragged rows of 32 kv-heads 226 us so, 232 with one.)
 template <bool MOBA, int kRowWaves>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void cache_rows_kernel(CacheDecodeArgs a) {
+__global__ __launch_bounds__(64 * kRowWaves, kRowWaves / 2) void cache_rows_kernel(CacheDecodeArgs a) {
   constexpr int kBlocks = kCacheRowBlocks;
   static_assert(kBlocks % 64 == 0 && kDecodeMaxGroup * kBlocks * 8 <= 4 * 8 * 64 * 16,
                 "the scores fit where the sums are joined");

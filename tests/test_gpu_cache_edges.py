@@ -1,0 +1,53 @@
+"""The paged 8-bit cache at the edges of what its calls allow: weights that cancel, NaN in what some
+heads attend, lengths near 2^31, cut-backs, table entries that are no page, and profiling
+of captured calls."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_ref as ref
+from paper_2502_13189_amd import binding
+from test_gpu_cache import DEV, WIDTHS, i32, some_cache, to_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    binding.load()
+
+
+@pytest.mark.parametrize("W", WIDTHS)
+@pytest.mark.parametrize("topk", [0, 2])
+def test_decode_weights_in_full(topk, W):
+    """Two keys whose weighted values all but cancel, out = (a - b p) / (1 + p) with b p near a: what
+    a rounding of the weights to fewer than 24 bits leaves shows in the result.
+
+    In units of u = 2^-24: the logit, at most 0.91 in the log2 domain, is a sum of two exact
+    products (2 u), times the scale (2 u) and rounded (u), so p is off by 5 * 0.91 * ln 2 = 3.2 u, and by
+    4 u from its exponential; the bf16 terms of a weight make it up to u; six MFMAs add, each
+    off by 2 u of the sum so far at most, which is at most a.  Of b p ~ a together less than 21 a u, that is less
+    than 12 u of mass = (a + b p) / (1 + p).  The rounding to bf16 is 2^-8 of the result."""
+    pairs = [(a, b) for a in range(8, 16) for b in range(a + 1, 16)]
+    S = len(pairs)
+    pool = ref.Pool(S, 1, 64)
+    k, v, q = np.zeros((2 * S, 1, 128)), np.zeros((2 * S, 1, 128)), torch.zeros((S, 1, 128), dtype=torch.float64)
+    slots = [s * 64 + i for s in range(S) for i in range(2)]
+    for s, (a, b) in enumerate(pairs):
+        k[2 * s + 1, 0, :2] = -1.0, -1.0 / 64
+        v[2 * s, 0], v[2 * s + 1, 0] = a, -b
+        z = math.log(b / a) * math.sqrt(128.0)
+        q[s, 0, 0] = float(torch.tensor(z).to(torch.bfloat16))
+        q[s, 0, 1] = (z - q[s, 0, 0]) * 64
+    q = q.to(DEV, torch.bfloat16)
+    ref.write(k, v, slots, pool)  # (all of them exact)
+    table = np.full((S, W), -1)
+    table[:, 0] = np.arange(S)
+    out, _ = binding.cache_decode(q, to_gpu(pool), i32(table), i32([2] * S), 64, topk)
+    want, _, mass = ref.decode(q.double().cpu().numpy(), pool, table, [2] * S, 64, topk)[:3]
+    err = np.abs(out.double().cpu().numpy() - want)
+    assert (err <= 12 * 2.0 ** -24 * mass + 2.0 ** -8 * np.abs(want)).all()
