@@ -378,7 +378,8 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  *   common factor), computed in 64 bits, NaN counting as the lowest; the topk - 1 highest (equal
  *   scores: lower block) and the current block are attended.  A topk of at least
  *   ceil(W * page_size / block_size) attends everything and runs as topk == 0.  At most
- *   4096 blocks per table row.
+ *   4096 blocks per table row.  NaN among a block's keys or values reaches no query head that
+ *   does not attend it.
  * S * W pages of page_size / 64 tiles, times Hkv, must be below 2^30, S * Hkv below 2^23.
  * out [S, Hq, 128] bf16 (may be q itself, with its strides; another view of q's memory is
  * MOBA_ERR_LAYOUT), lse [Hq, S] f32.

@@ -51,3 +51,34 @@ def test_decode_weights_in_full(topk, W):
     want, _, mass = ref.decode(q.double().cpu().numpy(), pool, table, [2] * S, 64, topk)[:3]
     err = np.abs(out.double().cpu().numpy() - want)
     assert (err <= 12 * 2.0 ** -24 * mass + 2.0 ** -8 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("W", WIDTHS)
+@pytest.mark.parametrize("hq,hkv,topk", [(4, 1, 2), (8, 2, 3), (16, 1, 4)])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_decode_nan_reaches_only_the_heads_that_attend_it(which, hq, hkv, topk, W):
+    """Every past block has a NaN, which cache_write leaves for what is not finite, in a dim of
+    its own; heads of a group choose different blocks, and each has the NaN of its own alone."""
+    rng = np.random.default_rng(20 + topk)
+    lens = [700, 64, 333]
+    pool, table = some_cache(rng, lens, hkv, 64, W)
+    clean = pool.copy()
+    for s, L in enumerate(lens):
+        for j in range((L - 1) // 64):
+            at = getattr(pool, which)[table[s, j]]  # [Hkv, 64, 128] or [Hkv, 1, 128, 64]
+            if which == "k":
+                at[:, 3 * j, j] = 0x7f
+            else:
+                at[:, 0, j, 3 * j] = 0xff
+    q = torch.from_numpy(rng.standard_normal((3, hq, ref.D))).to(DEV, torch.bfloat16)
+    out, lse = (x.double().cpu().numpy() for x in binding.cache_decode(
+        q, to_gpu(pool), i32(table), i32(lens), 64, topk))
+    nq = q.double().cpu().numpy()
+    want, want_lse = ref.decode(nq, pool, table, lens, 64, topk)[:2]
+    bad, bad_lse = np.isnan(want), np.isnan(want_lse)
+    groups = bad.reshape(3, hkv, hq // hkv, ref.D)
+    assert (groups.any(2) & ~groups.all(2)).any() or which == "k"  # (heads did choose differently)
+    np.testing.assert_array_equal(np.isnan(out), bad)
+    np.testing.assert_array_equal(np.isnan(lse), bad_lse)
+    fine = ref.decode(nq, clean, table, lens, 64, topk)  # (the same but where there is NaN)
+    ref.check_decode(np.where(bad, fine[0], out), np.where(bad_lse, fine[1], lse), fine)
