@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kCacheDecodeThreads, 2) void cache_attend_kernel(Ca
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = a.c.Hkv, G = a.G;
-  const auto units = [&](int s) { return (held(a, s) + kCacheTile - 1) / kCacheTile; };
+  const auto units = [&](int s) { return cache_steps(held(a, s)); };
   sum_rows(sums, a.S, units);
   const int w = blockIdx.x * (kCacheDecodeThreads / 64) + wave;
   // rows that attend nothing
@@ -737,7 +737,7 @@ __device__ __forceinline__ int block_list(const CacheDecodeArgs& a, Kept<NW>& k,
     if (heads) list[k.before[x] + __popcll(any & ((1ull << lane) - 1))] = (uint32_t)(64 * x + lane) | heads << 16;
   }
   if (tid == 0) list[nu] = (uint32_t)past | 0xffff0000u;
-  return nu * (a.B / kCacheTile) + (len - past * a.B + kCacheTile - 1) / kCacheTile;
+  return nu * (a.B / kCacheTile) + cache_steps(len - past * a.B);
 }
 
 // -------------------------------------------------------------------- rows
@@ -812,7 +812,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kRowWaves / 2) void cache_rows_kern
     for (int hl = wave; hl < G; hl += kRowWaves) write_nothing(a, s, g * G + hl, lane);
     return;
   }
-  int steps = (len + kCacheTile - 1) / kCacheTile;
+  int steps = cache_steps(len);
   if constexpr (MOBA) {
     const int past = past_blocks(a, s), nh = min(a.topk - 1, past);
     double* score = reinterpret_cast<double*>(sums.of);  // [G, kBlocks]

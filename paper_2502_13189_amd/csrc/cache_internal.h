@@ -2,11 +2,11 @@
 // side and its kernels.
 #pragma once
 
+#include "cache_rules.h"
 #include "moba_internal.h"
 
 namespace moba {
 
-constexpr int kCacheTile = 64;       // tokens of a V tile, and of a decode step
 constexpr int kCacheMaxPage = 256;   // largest page
 constexpr int kPlanMaxRequests = 4096;
 constexpr int kCacheMinExp = -100, kCacheMaxExp = 119;  // exponents of a page's scale

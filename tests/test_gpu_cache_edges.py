@@ -82,3 +82,53 @@ def test_decode_nan_reaches_only_the_heads_that_attend_it(which, hq, hkv, topk, 
     np.testing.assert_array_equal(np.isnan(lse), bad_lse)
     fine = ref.decode(nq, clean, table, lens, 64, topk)  # (the same but where there is NaN)
     ref.check_decode(np.where(bad, fine[0], out), np.where(bad_lse, fine[1], lse), fine)
+
+
+def far_request(length, where, fill):
+    """A request of `length` tokens in a table row of 2^25 pages of 64, of which only those at
+    `where` are pages of the pool; and the same pages in a row of their own, with its length.
+    fill(page's place in `where`, tokens) gives its keys and values."""
+    n = len(where)
+    pool = ref.Pool(n + 1, 1, 64)
+    near = np.arange(n)[None] + 1
+    table = torch.full((2, 1 << 25), -1, dtype=torch.int32, device=DEV)
+    held = 0
+    for i, j in enumerate(where):
+        m = min(64, length - 64 * j)
+        assert m > 0 and (m == 64 or j == where[-1])
+        table[0, j] = int(near[0, i])
+        ref.write(*fill(i, m), near[0, i] * 64 + np.arange(m), pool)
+        held += m
+    return pool, table, near, held
+
+
+@pytest.mark.parametrize("length", [2 ** 31 - 65, 2 ** 31 - 64, 2 ** 31 - 63, 2 ** 31 - 1])
+def test_decode_lengths_up_to_32_bits(length):
+    """Table rows that hold 2^31 tokens: nearly all of them are left out."""
+    rng = np.random.default_rng(21)
+    where = [0, 7, (1 << 24) + 5, (1 << 25) - 3, (length - 1) // 64]
+    pool, table, near, held = far_request(
+        length, where, lambda i, m: (rng.standard_normal((m, 1, 128)), rng.standard_normal((m, 1, 128))))
+    q = torch.from_numpy(rng.standard_normal((2, 2, 128))).to(DEV, torch.bfloat16)
+    out, lse = binding.cache_decode(q, to_gpu(pool), table, i32([length, 0]), 0, 0)
+    want = ref.decode(q.double().cpu().numpy(), pool, np.concatenate([near, near]), [held, 0], 0, 0)
+    ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("length", [2 ** 31 - 64, 2 ** 31 - 1])
+def test_decode_moba_lengths_up_to_32_bits(length):
+    """2048 blocks of 2^20 tokens: block 3 scores above all others, which are empty but for
+    block 9, which scores below them."""
+    rng = np.random.default_rng(22)
+    per = 1 << 14
+    where = [3 * per + 1, 3 * per + 70, 9 * per, (length - 1) // 64 - 600, (length - 1) // 64]
+
+    def fill(i, m):
+        return (0.5, 0.5, -0.5, 0.5, 0.5)[i] + rng.standard_normal((m, 1, 128)), rng.standard_normal((m, 1, 128))
+
+    pool, table, near, held = far_request(length, where, fill)
+    q = torch.from_numpy(0.3 + 0.1 * rng.standard_normal((2, 2, 128))).to(DEV, torch.bfloat16)
+    out, lse = binding.cache_decode(q, to_gpu(pool), table, i32([length, 0]), 1 << 20, 2)
+    kept = near[:, [0, 1, 3, 4]]
+    want = ref.decode(q.double().cpu().numpy(), pool, np.concatenate([kept, kept]), [held - 64, 0], 0, 0)
+    ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
