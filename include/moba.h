@@ -296,7 +296,8 @@ moba_status moba_route(const moba_tensor* sel, const moba_tensor* cu_seqlens, in
  *   k_scale, v_scale [N, Hkv] f32 contiguous: a page's key is k * k_scale, for all P
  *           tokens of a kv-head
  *   k_sum   [N, Hkv, 128] f32 contiguous: the sum of the page's keys as they are held
- * k and v must be 16-byte aligned with page and head strides that are multiples of 16.
+ * k, v and k_sum must be 16-byte aligned, k and v with page and head strides that are multiples
+ * of 16.
  * The pool's contents need no initialisation: what a page holds past a request's length is
  * never used, whatever its bits.
  */

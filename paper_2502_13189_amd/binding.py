@@ -316,7 +316,8 @@ def route(sel, cu_seqlens, block_size: int, num_kv_heads: int, stream=None):
 class PagedCache(NamedTuple):
     """A pool of N pages of P tokens (64, 128, 192 or 256) in 8 bits, as include/moba.h
     describes it.  Every tensor may be a slice of a larger pool (a layer's) whose page
-    and head strides are multiples of 16 bytes; scales and sums are contiguous."""
+    and head strides are multiples of 16 bytes; scales and sums are contiguous, and k, v and
+    k_sum begin at multiples of 16 bytes."""
     k: torch.Tensor        # [N, Hkv, P, 128] float8_e4m3fn
     v: torch.Tensor        # [N, Hkv, P // 64, 128, 64] float8_e4m3fn, token index innermost
     k_scale: torch.Tensor  # [N, Hkv] fp32: the page's keys are k * k_scale

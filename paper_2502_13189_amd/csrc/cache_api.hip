@@ -52,6 +52,7 @@ moba_status check_cache(const moba_cache* c, CachePool* p) {
   if ((st = check_contig(c->k_scale, MOBA_F32, 2, sums)) != MOBA_OK) return st;
   if ((st = check_contig(c->v_scale, MOBA_F32, 2, sums)) != MOBA_OK) return st;
   if ((st = check_contig(c->k_sum, MOBA_F32, 3, sums)) != MOBA_OK) return st;
+  if ((reinterpret_cast<uintptr_t>(c->k_sum->data) & 15) != 0) return MOBA_ERR_LAYOUT;
   p->k_scale = static_cast<float*>(c->k_scale->data);
   p->v_scale = static_cast<float*>(c->v_scale->data);
   p->k_sum = static_cast<float*>(c->k_sum->data);
