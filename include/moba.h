@@ -332,6 +332,10 @@ typedef struct {
  * list does not hold those of every request up to it that was not refused for the first
  * reason.  A refused request keeps its length, pages and free list untouched; the
  * caller sees it in lens_out, and in slots.
+ * A request is cut back by lowering its length between two steps.  The pages it is taken to hold
+ * are the first ceil(lens[s] / page_size) of its row, so the caller who lowers it past a page's
+ * begin also appends the pages behind the new end to the free list (and raises num_free):
+ * nothing else gives them back.
  * All tensors are contiguous but for the table's row stride.  S <= 4096, S * W and N below
  * 2^31.  Lengths below 0 or above W * page_size count as 0 and W * page_size, a num_free outside [0, N]
  * as the nearer end; pages returned beyond N are dropped.
@@ -362,8 +366,8 @@ moba_status moba_cache_plan(const moba_tensor* add, const moba_tensor* lens, mob
  *   scale = 2^e,  k_sum = the exact sum over tokens 0 .. o + n - 1, rounded once (NaN if
  *           one of the keys is NaN)
  * A power of two costs e4m3 no precision, and rescaling by one none above its subnormals.
- * Writing the same tokens to the same slots again changes nothing; a request may be cut
- * back (lens) and written on from any offset.
+ * Writing the same tokens to the same slots again changes nothing; a request that was cut back
+ * (see moba_cache_plan) is written on from any offset.
  */
 moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const moba_tensor* slots,
                              const moba_cache* cache, hipStream_t stream);

@@ -396,6 +396,8 @@ def cache_plan(add, lens, table, free_pages, num_free, page_size: int, num_token
     int32: tokens held; table [S, W] int32 and free_pages [N] int32 are updated in place (the
     first num_free[0] entries are free); num_tokens: rows of the step's arrays, at least
     the new tokens'.  Requests that do not fit are refused whole (their slots are -1).
+    Who cuts a request back (lowers its length) past a page's begin appends the pages behind
+    its new end to free_pages and raises num_free.
     lens_out and num_free_out may be lens and num_free themselves: a captured step then
     carries its state from replay to replay."""
     status, *out = _cache_call("plan", add, stream, add, lens, table, free_pages, num_free, page_size,

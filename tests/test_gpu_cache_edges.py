@@ -132,3 +132,43 @@ def test_decode_moba_lengths_up_to_32_bits(length):
     kept = near[:, [0, 1, 3, 4]]
     want = ref.decode(q.double().cpu().numpy(), pool, np.concatenate([kept, kept]), [held - 64, 0], 0, 0)
     ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("back", [1, 64, 100, 250])
+def test_cut_back_and_grown_again(back):
+    """A request loses its last tokens, and the pages behind its new end go on the free list; it
+    and another one grow, it is written on and decoded, both end: every page is on the list."""
+    rng = np.random.default_rng(back)
+    N, lens, L = 9, [300, 10], 300 - back
+    pool = ref.Pool(N, 1, 64)
+    cache, table, free = to_gpu(pool), i32(np.full((2, 7), -1)), i32(rng.permutation(N))
+    lens_now, nf = i32([0, 0]), i32([N])
+    w_table, w_free, w_lens, n = np.full((2, 7), -1), free.cpu().numpy().copy(), np.zeros(2, int), N
+
+    def step(add, T=400):
+        nonlocal w_lens, n
+        p = binding.cache_plan(i32(add), lens_now, table, free, nf, 64, T, lens_out=lens_now, num_free_out=nf)
+        cu, slots, w_lens, n, refused = ref.plan(add, w_lens, w_table, w_free, n, 64, T)
+        np.testing.assert_array_equal(p.slots.cpu(), slots)
+        np.testing.assert_array_equal(table.cpu(), w_table)
+        np.testing.assert_array_equal(free.cpu(), w_free)
+        assert int(nf) == n and int(p.refused) == refused == 0
+        k, v = (torch.from_numpy(rng.standard_normal((T, 1, 128))).to(DEV, torch.bfloat16) for _ in range(2))
+        binding.cache_write(k, v, p.slots, cache)
+        ref.write(k.double().cpu().numpy(), v.double().cpu().numpy(), slots, pool)
+
+    step(lens)
+    held, gone = -(-300 // 64), -(-L // 64)
+    lens_now[0] = w_lens[0] = L
+    free[n:n + held - gone] = table[0, gone:held]
+    w_free[n:n + held - gone] = w_table[0, gone:held]
+    n += held - gone
+    nf.fill_(n)
+    step([90, 100])
+    assert n + sum(-(-int(x) // 64) for x in w_lens) == N
+    q = torch.from_numpy(rng.standard_normal((2, 2, 128))).to(DEV, torch.bfloat16)
+    out, lse = binding.cache_decode(q, cache, table, lens_now, 0, 0)
+    want = ref.decode(q.double().cpu().numpy(), pool, w_table, w_lens, 0, 0)
+    ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
+    step([-1, -1])
+    assert n == N and sorted(w_free[:n]) == list(range(N))
