@@ -322,7 +322,8 @@ typedef struct {
  * cu_new   [S + 1] i32, output: exclusive sums of max(add, 0), at most T: request s's new
  *          tokens are rows cu_new[s] .. cu_new[s + 1] - 1 of the step's arrays
  * slots    [T] i64, output: page * page_size + offset of every new token, -1 for those of
- *          refused requests and past the last one
+ *          refused requests and past the last one (where a page, as the table or the free list
+ *          has it, is negative, so are its tokens' slots)
  * refused  [1] i32, output: requests refused
  *
  * The pages of ended requests go back first: they are appended to the free list, request

@@ -72,6 +72,11 @@ __device__ __forceinline__ uint32_t page_of(uint32_t x, int P) {
   const uint32_t t = x / kCacheTile;
   return P == kCacheTile ? t : P == 2 * kCacheTile ? t / 2 : P == 3 * kCacheTile ? t / 3 : t / 4;
 }
+// The slot of a page's token `at`.  Where a table or the free list has a negative entry, a negative
+// one, and not a refused token's -1 (a request's first slot tells the second launch which it is).
+__device__ __forceinline__ int64_t slot_in(int32_t page, int P, uint32_t at) {
+  return (int64_t)page * P + (page >= 0 ? at : 0u);
+}
 // Pages of x tokens (x up to 2^31 - 1).
 __device__ __forceinline__ uint32_t pages_of(uint32_t x, int P) { return page_of(x + P - 1, P); }
 
@@ -224,7 +229,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs 
       for (int x = 0; x < (int)min(tok[i], a.T - my_cu[i]); x++) {
         const uint32_t pos = (uint32_t)len[i] + x, j = page_of(pos, P);
         a.slots[my_cu[i] + x] =
-            granted[i] ? (int64_t)(j < h ? last_page[i] : new_page[i]) * P + (pos - j * P) : -1;
+            granted[i] ? slot_in(j < h ? last_page[i] : new_page[i], P, pos - j * P) : -1;
       }
     }
     if (own_slots)
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(CachePlanArgs 
   const auto slot_of = [&](int s, uint32_t pos) {
     const uint32_t j = page_of(pos, P), h = held(s);
     const int page = j < h ? a.table[s * a.t_ss + j] : a.free_pages[avail - 1 - (pre[s] + (int64_t)(j - h))];
-    return (int64_t)page * P + (pos - j * P);
+    return slot_in(page, P, pos - j * P);
   };
   if (own_pages)
     each_item(pre, S, (uint32_t)take, [&](uint32_t i, int) { return a.free_pages[avail - 1 - i]; },
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
     if (r < a.S) {
       const int c = a.cu[r];
       const uint32_t now = (uint32_t)a.lens_out[r], tok = (uint32_t)max(a.add[r], 0);
-      if (c < a.cu[r + 1] && a.slots[c] >= 0) need = pages_of(now, P) - pages_of(now - tok, P);
+      if (c < a.cu[r + 1] && a.slots[c] != -1) need = pages_of(now, P) - pages_of(now - tok, P);
     }
     const int64_t upto = group_scan(need, part);
     before[r] = (int32_t)(upto - need);
@@ -319,11 +324,11 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
     } else {
       page = *at;
     }
-    return (int64_t)page * P + (pos - j * P);
+    return slot_in(page, P, pos - j * P);
   };
   if (lo == hi && w0 + 64 * kSlotPer <= all) {  // one request's, as in a long prompt
     const int r = __builtin_amdgcn_readfirstlane(lo), begin = a.cu[r];
-    const bool ok = a.slots[begin] >= 0;
+    const bool ok = a.slots[begin] != -1;
     const uint32_t old = (uint32_t)(a.lens_out[r] - a.add[r]);
     const uint32_t pos0 = old + (uint32_t)(w0 - begin) + lane, h = pages_of(old, P);
     int64_t slot[kSlotPer];
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(kSlotThreads) void cache_slots_kernel(CachePlanArgs
         while (s + 1 < a.S && a.cu[s + 1] <= x) s++;
         c0 = a.cu[s];
         end = a.cu[s + 1];
-        granted = a.slots[c0] >= 0;
+        granted = a.slots[c0] != -1;
         old = (int64_t)a.lens_out[s] - a.add[s];
         if (granted) h = pages_of((uint32_t)old, P);
       }

@@ -172,3 +172,28 @@ def test_cut_back_and_grown_again(back):
     ref.check_decode(out.double().cpu().numpy(), lse.double().cpu().numpy(), want)
     step([-1, -1])
     assert n == N and sorted(w_free[:n]) == list(range(N))
+
+
+@pytest.mark.parametrize("scale", [1, 100, 2000, 10000])
+@pytest.mark.parametrize("entry", [-1, -3])
+def test_plan_of_a_request_whose_last_page_is_none(entry, scale):
+    """A held table entry that is negative gives its tokens negative slots; the other requests,
+    and the pages that this one takes, are as they would be.  Short steps, and steps whose
+    slots, and whose pages, a second launch writes."""
+    lens, add = [63, 127, 64, 0], [min(4, scale) if scale < 100 else 4 * scale, 3 * scale, scale, 2]
+    N, T = sum(add) // 64 + 12, sum(add) + 5
+    table = np.full((4, 700), -9)
+    table[0, 0], table[1, :2], table[2, 0] = 0, (1, entry), 2
+    rng = np.random.default_rng(scale)
+    free = np.concatenate([rng.permutation(np.arange(3, N)), [0, 1, 2]])
+    g_table, g_free = i32(table), i32(free)
+    p = binding.cache_plan(i32(add), i32(lens), g_table, g_free, i32([N - 3]), 64, T)
+    cu, slots, new, n, refused = ref.plan(add, lens, table, free, N - 3, 64, T)
+    assert refused == 0 and (slots[cu[1]] < 0) and (slots[cu[1] + 1:cu[-1]] >= 0).all()
+    got = p.slots.cpu().numpy()
+    np.testing.assert_array_equal(np.maximum(got, -1), np.maximum(slots, -1))
+    np.testing.assert_array_equal(p.cu_new.cpu(), cu)
+    np.testing.assert_array_equal(p.lens.cpu(), new)
+    assert int(p.num_free) == n and int(p.refused) == 0
+    np.testing.assert_array_equal(g_table.cpu(), table)
+    np.testing.assert_array_equal(g_free.cpu(), free)
