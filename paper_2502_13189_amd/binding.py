@@ -418,9 +418,10 @@ def cache_decode_workspace_bytes(num_requests: int, table_width: int, num_q_head
                                  num_kv_heads: int, page_size: int, block_size: int,
                                  topk: int) -> int:
     """Bytes of cache_decode()'s workspace (0: such a call would be refused)."""
+    # (what does not fit 32 bits is refused for its value; ctypes would cut it off)
     return int(load().moba_cache_decode_workspace_bytes(
-        int(num_requests), int(table_width), int(num_q_heads), int(num_kv_heads), int(page_size),
-        int(block_size), int(topk)))
+        *(max(-1, min(int(x), 2 ** 31 - 1))
+          for x in (num_requests, table_width, num_q_heads, num_kv_heads, page_size, block_size, topk))))
 
 
 def cache_decode(q, cache: PagedCache, table, lens, block_size: int, topk: int, out=None, lse=None,
