@@ -468,7 +468,8 @@ const char* moba_status_string(moba_status status);
 
 /*
  * Per-phase timing.  While enabled, every entry point records HIP events
- * around each phase on the caller's stream.  moba_profile_read waits for the
+ * around each phase on the caller's stream (but not while a graph captures that
+ * stream: replays are not timed).  moba_profile_read waits for the
  * recorded events, writes up to max_phases entries and resets the counters;
  * it returns the number of phases written.
  */

@@ -27,6 +27,10 @@ struct Phase {
   bool on = false;
   Phase(const char* name, hipStream_t s) : st(s) {
     if (!g_prof || !name) return;
+    // (an event recorded into a graph has no time; asking for it is an error, which the next
+    // launch would be told of)
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (s && (hipStreamIsCapturing(s, &capture) != hipSuccess || capture != hipStreamCaptureStatusNone)) return;
     rec.name = name;
     if (hipEventCreate(&rec.a) != hipSuccess) return;
     if (hipEventCreate(&rec.b) != hipSuccess) { (void)hipEventDestroy(rec.a); return; }

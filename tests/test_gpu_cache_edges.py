@@ -197,3 +197,33 @@ def test_plan_of_a_request_whose_last_page_is_none(entry, scale):
     assert int(p.num_free) == n and int(p.refused) == 0
     np.testing.assert_array_equal(g_table.cpu(), table)
     np.testing.assert_array_equal(g_free.cpu(), free)
+
+
+def test_profiling_leaves_captured_calls_out():
+    """A captured step while phases are timed: eager calls are counted, replays are not, and the
+    calls after the count is read go on as before."""
+    rng = np.random.default_rng(23)
+    lens = [700, 64]
+    pool, table = some_cache(rng, lens, 1, 64, 400)
+    cache, t, ln = to_gpu(pool), i32(table), i32(lens)
+    q = torch.randn((2, 4, 128), device=DEV).to(torch.bfloat16)
+    want = binding.cache_decode(q, cache, t, ln, 64, 2)
+    torch.cuda.synchronize()
+    binding.profile_read()
+    binding.profile_enable(True)
+    try:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = binding.cache_decode(q, cache, t, ln, 64, 2)
+        for _ in range(3):
+            got[0].zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        binding.cache_decode(q, cache, t, ln, 64, 2)
+        phases = binding.profile_read()
+        assert {k: n for k, (n, _) in phases.items()} == {"cache_gate": 1, "cache_attend": 1, "cache_join": 1}
+    finally:
+        binding.profile_enable(False)
+    again = binding.cache_decode(q, cache, t, ln, 64, 2)
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])
