@@ -331,7 +331,8 @@ typedef struct {
  * from the list's end, request by request.  A request is refused, as a whole, where its
  * pages would not fit its table row or its tokens would end past T; or where it needs pages and the
  * list does not hold those of every request up to it that was not refused for the first
- * reason.  A refused request keeps its length, pages and free list untouched; the
+ * reason.  (A request that gets no token counts as refused, too, where those of the requests
+ * before it end past T.)  A refused request keeps its length, pages and free list untouched; the
  * caller sees it in lens_out, and in slots.
  * A request is cut back by lowering its length between two steps.  The pages it is taken to hold
  * are the first ceil(lens[s] / page_size) of its row, so the caller who lowers it past a page's
@@ -394,7 +395,8 @@ moba_status moba_cache_write(const moba_tensor* k, const moba_tensor* v, const m
  * are left out as if masked (their page's k_sum counts as 0).  Hq / Hkv must not exceed 16.
  * workspace: moba_cache_decode_workspace_bytes of device memory, 16-byte aligned; it needs no
  * initialisation and nothing is kept in it after the call.  fp32 softmax and sums; the keys, the
- * queries, the values and the weights (as three bf16 terms) enter the matrix cores exactly.
+ * queries and the values enter the matrix cores exactly, the weights with all 24 bits (as
+ * three bf16 terms).
  * Results do not depend on timing; a request's split over work-groups, and with it its
  * rounding, depends on the whole batch.
  */

@@ -105,12 +105,12 @@ size_t decode_layout(const DecodeShape& d, char* base, CacheDecodeArgs* a) {
 // step, so a row's most (what its table row can hold, MoBA: select) is held against what
 // the other way takes: its launches, while there is little to do, and the batch's share
 // of the chip where there is much.  Whole calls, split and by rows, all rows full:
-//   full  64 tokens .. 1024, up to 128 rows        10.5 .. 13.3 and 7.6 .. 10.5 us
-//         2048: 16 rows 12.2, 15.2; 128 rows 18.4, 16.4 (ragged 12.7, 13.7); 2048 rows 188, 183
-//         4096: 16 rows 13.4, 25.5; 512 rows 98, 93 (ragged 28, 34); 8192: 512 rows 184, 181
-//   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 16.0, 18.0 (ragged 12.2, 8.1), 64 rows 19.3,
-//         19.6; 4096: 128 rows 29.9, 28.7, 2048 rows 271, 253; 8192: 128 rows 33.6, 33.8 (ragged
-//         23.3, 27.3), 512 rows 94, 90
+//   full  64 tokens .. 1024, up to 128 rows        11.1 .. 13.5 and 7.4 .. 11.3 us
+//         2048: 16 rows 11.6, 16.0; 128 rows 18.6, 17.6 (ragged 12.5, 15.0); 2048 rows 187, 183
+//         4096: 16 rows 13.0, 26.1; 512 rows 99, 94 (ragged 28, 35); 8192: 512 rows 185, 182
+//   MoBA (256, top-4: up to 52 steps)  2048: 2 rows 16.4, 18.7 (ragged 13.4, 7.7), 64 rows 19.8,
+//         20.8; 4096: 128 rows 30.1, 31.0, 2048 rows 272, 255; 8192: 128 rows 34.6, 36.2 (ragged
+//         23.7, 28.9), 512 rows 95, 91
 bool rows_in_one(const DecodeShape& d) {
   const int64_t rows = d.S * d.Hkv, held = d.W * (d.P / kCacheTile);
   if (d.full) return held <= std::min<int64_t>(std::max<int64_t>(rows / 4, 16), 64);
@@ -119,10 +119,11 @@ bool rows_in_one(const DecodeShape& d) {
   return d.most + d.W / 32 <= std::min<int64_t>(std::max<int64_t>(rows / 3, 34), 256);
 }
 
-// MoBA: work-groups for a (request, kv-head), whose waves have a step or more.  (256, 512, 768,
-// 1024 work-groups: 8 ragged requests 44.2, 44.1, 47.1, 49.3 us, 32 x 65536 tokens 180, 184, 187,
-// 187, ragged 91, 64, 70, 61.  At most 64, 256, 1024 steps: 64 ragged requests of up to 32768
-// tokens 77, 88, 89 us, all full 196, 189, 190.)
+// MoBA: work-groups for a (request, kv-head), whose waves have a step or more.  (Blocks of
+// 1024, top-4; 256, 512, 768, 1024 work-groups: 8 ragged requests 42.4, 42.2, 42.7, 45.5 us, 32 x
+// 65536 tokens 181, 186, 189, 185, ragged 103, 69, 71, 62; 1M tokens, blocks of 4096, top-12, 84.2,
+// 84.9, 87.4, 90.9.  At most 64, 256, 1024 steps: 64 requests of 32768 tokens 310, 312, 312, ragged
+// 107, 148, 148: a batch of this kind alone would be better off with 64.)
 int parts_of(int64_t rows, int64_t most) {
   if (rows == 0 || rows >= int64_t(1) << 19) return 1;  // (as far as the grids go)
   const int64_t n = std::max(ceil_div(kCachePartGroups, rows), ceil_div(most, kCachePartSteps));

@@ -21,9 +21,10 @@
 //           page's token-minor tile.  e4m3 is exact in bf16; the weights enter as three
 //           bf16 terms, which hold their 24 bits (in two, 17 bits, whole calls over 1M tokens take
 //           355.4 us, so 355.8; a ragged batch 46.0 and 47.2), the scales through the logits and the
-//           weights.  1M tokens, 32/8 heads: 2.15 GB in 345 us, 6.2
-//           TB/s, what bare loads reach; more loads in flight (next keys or whole steps
-//           ahead) or more waves gain nothing.
+//           weights.  1M tokens, 32/8 heads: 2.15 GB, 354 us a call in
+//           a row with the join (6.1 TB/s, bare loads reach 6.2), 349 us the launch at
+//           best; more loads in flight (next keys or whole steps ahead) or more waves gain
+//           nothing.
 //   gate    MoBA: a wave adds a block's k_sum rows and takes its scores with the group's
 //           heads, in 64 bits
 //   parts   MoBA: a wave finds the (k-1)-th highest score of a head bit by bit; the group's
@@ -916,8 +917,8 @@ hipError_t launch_cache_rows(bool full, const CacheDecodeArgs& a, hipStream_t st
   const unsigned groups = (unsigned)(a.S * a.c.Hkv);
   // Eight waves finish a row sooner (its gate and selection above all); where there are rows
   // for four work-groups of four waves on every CU, the shorter ones run on past the longer:
-  // 6144 rows of 16 .. 512 tokens 70 -> 49 us, 2048 rows of 16 .. 1024 37 -> 31, MoBA 16 .. 4096 84
-  // -> 80; all rows equal, or up to 4096 tokens with full attention: 2% slower.
+  // 6144 rows of 16 .. 512 tokens 73 -> 54 us, 2048 rows of 16 .. 1024 39 -> 32, MoBA 16 .. 4096 88
+  // -> 82; all rows equal, or up to 4096 tokens with full attention: 2 to 4% slower.
   const bool four = groups >= 512 && (!full || a.W * a.c.P <= 2048);
   if (full && four) cache_rows_kernel<false, 4><<<groups, 64 * 4, 0, st>>>(a);
   else if (full) cache_rows_kernel<false, 8><<<groups, 64 * 8, 0, st>>>(a);

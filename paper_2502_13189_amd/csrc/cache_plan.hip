@@ -10,7 +10,7 @@
 // kPlanOwnPages, the tables' new pages, where its work-groups have a thread for every request.
 //
 // Measured: 64 requests, one token each, two ending: 5.0 us (a launch that does nothing takes
-// about 3); 1M tokens of 8 prompts into 16384 pages: 5.9 us, and 8.6 for their slots and
+// about 3); 1M tokens of 8 prompts into 16384 pages: 5.7 us, and 8.8 for their slots and
 // pages (with the pages in the first launch, 12.4 and 6.1).
 #include "cache_internal.h"
 

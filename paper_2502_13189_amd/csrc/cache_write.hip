@@ -16,9 +16,9 @@
 // such a run is read again and rounded value by value.  A run of one token, a request's in a
 // decode step, is one wave's, several in a work-group side by side.
 //
-// Measured: 117017 tokens of ragged prompts, 8 kv-heads, bf16, pages of 128 (724 MB): 150
-// us, 4.8 TB/s, the rate of a large copy (with the elements held, measured and rounded as
-// floats, one by one, 347).  One token for each of 62 requests: 6 us; of 1024: 28 (as whole
+// Measured: 117017 tokens of ragged prompts, 8 kv-heads, bf16, pages of 128 (724 MB): 149
+// us a call in a row, 4.8 TB/s, the rate of a large copy (with the elements held, measured and rounded as
+// floats, one by one, 347).  One token for each of 62 requests: 7 us; of 1024: 28 (as whole
 // work-groups' runs 40), with pages of 256 28 too (196).  A wave per tile, V turned over in
 // registers alone, was slower but for pages of 256.
 #include "cache_internal.h"
