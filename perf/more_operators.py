@@ -191,7 +191,7 @@ def _prepare_attn(case, gen):
     lens, H = _ints(case["lens"]), case["heads"]
     T = sum(lens)
     bf = torch.bfloat16
-    st = {"op": case["op"], "lens": lens, "cu": _cu(lens)}
+    st = {"op": case["op"], "longest": max(lens), "cu": _cu(lens)}
     st["q"] = torch.randn((T, H, QK), generator=gen, device=DEV).to(bf)
     # keys and values of a head stand together, as one projection of the latent vector gives them
     kv = torch.randn((T, H, NOPE + VDIM), generator=gen, device=DEV).to(bf)
@@ -271,35 +271,50 @@ def _plain_rope(st):
     return {n: _turn(st[n], st["pos"], st["freqs"], st["amplitude"], st["pairs"], sign) for n in ("q", "k")}
 
 
-def _scores(st, h, a, b):
-    """Scaled scores [b - a, b - a] of head h among tokens a .. b - 1, the future masked, and
-    that head's queries and keys in 32 bits."""
-    q = st["q"][a:b, h].float()
-    k = torch.cat([st["k"][a:b, h], st["kr"][a:b]], 1).float()
-    z = torch.matmul(q, k.t()) * SCALE
-    n = torch.arange(b - a, device=DEV)
+def _rows(st):
+    """Token of every place [S, longest] of the padded batch, and whether it is one."""
+    cu = st["cu"].long()
+    at = torch.arange(st["longest"], device=DEV)
+    ok = at < (cu[1:] - cu[:-1])[:, None]
+    return torch.where(ok, cu[:-1, None] + at, 0), ok
+
+
+def _chunks(S, H, n):
+    """(sequences, heads) whose scores are taken at once."""
+    heads = max(1, min(H, (1 << 31) // (n * n)))
+    seqs = max(1, min(S, (1 << 31) // (n * n * heads)))
+    return [(slice(s, s + seqs), slice(h, h + heads)) for s in range(0, S, seqs) for h in range(0, H, heads)]
+
+
+def _padded(x, row, heads):
+    """x [T, H, D] -> [S, heads, longest, D] in 32 bits."""
+    return x[row][:, :, heads].transpose(1, 2).float().contiguous()
+
+
+def _scores(st, row, heads):
+    """Scaled scores [S, heads, n, n], the future masked, and the queries and keys in 32 bits."""
+    q = _padded(st["q"], row, heads)
+    k = _padded(st["k"], row, heads)
+    k = torch.cat([k, _padded(st["kr"][:, None], row, slice(0, 1)).expand(-1, k.shape[1], -1, -1)], 3)
+    z = torch.matmul(q, k.transpose(2, 3).contiguous()).mul_(SCALE)
+    n = torch.arange(row.shape[1], device=DEV)
     return z.masked_fill_(n > n[:, None], -math.inf), q, k
-
-
-def _spans(lens):
-    at = 0
-    for n in lens:
-        yield at, at + n
-        at += n
 
 
 def _plain_prefill(st):
     T, H = st["q"].shape[:2]
     out = torch.empty((T, H, VDIM), dtype=torch.bfloat16, device=DEV)
     lse = torch.empty((H, T), device=DEV)
-    for a, b in _spans(st["lens"]):
-        for h in range(H):
-            z, _, _ = _scores(st, h, a, b)
-            m = z.amax(1, keepdim=True)
-            p = z.sub_(m).exp_()
-            l = p.sum(1, keepdim=True)
-            out[a:b, h] = (torch.matmul(p, st["v"][a:b, h].float()) / l).to(torch.bfloat16)
-            lse[h, a:b] = (l.log() + m)[:, 0]
+    row, ok = _rows(st)
+    for s, h in _chunks(row.shape[0], H, row.shape[1]):
+        z, _, _ = _scores(st, row[s], h)
+        m = z.amax(3, keepdim=True)
+        p = z.sub_(m).exp_()
+        l = p.sum(3, keepdim=True)
+        o = torch.matmul(p, _padded(st["v"], row[s], h)) / l
+        r = row[s][ok[s]]
+        out[r, h] = o.transpose(1, 2)[ok[s]].to(torch.bfloat16)
+        lse[h, r] = (l.log() + m)[..., 0].transpose(1, 2)[ok[s]].t()
     return {"out": out, "lse": lse}
 
 
@@ -310,19 +325,20 @@ def _plain_grad(st):
     dk = torch.empty((T, H, NOPE), dtype=bf, device=DEV)
     dv = torch.empty((T, H, VDIM), dtype=bf, device=DEV)
     dkr = torch.zeros((T, ROPE), device=DEV)
-    for a, b in _spans(st["lens"]):
-        for h in range(H):
-            z, q, k = _scores(st, h, a, b)
-            p = z.sub_(st["lse"][h, a:b, None]).exp_()
-            do = st["dout"][a:b, h].float()
-            dv[a:b, h] = torch.matmul(p.t(), do).to(bf)
-            dp = torch.matmul(do, st["v"][a:b, h].float().t())
-            delta = (p * dp).sum(1, keepdim=True)
-            ds = dp.sub_(delta).mul_(p).mul_(SCALE)
-            dq[a:b, h] = torch.matmul(ds, k).to(bf)
-            g = torch.matmul(ds.t(), q)
-            dk[a:b, h] = g[:, :NOPE].to(bf)
-            dkr[a:b] += g[:, NOPE:]
+    row, ok = _rows(st)
+    for s, h in _chunks(row.shape[0], H, row.shape[1]):
+        z, q, k = _scores(st, row[s], h)
+        p = z.sub_(st["lse"][h][:, row[s]].transpose(0, 1)[..., None]).exp_()
+        p *= ok[s][:, None, :, None]  # places that are no tokens have no gradient
+        do = _padded(st["dout"], row[s], h)
+        r = row[s][ok[s]]
+        dv[r, h] = torch.matmul(p.transpose(2, 3).contiguous(), do).transpose(1, 2)[ok[s]].to(bf)
+        dp = torch.matmul(do, _padded(st["v"], row[s], h).transpose(2, 3).contiguous())
+        ds = dp.sub_((p * dp).sum(3, keepdim=True)).mul_(p).mul_(SCALE)
+        dq[r, h] = torch.matmul(ds, k).transpose(1, 2)[ok[s]].to(bf)
+        g = torch.matmul(ds.transpose(2, 3).contiguous(), q).transpose(1, 2)[ok[s]]
+        dk[r, h] = g[..., :NOPE].to(bf)
+        dkr[r] += g[..., NOPE:].sum(1)
     return {"dq": dq, "dk": dk, "dkr": dkr.to(bf), "dv": dv}
 
 
