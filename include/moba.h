@@ -67,8 +67,8 @@ extern "C" {
 #endif
 
 /* MOBA_F8E4M3: 8-bit floats, 4 exponent and 3 mantissa bits, largest 448, no infinities
- * (only in the paged cache) */
-typedef enum { MOBA_F32 = 0, MOBA_BF16 = 1, MOBA_I32 = 2, MOBA_I64 = 3, MOBA_F8E4M3 = 4 } moba_dtype;
+ * (only in the paged cache); MOBA_F64: only the frequencies of rotary positions */
+typedef enum { MOBA_F32 = 0, MOBA_BF16 = 1, MOBA_I32 = 2, MOBA_I64 = 3, MOBA_F8E4M3 = 4, MOBA_F64 = 5 } moba_dtype;
 
 typedef struct {
   void* data;        /* host or device pointer, see each argument */
@@ -411,6 +411,125 @@ moba_status moba_cache_decode(const moba_tensor* q, const moba_cache* cache,
  */
 size_t moba_cache_decode_workspace_bytes(int64_t S, int64_t W, int32_t Hq, int32_t Hkv,
                                          int32_t page_size, int32_t block_size, int32_t topk);
+
+/*
+ * Rotary positions
+ * ----------------
+ * Pair i of a head, x and y, at position p becomes
+ *   x' = amplitude (x cos(p f_i) - y sin(p f_i)),  y' = amplitude (x sin(p f_i) + y cos(p f_i)).
+ * The R / 2 pairs are dims (i, i + R / 2) of the head's first R dims, or, interleaved, (2 i, 2 i + 1); dims
+ * from R on are copied.  To turn the last dims of wider heads, pass views of them.
+ *
+ *   freqs   [R / 2] f64 contiguous: radians a position, scaled for longer contexts as the caller
+ *           wants it.  Angles are formed in 64-bit integers (a fraction of a turn): exact to 2^-53 of a
+ *           frequency at any position, of either sign
+ *   pos     [T] i32 or i64 contiguous: the rows' positions; or NULL, with
+ *   cu_seqlens [S + 1] i32 contiguous, DEVICE memory, non-decreasing: row t of sequence s stands at
+ *           position start[s] + t - cu_seqlens[s]; rows outside [cu_seqlens[0], cu_seqlens[S]) are left as they are
+ *   start   [S] i32 contiguous, or NULL: every sequence begins at position 0
+ */
+typedef struct {
+  const moba_tensor* freqs;
+  const moba_tensor* pos;
+  const moba_tensor* cu_seqlens;
+  const moba_tensor* start;
+  float amplitude;
+  int32_t interleaved;
+} moba_rotation;
+
+/*
+ * q [T, Hq, D], k [T, Hk, D] (with k_out, or both NULL) bf16 or f32 (the same), last dim contiguous, any
+ * token and head stride, any D from 2 to 4096; q_out, k_out of the same shapes and dtype, may be q and k
+ * themselves (with their strides), but share no memory with them otherwise (MOBA_ERR_LAYOUT).  One
+ * launch; products in fp32, rounded once.  Nothing is read back or allocated: calls can be
+ * captured, and overlap on different streams.
+ */
+moba_status moba_rope(const moba_tensor* q, const moba_tensor* k, const moba_rotation* rot,
+                      moba_tensor* q_out, moba_tensor* k_out, hipStream_t stream);
+
+/* The gradients of moba_rope w.r.t. q and k from those w.r.t. q_out and k_out: the same with -p. */
+moba_status moba_rope_backward(const moba_tensor* dq_out, const moba_tensor* dk_out,
+                               const moba_rotation* rot, moba_tensor* dq, moba_tensor* dk,
+                               hipStream_t stream);
+
+/*
+ * Latent attention
+ * ----------------
+ * Keys and values of all heads come from one latent vector c of 512 numbers a token, and one rotary
+ * key of 64.  Two forms:
+ * expanded (prefill, training): the caller has projected c to each head's k and v.
+ *   q      [T, H, 192] bf16: a head's 128 dims without position, then its 64 rotary ones
+ *   k, v   [T, H, 128] bf16;  k_rope [T, 64] bf16: the rotary key, shared by all heads
+ *   scores scale (<q[0:128], k> + <q[128:192], k_rope>), causal in each sequence
+ * absorbed (decode): the projections are folded into the query, which scores c itself.
+ *   q_c    [S, H, 512], q_rope [S, H, 64] bf16
+ *   scores scale (<q_c, c> + <q_rope, k_rope>);  out [S, H, 512] bf16 = sum of weights times c
+ * Rotary positions are applied beforehand (moba_rope; moba_latent_write applies the key's).
+ *
+ * Last dims contiguous, rows 16-byte aligned, any token and head stride (token strides below 2^24
+ * elements).  scale is positive and finite (1 / sqrt(192) is usual).  cu_seqlens [S + 1] i32 contiguous
+ * is in DEVICE memory, non-decreasing and within [0, T]: nothing is read back, and a padded batch keeps
+ * its rows outside [cu_seqlens[0], cu_seqlens[S]) as they are, in all outputs.  T * H < 2^28.
+ * Nothing is allocated or kept between calls: calls can be captured into HIP graphs, and calls that share no
+ * memory (workspaces included) may overlap on different streams.  None of the tensors a call writes may overlap
+ * another of its tensors.  Results do not depend on timing.
+ */
+
+/*
+ * Causal latent attention, expanded.  out [T, H, 128] bf16, lse [H, T] f32 (natural log).  fp32 softmax
+ * and sums; the weights enter the matrix cores as bf16.  A value that is not finite reaches the rows that
+ * attend it and no others.
+ */
+moba_status moba_latent_forward(const moba_tensor* q, const moba_tensor* k, const moba_tensor* k_rope,
+                                const moba_tensor* v, const moba_tensor* cu_seqlens, float scale,
+                                moba_tensor* out, moba_tensor* lse, hipStream_t stream);
+
+/*
+ * Its gradients.  out, lse: moba_latent_forward's results for these inputs; dout [T, H, 128].  dq [T, H,
+ * 192], dk, dv [T, H, 128], dk_rope [T, 64] (the sum over the heads, in their order) are overwritten.
+ * Weights and score gradients enter the second products as bf16, all sums are fp32, no atomics.
+ * workspace: moba_latent_backward_workspace_bytes of device memory, 16-byte aligned, uninitialised.
+ * Inputs are finite: a value that is not may reach any gradient of its own sequence (no other's but
+ * through nothing: sequences share no sums).
+ */
+moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, const moba_tensor* k_rope,
+                                 const moba_tensor* v, const moba_tensor* cu_seqlens, float scale,
+                                 const moba_tensor* out, const moba_tensor* lse, const moba_tensor* dout,
+                                 moba_tensor* dq, moba_tensor* dk, moba_tensor* dk_rope, moba_tensor* dv,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* 0: such a call would be refused (or has no tokens). */
+size_t moba_latent_backward_workspace_bytes(int64_t T, int32_t num_heads);
+
+/*
+ * Writes new latent vectors and rotary keys into their slots of a paged cache.
+ * pages  [N, P, 576] bf16, P 64, 128, 192 or 256, a page's rows contiguous, any page stride that is a
+ *        multiple of 8: a token's row is c, then k_rope.  Uninitialised pages are fine
+ * c [T, 512], k_rope [T, 64] bf16, any token stride; slots [T] i64 contiguous as moba_cache_plan
+ *        writes them: page * P + offset; a token whose slot is negative or not of the pool is left
+ *        out.  No slot may come twice
+ * rot    NULL: k_rope is stored as it is; else it is turned first (R = 64), and rounded once
+ */
+moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, const moba_tensor* slots,
+                              const moba_rotation* rot, moba_tensor* pages, hipStream_t stream);
+
+/*
+ * Latent attention of one new query per request over the paged cache, absorbed.
+ * table [S, W] i32 (rows contiguous, any row stride), lens [S] i32, as for moba_cache_decode: a request
+ * with lens[s] <= 0 gets out 0 and lse -inf; lens[s] above W * P counts as W * P; tokens of a table
+ * entry outside [0, N) are left out as if masked.  H <= 4096, S * H < 2^24, S * W * P / 64 < 2^30.
+ * out [S, H, 512] bf16, lse [H, S] f32.  What pages hold past a request's length is never used, whatever
+ * its bits.  fp32 softmax and sums; the weights enter the matrix cores as bf16.  A request's
+ * split over work-groups, and with it its rounding, depends on the whole batch.
+ * workspace: moba_latent_decode_workspace_bytes of device memory, 16-byte aligned, uninitialised.
+ */
+moba_status moba_latent_decode(const moba_tensor* q_c, const moba_tensor* q_rope, const moba_tensor* pages,
+                               const moba_tensor* table, const moba_tensor* lens, float scale,
+                               moba_tensor* out, moba_tensor* lse, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+
+/* 0: such a call would be refused (or S == 0).  Host-only arithmetic. */
+size_t moba_latent_decode_workspace_bytes(int64_t S, int64_t W, int32_t num_heads, int32_t page_size);
 
 /*
  * Workspace sizing query: the device workspace bytes moba_forward needs to

@@ -9,6 +9,7 @@ raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import NamedTuple
 
@@ -17,7 +18,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoba.so")
 
-MOBA_F32, MOBA_BF16, MOBA_I32, MOBA_I64, MOBA_F8E4M3 = 0, 1, 2, 3, 4
+MOBA_F32, MOBA_BF16, MOBA_I32, MOBA_I64, MOBA_F8E4M3, MOBA_F64 = 0, 1, 2, 3, 4, 5
 _DT = {torch.float32: MOBA_F32, torch.bfloat16: MOBA_BF16, torch.int32: MOBA_I32,
        torch.int64: MOBA_I64, torch.float8_e4m3fn: MOBA_F8E4M3}
 
@@ -78,12 +79,22 @@ def load() -> ctypes.CDLL:
         "moba_cache_plan": [vp] * 5 + [i32] + [vp] * 6,
         "moba_cache_write": [vp] * 5,
         "moba_cache_decode": [vp] * 4 + [i32, i32] + [vp] * 3 + [ctypes.c_size_t, vp],
+        "moba_rope": [vp] * 6,
+        "moba_rope_backward": [vp] * 6,
+        "moba_latent_forward": [vp] * 5 + [ctypes.c_float] + [vp] * 3,
+        "moba_latent_backward": [vp] * 5 + [ctypes.c_float] + [vp] * 8 + [ctypes.c_size_t, vp],
+        "moba_latent_write": [vp] * 6,
+        "moba_latent_decode": [vp] * 5 + [ctypes.c_float] + [vp] * 3 + [ctypes.c_size_t, vp],
     }.items():
         f = getattr(lib, name)
         f.argtypes = args
         f.restype = ctypes.c_int
     lib.moba_cache_decode_workspace_bytes.restype = ctypes.c_size_t
     lib.moba_cache_decode_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32, i32]
+    lib.moba_latent_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.moba_latent_backward_workspace_bytes.argtypes = [i64, i32]
+    lib.moba_latent_decode_workspace_bytes.restype = ctypes.c_size_t
+    lib.moba_latent_decode_workspace_bytes.argtypes = [i64, i64, i32, i32]
     lib.moba_workspace_bytes.restype = ctypes.c_size_t
     lib.moba_workspace_bytes.argtypes = [i64, i32, i32, i32, i64, i32]
     lib.moba_workspace_held_bytes.restype = ctypes.c_size_t
@@ -335,6 +346,7 @@ class CachePlan(NamedTuple):
 
 
 _cache_ext = None
+_latent_ext = None
 
 
 def _cache_module():
@@ -352,14 +364,37 @@ def _cache_module():
     return _cache_ext
 
 
+def _latent_module():
+    """The marshalling of rotary positions' and latent attention's calls
+    (csrc/latent_binding.cpp).  Raises if it has not been built."""
+    global _latent_ext
+    if _latent_ext is None:
+        load()
+        try:
+            from . import _latent_binding
+        except ImportError as e:
+            raise RuntimeError("_latent_binding.so does not load; build it with "
+                               "`python -m paper_2502_13189_amd.build`") from e
+        _latent_ext = _latent_binding
+    return _latent_ext
+
+
 def _cache_call(fn: str, t: torch.Tensor, stream, *args):
-    """_cache_binding's fn on `stream` or the current stream of t's device, which is made current.
+    return _call(getattr(_cache_ext or _cache_module(), fn), "the paged cache's", t, stream, *args)
+
+
+def _latent_call(fn: str, t: torch.Tensor, stream, *args):
+    return _call(getattr(_latent_ext or _latent_module(), fn), "rotary positions' and latent attention's", t,
+                 stream, *args)
+
+
+def _call(f, owner: str, t: torch.Tensor, stream, *args):
+    """A module's f on `stream` or the current stream of t's device, which is made current.
     What the call allocates is allocated for that stream, so that memory it drops is not
     given out again before the call is done with it."""
-    f = getattr(_cache_ext or _cache_module(), fn)
     device = t.get_device()
     if device < 0:
-        raise ValueError("the paged cache's tensors live on a GPU")
+        raise ValueError("%s tensors live on a GPU" % owner)
     if stream is not None:
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
@@ -437,6 +472,136 @@ def cache_decode(q, cache: PagedCache, table, lens, block_size: int, topk: int, 
                                    lse, workspace)
     if status:
         raise MobaError("moba_cache_decode", status)
+    return out, lse
+
+
+class Rotation(NamedTuple):
+    """How fast the pairs of a head's first 2 * len(freqs) dims turn, and which dims make a pair."""
+    freqs: torch.Tensor         # [R / 2] float64 on the GPU, radians a position
+    amplitude: float = 1.0      # factor of the result
+    interleaved: bool = False   # pairs (2i, 2i + 1); otherwise (i, i + R / 2)
+
+
+def rotation(rot_dim: int, base: float = 10000.0, scaling=None, factor: float = 1.0, original_length=None,
+             low: float = 1.0, high: float = 32.0, interleaved: bool = False, device="cuda") -> Rotation:
+    """Rotary frequencies base ** (-2 i / rot_dim), as they are or scaled for contexts `factor` times as
+    long as the `original_length` a model was trained on:
+      "linear"  divided by factor (position interpolation)
+      "base"    of a base factor ** (rot_dim / (rot_dim - 2)) as large: the slowest pair is interpolated,
+                the fastest is not
+      "parts"   pairs that turn fewer than `low` times over original_length are interpolated, more than
+                `high` times kept, and in between mixed linearly by that number; the amplitude is
+                0.1 ln(factor) + 1 (NTK-by-parts with its attention temperature, arXiv 2309.00071)"""
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError("rot_dim must be even and positive")
+    if scaling not in (None, "linear", "base", "parts"):
+        raise ValueError("scaling must be None, 'linear', 'base' or 'parts'")
+    if not base > 0.0 or not factor >= 1.0:
+        raise ValueError("base must be positive, factor at least 1")
+    base, factor = float(base), float(factor)
+    if scaling == "base":
+        if rot_dim == 2:
+            raise ValueError("a single pair has no slowest and fastest: scaling 'base' needs rot_dim > 2")
+        base *= factor ** (rot_dim / (rot_dim - 2))
+    freqs = [base ** (-2 * i / rot_dim) for i in range(rot_dim // 2)]
+    amplitude = 1.0
+    if scaling == "linear":
+        freqs = [f / factor for f in freqs]
+    if scaling == "parts":
+        if not original_length or not low < high:
+            raise ValueError("scaling 'parts' needs original_length, and low < high")
+        turns = [original_length * f / (2 * math.pi) for f in freqs]
+        keep = [min(1.0, max(0.0, (t - low) / (high - low))) for t in turns]
+        freqs = [f * (k + (1.0 - k) / factor) for f, k in zip(freqs, keep)]
+        amplitude = 0.1 * math.log(factor) + 1.0
+    return Rotation(torch.tensor(freqs, dtype=torch.float64, device=device), amplitude, bool(interleaved))
+
+
+def rope(q, k, rot: Rotation, pos=None, cu_seqlens=None, start=None, q_out=None, k_out=None, stream=None):
+    """Rotary positions of queries [T, Hq, D] and keys [T, Hk, D] (bf16 or fp32; k may be None): the
+    first 2 * len(rot.freqs) dims of every head are turned, the others copied.  Rows stand at pos [T] (int32
+    or int64), or, packed, row t of sequence s at start[s] + t - cu_seqlens[s] (int32 on the GPU; start None:
+    0), rows of no sequence left as they are.  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    status, qo, ko = _latent_call("rope", q, stream, False, q, k, rot, pos, cu_seqlens, start, q_out, k_out)
+    if status:
+        raise MobaError("moba_rope", status)
+    return qo, ko
+
+
+def rope_backward(dq_out, dk_out, rot: Rotation, pos=None, cu_seqlens=None, start=None, dq=None, dk=None,
+                  stream=None):
+    """Gradients of rope() w.r.t. q and k from those w.r.t. its results (dk_out may be None; dq and dk may be
+    dq_out and dk_out).  Returns (dq, dk)."""
+    status, gq, gk = _latent_call("rope", dq_out, stream, True, dq_out, dk_out, rot, pos, cu_seqlens, start, dq,
+                                  dk)
+    if status:
+        raise MobaError("moba_rope_backward", status)
+    return gq, gk
+
+
+_LATENT_SCALE = 1.0 / math.sqrt(192.0)
+
+
+def latent_forward(q, k, k_rope, v, cu_seqlens, scale=None, out=None, lse=None, stream=None):
+    """Causal latent attention, expanded: q [T, H, 192] (128 dims, then 64 rotary ones), k [T, H, 128],
+    k_rope [T, 64] shared by all heads, v [T, H, 128], all bf16, rotary positions applied; cu_seqlens [S + 1]
+    int32 on the GPU.  scale: None for 1 / sqrt(192).  Returns (out [T, H, 128], lse [H, T] fp32)."""
+    status, out, lse = _latent_call("forward", q, stream, q, k, k_rope, v, cu_seqlens,
+                                    _LATENT_SCALE if scale is None else scale, out, lse)
+    if status:
+        raise MobaError("moba_latent_forward", status)
+    return out, lse
+
+
+def latent_backward_workspace_bytes(T: int, num_heads: int) -> int:
+    """Bytes of latent_backward()'s workspace (0: such a call would be refused)."""
+    return int(load().moba_latent_backward_workspace_bytes(*(max(-1, min(int(x), 2 ** 31 - 1))
+                                                             for x in (T, num_heads))))
+
+
+def latent_backward(q, k, k_rope, v, cu_seqlens, out, lse, dout, scale=None, dq=None, dk=None, dk_rope=None,
+                    dv=None, workspace=None, stream=None):
+    """Gradients of latent_forward() (out and lse its results, dout [T, H, 128]).  workspace: uint8, at least
+    latent_backward_workspace_bytes() of it; by default a fresh one per call.  Returns (dq [T, H, 192], dk
+    [T, H, 128], dk_rope [T, 64], dv [T, H, 128])."""
+    status, *grads = _latent_call("backward", q, stream, q, k, k_rope, v, cu_seqlens, out, lse, dout,
+                                  _LATENT_SCALE if scale is None else scale, dq, dk, dk_rope, dv, workspace)
+    if status:
+        raise MobaError("moba_latent_backward", status)
+    return tuple(grads)
+
+
+def latent_cache_new(num_pages: int, page_size: int = 64, device="cuda") -> torch.Tensor:
+    """Pages [num_pages, page_size, 576] bf16 of a latent cache: a token's row is its latent vector (512)
+    and its rotary key (64).  Uninitialised: nothing reads what was not written."""
+    if page_size not in (64, 128, 192, 256):
+        raise ValueError("page_size must be 64, 128, 192 or 256")
+    return torch.empty((int(num_pages), page_size, 576), dtype=torch.bfloat16, device=device)
+
+
+def latent_write(c, k_rope, slots, pages, rot=None, pos=None, cu_seqlens=None, start=None, stream=None) -> None:
+    """Writes latent vectors c [T, 512] and rotary keys k_rope [T, 64] (bf16) into their slots [T] int64
+    (negative: left out), as cache_plan() gives them.  With a Rotation, the keys are turned on the way;
+    positions as for rope()."""
+    _check("moba_latent_write", _latent_call("write", c, stream, c, k_rope, slots, pages, rot, pos, cu_seqlens,
+                                             start))
+
+
+def latent_decode_workspace_bytes(num_requests: int, table_width: int, num_heads: int, page_size: int) -> int:
+    """Bytes of latent_decode()'s workspace (0: such a call would be refused)."""
+    return int(load().moba_latent_decode_workspace_bytes(
+        *(max(-1, min(int(x), 2 ** 31 - 1)) for x in (num_requests, table_width, num_heads, page_size))))
+
+
+def latent_decode(q_c, q_rope, pages, table, lens, scale=None, out=None, lse=None, workspace=None, stream=None):
+    """Latent attention of one new query per request, absorbed, over the lens[s] tokens its pages hold: q_c
+    [S, H, 512], q_rope [S, H, 64] bf16; table [S, W], lens [S] int32.  A request with lens[s] <= 0 gets out 0
+    and lse -inf.  workspace: uint8, at least latent_decode_workspace_bytes() of it; by default a fresh
+    one per call.  Returns (out [S, H, 512] bf16, lse [H, S])."""
+    status, out, lse = _latent_call("decode", q_c, stream, q_c, q_rope, pages, table, lens,
+                                    _LATENT_SCALE if scale is None else scale, out, lse, workspace)
+    if status:
+        raise MobaError("moba_latent_decode", status)
     return out, lse
 
 

@@ -1,0 +1,273 @@
+// Causal latent attention, expanded form: z_ij = scale (<q_i[0:128], k_j> + <q_i[128:192], kr_j>),
+// out_i = sum_j softmax(z_i)_j v_j, where kr is one rotary key for all heads.
+//
+// Bound by the matrix cores: 640 operations a scored pair and 640 bytes a (head, token).  Work-group = 8
+// waves = 256 queries of one head; wave w owns queries 32w .. 32w + 31, one per lane column.  Keys come
+// in tiles of 64: k and v (128 dims each) and kr (64) are staged row-major in LDS by DMA, two
+// buffers each (80 KiB), tile i + 1 in flight while tile i is used, one barrier a tile.  On
+// v_mfma_f32_32x32x16_bf16, per tile and wave:
+//   S^T (keys x queries) = K . Q^T    2 halves x 12 k-steps, Q in registers
+//   online softmax in 32 bits: a lane holds one query and 32 of the 64 keys.  Weights are formed
+//     under the running max, which is raised only when a lane's weights sum to more than 2^8
+//   O^T (dims x queries) += V^T . P^T  4 dim tiles x 4 k-steps, V^T by transposed LDS reads
+// The weights enter the second product as bf16 (2^-9 of each, independent of each other: it adds
+// to the result about what its own rounding to bf16 does); all sums are fp32.
+#include "latent_tile.h"
+
+#include <math.h>
+
+#include <type_traits>
+
+namespace moba {
+namespace {
+
+constexpr int kWaves = kLatRows / 32;
+constexpr int kBufChunks = 2 * kWide + kSlim;  // k, v, kr
+constexpr float kSumLimit = 256.0f;
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kStageRow = kNope / 8 + 1;  // 16-byte chunks of a staged result row (one pad)
+
+// P^T operands of the tile under the running max m; returns the lane's sum of weights.
+__device__ __forceinline__ float weights(const f32x16 (&s)[2], float m, bf16x8 (&pb)[4], float c2) {
+  float ts = 0.0f;
+#pragma unroll
+  for (int th = 0; th < 2; th++)
+#pragma unroll
+    for (int s2 = 0; s2 < 2; s2++) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[th][8 * s2 + 2 * e], c2, -m));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[th][8 * s2 + 2 * e + 1], c2, -m));
+        w[e] = pack_bf16(p0, p1);
+        ts += p0 + p1;
+      }
+      pb[2 * th + s2] = as_bf16x8(u32x4{w[0], w[1], w[2], w[3]});
+    }
+  return ts;
+}
+
+template <bool EDGE>
+__device__ __forceinline__ void softmax(f32x16 (&s)[2], float& m, float& l, f32x16 (&o)[4],
+                                        bf16x8 (&pb)[4], int hi, float c2) {
+  if (EDGE) mask_keys(s, -4, hi);
+  float ts = 0.0f;
+  bool redo = __builtin_amdgcn_ballot_w64(m == -INFINITY) != 0;
+  if (!redo) {
+    ts = weights(s, m, pb, c2);
+    redo = __builtin_amdgcn_ballot_w64(!(ts <= kSumLimit)) != 0;
+  }
+  if (redo) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int th = 0; th < 2; th++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[th][r]);
+    mx = fmaxf(mx, xor32(mx)) * c2;
+    const float m_new = fmaxf(m, mx);
+    const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+    l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+      for (int r = 0; r < 16; r++) o[dt][r] *= alpha;
+    m = m_new;
+    ts = weights(s, m == -INFINITY ? 0.0f : m, pb, c2);
+  }
+  l += ts;
+}
+
+// Whether a wide tile holds a value that is not finite (all lanes alike).
+__device__ __forceinline__ bool holds_odd(const char* vb, int lane) {
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 most = 0;
+#pragma unroll
+  for (int j = 0; j < kWide / 64; j++) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(vb + (64 * j + lane) * 16) & 0x7f807f80u;
+    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x8, w));
+  }
+  int odd = 0;
+#pragma unroll
+  for (int e = 0; e < 8; e++) odd |= most[e] == 0x7f80;
+  return __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+}
+
+// O^T += V^T . P^T of an edge tile that holds values that are not finite: a weight of 0 must not
+// meet them, since a row may not see what it does not attend.  One key at a time, and a row takes
+// the product of those that it attends.  hi: keys of the tile that the lane's row attends.
+__device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const uint32_t (&ov)[2][4],
+                                          const bf16x8 (&pb)[4], int hi, int hh) {
+#pragma unroll
+  for (int ks = 0; ks < 4; ks++)
+#pragma unroll 1
+    for (int kk = 0; kk < 16; kk++) {
+      u32x4 only;  // element e of an operand: key 16 ks + 8 (e / 4) + 4 hh + e % 4
+#pragma unroll
+      for (int w = 0; w < 4; w++) {
+        const int k0 = 8 * (w >> 1) + 4 * hh + 2 * (w & 1);
+        only[w] = k0 == kk ? 0xffffu : k0 + 1 == kk ? 0xffff0000u : 0;
+      }
+      const bool attends = 16 * ks + kk < hi;
+#pragma unroll
+      for (int dt = 0; dt < 4; dt++) {
+        const char* b = vb + 16 * ks * 256;
+        const u32x4 v = __builtin_bit_cast(u32x4, join16(tr16(b + ov[0][dt]), tr16(b + ov[1][dt])));
+        f32x16 t;
+#pragma unroll
+        for (int r = 0; r < 16; r++) t[r] = 0.0f;
+        t = mfma(as_bf16x8(v & only), pb[ks], t);
+#pragma unroll
+        for (int r = 0; r < 16; r++) o[dt][r] += attends ? t[r] : 0.0f;
+      }
+    }
+}
+
+__global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentArgs a) {
+  __shared__ u32x4 lds[2 * kBufChunks];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qc = lane & 31, hh = lane >> 5;
+
+  Work wk;
+  if (!latent_work<true>(a, latent_places(a.T, a.S, kLatRows), &wk)) return;
+  Place pl;
+  if (!latent_place(a, wk.place, kLatRows, &pl)) return;
+  const int h = __builtin_amdgcn_readfirstlane(wk.h);
+  const int row = pl.t0 + 32 * wave + qc;         // this lane's query, within the sequence
+  const int rc = min(row, pl.len - 1);
+  const int kend = min(pl.t0 + kLatRows, pl.len);
+
+  bf16x8 qf[12];
+  {
+    const __hip_bfloat16* qrow = a.q + (pl.tok0 + rc) * a.q_st + (int64_t)h * a.q_sh + 8 * hh;
+#pragma unroll
+    for (int kk = 0; kk < 12; kk++) qf[kk] = as_bf16x8(*reinterpret_cast<const u32x4*>(qrow + 16 * kk));
+  }
+  const auto rows = [&](const __hip_bfloat16* p, int64_t st, int64_t sh) {
+    return Rows{scalar_ptr(p + pl.tok0 * st + (int64_t)h * sh), (uint32_t)(st * 2), pl.len};
+  };
+  const Rows rk = rows(a.k, a.k_st, a.k_sh), rv = rows(a.v, a.v_st, a.v_sh), rr = rows(a.kr, a.kr_st, 0);
+  const auto stage = [&](int i, u32x4* buf) {
+    stage_tile<kWaves, true>(rk, i, buf, wave, lane);
+    stage_tile<kWaves, true>(rv, i, buf + kWide, wave, lane);
+    stage_tile<kWaves, false>(rr, i, buf + 2 * kWide, wave, lane);
+  };
+
+  // operand offsets: rows qc (+ 32: the same swizzle, 32 rows on), chunk 2 kk + hh
+  uint32_t ok[8], orr[4], ov[2][4];
+#pragma unroll
+  for (int kk = 0; kk < 8; kk++) ok[kk] = at_wide(qc, 2 * kk + hh);
+#pragma unroll
+  for (int kk = 0; kk < 4; kk++) orr[kk] = at_slim(qc, 2 * kk + hh);
+  const TrLane tl = tr_lane(qc, hh);
+#pragma unroll
+  for (int x = 0; x < 2; x++)
+#pragma unroll
+    for (int dt = 0; dt < 4; dt++) ov[x][dt] = tr_wide(tl, dt, x);
+
+  const float c2 = a.scale_log2;
+  f32x16 o[4];
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+    for (int r = 0; r < 16; r++) o[dt][r] = 0.0f;
+
+  const int n = (kend + kLatTile - 1) / kLatTile;
+  stage(0, lds);
+  dma_wait();
+  __syncthreads();
+  const auto step = [&](auto masked, int i) {
+    constexpr bool edge = decltype(masked)::value;
+    const char* buf = reinterpret_cast<const char*>(lds + (i & 1) * kBufChunks);
+    if (i + 1 < n) stage(i + 1, lds + ((i + 1) & 1) * kBufChunks);
+    f32x16 s[2];
+    {
+      const char* bk = buf;
+      const char* br = buf + 2 * kWide * 16;
+#pragma unroll
+      for (int th = 0; th < 2; th++)
+#pragma unroll
+        for (int r = 0; r < 16; r++) s[th][r] = 0.0f;
+      u32x4 op[24];
+#pragma unroll
+      for (int j = 0; j < 24; j++) {
+        const int th = j & 1, kk = j >> 1;
+        op[j] = kk < 8 ? *reinterpret_cast<const u32x4*>(bk + 8192 * th + ok[kk & 7])
+                       : *reinterpret_cast<const u32x4*>(br + 4096 * th + orr[(kk - 8) & 3]);
+      }
+#pragma unroll
+      for (int j = 0; j < 24; j++) s[j & 1] = mfma(as_bf16x8(op[j]), qf[j >> 1], s[j & 1]);
+      __builtin_amdgcn_sched_group_barrier(0x100, kPre, 0);
+#pragma unroll
+      for (int j = 0; j < 24 - kPre; j++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, kPre, 0);
+    }
+    const int u0 = i * kLatTile;
+    const int hi = row + 1 - u0 - 4 * hh;
+    bf16x8 pb[4];
+    softmax<edge>(s, m, l, o, pb, hi, c2);
+    const char* bv = buf + kWide * 16;
+    if (edge && holds_odd(bv, lane)) {
+      pv_by_key(o, bv, ov, pb, row + 1 - u0, hh);
+    } else {
+      s16x4 t0[16], t1[16];
+#pragma unroll
+      for (int j = 0; j < 16; j++) {
+        const char* b = bv + 16 * (j >> 2) * 256;
+        t0[j] = tr16(b + ov[0][j & 3]);
+        t1[j] = tr16(b + ov[1][j & 3]);
+      }
+#pragma unroll
+      for (int j = 0; j < 16; j++) o[j & 3] = mfma(join16(t0[j], t1[j]), pb[j >> 2], o[j & 3]);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2 * kPre, 0);
+#pragma unroll
+      for (int j = 0; j < 16 - kPre; j++) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, kPre, 0);
+    }
+    dma_wait();
+    __syncthreads();
+  };
+  const int nfull = pl.t0 / kLatTile;  // tiles before the diagonal's
+  for (int i = 0; i < nfull; i++) step(std::false_type(), i);
+  for (int i = nfull; i < n; i++) step(std::true_type(), i);
+
+  // the buffers are free: each wave stages its 32 rows and writes them whole
+  const float lt = l + xor32(l);
+  const float inv = 1.0f / lt;
+  if (hh == 0 && row < pl.len)
+    a.lse[(int64_t)h * a.T + pl.tok0 + row] = (m + __builtin_amdgcn_logf(lt)) * kLn2;
+  u32x4* stg = lds + wave * 32 * kStageRow;
+  uint2* srow = reinterpret_cast<uint2*>(stg + qc * kStageRow);
+#pragma unroll
+  for (int dt = 0; dt < 4; dt++)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; r4++)
+      srow[(32 * dt + 8 * r4 + 4 * hh) >> 2] =
+          make_uint2(pack_bf16(o[dt][4 * r4] * inv, o[dt][4 * r4 + 1] * inv),
+                     pack_bf16(o[dt][4 * r4 + 2] * inv, o[dt][4 * r4 + 3] * inv));
+  __builtin_amdgcn_s_waitcnt(0);  // (a wave's own LDS writes, read by its other lanes)
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    const int rr2 = 4 * j + (lane >> 4), t = pl.t0 + 32 * wave + rr2;
+    if (t < pl.len)
+      reinterpret_cast<u32x4*>(a.out + (pl.tok0 + t) * a.o_st + (int64_t)h * a.o_sh)[lane & 15] =
+          stg[rr2 * kStageRow + (lane & 15)];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_latent_forward(const LatentArgs& a, hipStream_t st) {
+  latent_forward_kernel<<<latent_grid(a, kLatRows), 64 * kWaves, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace moba

@@ -1,0 +1,188 @@
+// Rotary positions.  A pair (x, y) of a head's dims at position p becomes
+//   (x cos(p f) - y sin(p f), x sin(p f) + y cos(p f)) * amplitude
+// with the pair's frequency f; the gradient is the same with -p.  Pairs are dims (i, i + half) or
+// (2i, 2i + 1) of the first 2 half dims of a head.
+//
+// Bound by memory: every element is read and written once.  A thread takes one group of `vec` pairs of
+// a token, forms its cosines and sines once (about 30 instructions a pair, most of it the 64-bit
+// turns) and applies them to kHeads heads, whose two 16-byte pieces each are loaded before the first is
+// used.
+#include "rope_internal.h"
+
+namespace moba {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename E, int V, bool INTERLEAVED, int HEADS>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a, int64_t t0, uint32_t total, uint32_t items,
+                                                       uint32_t groups) {
+  const uint32_t x = blockIdx.x * kThreads + threadIdx.x;
+  if (x >= total) return;
+  const uint32_t row = x / items, item = x - row * items;
+  const int64_t t = t0 + row / groups;
+  const int h0 = (int)(row % groups) * HEADS, heads = a.Hq + a.Hk;
+  int64_t p;
+  if (!row_position(a.r, t, &p)) return;
+  const int nturn = a.r.half / V;
+  const bool turns = (int)item < nturn;
+  // the thread's two pieces of a head
+  int d0, d1;
+  bool both = true;
+  if (turns) {
+    d0 = INTERLEAVED ? 2 * V * (int)item : V * (int)item;
+    d1 = INTERLEAVED ? d0 + V : d0 + a.r.half;
+  } else {
+    d0 = 2 * a.r.half + 2 * V * ((int)item - nturn);
+    both = d0 + V < a.D;
+    d1 = both ? d0 + V : d0;
+  }
+  using P = Piece<E, V>;
+  P u[HEADS], w[HEADS];
+#pragma unroll
+  for (int i = 0; i < HEADS; i++) {
+    const int h = min(h0 + i, heads - 1);
+    const E* src = h < a.Hq ? static_cast<const E*>(a.q) + t * a.q_st + h * a.q_sh
+                            : static_cast<const E*>(a.k) + t * a.k_st + (h - a.Hq) * a.k_sh;
+    u[i] = *reinterpret_cast<const P*>(src + d0);
+    w[i] = *reinterpret_cast<const P*>(src + d1);
+  }
+  if (turns) {
+    float c[V], s[V];
+#pragma unroll
+    for (int j = 0; j < V; j++) cos_sin_at(a.r, V * (int)item + j, p, &c[j], &s[j]);
+#pragma unroll
+    for (int i = 0; i < HEADS; i++)
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        // (interleaved, the 2V elements of u and w are V pairs)
+        E& e0 = INTERLEAVED ? (2 * j < V ? u[i].e[(2 * j) % V] : w[i].e[(2 * j) % V]) : u[i].e[j];
+        E& e1 = INTERLEAVED ? (2 * j + 1 < V ? u[i].e[(2 * j + 1) % V] : w[i].e[(2 * j + 1) % V]) : w[i].e[j];
+        float f0 = to_f32(e0), f1 = to_f32(e1);
+        turn_pair(f0, f1, c[j], s[j]);
+        e0 = from_f32<E>(f0);
+        e1 = from_f32<E>(f1);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < HEADS; i++) {
+    const int h = h0 + i;
+    if (h >= heads) break;
+    E* dst = h < a.Hq ? static_cast<E*>(a.qo) + t * a.qo_st + h * a.qo_sh
+                      : static_cast<E*>(a.ko) + t * a.ko_st + (h - a.Hq) * a.ko_sh;
+    *reinterpret_cast<P*>(dst + d0) = u[i];
+    if (both) *reinterpret_cast<P*>(dst + d1) = w[i];
+  }
+}
+
+template <typename E, int V, bool INTERLEAVED, int HEADS>
+hipError_t rope_launches(const RopeArgs& a, hipStream_t st) {
+  const uint32_t rest = a.copy ? (uint32_t)((a.D - 2 * a.r.half + 2 * V - 1) / (2 * V)) : 0;
+  const uint32_t items = (uint32_t)(a.r.half / V) + rest;
+  const uint32_t groups = (uint32_t)((a.Hq + a.Hk + HEADS - 1) / HEADS);
+  const int64_t per = (int64_t)items * groups;        // threads of a token (host: below 2^31)
+  const int64_t most = ((int64_t(1) << 31) - 1) / per;  // tokens of a launch
+  for (int64_t t = 0; t < a.T; t += most) {
+    const int64_t n = a.T - t < most ? a.T - t : most;
+    const uint32_t total = (uint32_t)(n * per);
+    rope_kernel<E, V, INTERLEAVED, HEADS>
+        <<<(total + kThreads - 1) / kThreads, kThreads, 0, st>>>(a, t, total, items, groups);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// Heads a thread takes: as many as leave every SIMD some waves.
+template <typename E, int V, bool INTERLEAVED>
+hipError_t rope_heads(const RopeArgs& a, hipStream_t st) {
+  const int64_t threads = a.T * (a.Hq + a.Hk) * (a.D / (2 * V));
+  if (threads >= int64_t(1) << 20) return rope_launches<E, V, INTERLEAVED, 4>(a, st);
+  return rope_launches<E, V, INTERLEAVED, 1>(a, st);
+}
+
+template <typename E, int V>
+hipError_t rope_layout(bool interleaved, const RopeArgs& a, hipStream_t st) {
+  return interleaved ? rope_heads<E, V, true>(a, st) : rope_heads<E, V, false>(a, st);
+}
+
+// ================================================================ latent write
+// A token's row of the cache: 512 numbers as they are, then the 64 of the rotary key, turned.  72
+// threads a token, 16 bytes each: a copy, bound by memory.
+constexpr int kRank = 512, kRot = 64, kRowLen = kRank + kRot, kRowPieces = kRowLen / 8;
+
+template <bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void latent_write_kernel(LatentWriteArgs a, int64_t t0, uint32_t total) {
+  const uint32_t x = blockIdx.x * kThreads + threadIdx.x;
+  if (x >= total) return;
+  const uint32_t row = x / kRowPieces;
+  const int piece = (int)(x - row * kRowPieces);
+  const int64_t t = t0 + row;
+  const int64_t slot = a.slots[t];
+  if (slot < 0 || slot >= (int64_t)a.N * a.P) return;
+  const int64_t page = slot / a.P;
+  __hip_bfloat16* dst = a.pages + page * a.p_sp + (slot - page * a.P) * kRowLen;
+  if (piece < kRank / 8) {
+    reinterpret_cast<uint4*>(dst)[piece] = reinterpret_cast<const uint4*>(a.c + t * a.c_st)[piece];
+    return;
+  }
+  const int i = piece - kRank / 8;  // 4 pairs of the rotary key
+  const __hip_bfloat16* src = a.kr + t * a.kr_st;
+  dst += kRank;
+  using P = Piece<__hip_bfloat16, 4>;
+  const int d0 = INTERLEAVED ? 8 * i : 4 * i, d1 = INTERLEAVED ? d0 + 4 : d0 + kRot / 2;
+  P u = *reinterpret_cast<const P*>(src + d0), w = *reinterpret_cast<const P*>(src + d1);
+  int64_t p;
+  if (a.rotate) {
+    if (!row_position(a.r, t, &p)) p = 0;  // (a row of no sequence that has a slot: as it is)
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      float c, s;
+      cos_sin_at(a.r, 4 * i + j, p, &c, &s);
+      __hip_bfloat16& e0 = INTERLEAVED ? (j < 2 ? u.e[(2 * j) % 4] : w.e[(2 * j) % 4]) : u.e[j];
+      __hip_bfloat16& e1 = INTERLEAVED ? (j < 2 ? u.e[(2 * j + 1) % 4] : w.e[(2 * j + 1) % 4]) : w.e[j];
+      float f0 = to_f32(e0), f1 = to_f32(e1);
+      turn_pair(f0, f1, c, s);
+      e0 = from_f32<__hip_bfloat16>(f0);
+      e1 = from_f32<__hip_bfloat16>(f1);
+    }
+  }
+  *reinterpret_cast<P*>(dst + d0) = u;
+  *reinterpret_cast<P*>(dst + d1) = w;
+}
+
+}  // namespace
+
+hipError_t launch_rope(bool bf16, bool interleaved, int vec, const RopeArgs& a, hipStream_t st) {
+  if (a.T == 0 || a.Hq + a.Hk == 0) return hipSuccess;
+  if (bf16) {
+    using E = __hip_bfloat16;
+    switch (vec) {
+      case 8: return rope_layout<E, 8>(interleaved, a, st);
+      case 4: return rope_layout<E, 4>(interleaved, a, st);
+      case 2: return rope_layout<E, 2>(interleaved, a, st);
+      default: return rope_layout<E, 1>(interleaved, a, st);
+    }
+  }
+  switch (vec) {
+    case 4: return rope_layout<float, 4>(interleaved, a, st);
+    case 2: return rope_layout<float, 2>(interleaved, a, st);
+    default: return rope_layout<float, 1>(interleaved, a, st);
+  }
+}
+
+hipError_t launch_latent_write(bool interleaved, const LatentWriteArgs& a, hipStream_t st) {
+  constexpr int64_t most = ((int64_t(1) << 31) - 1) / kRowPieces;
+  for (int64_t t = 0; t < a.T; t += most) {
+    const int64_t n = a.T - t < most ? a.T - t : most;
+    const uint32_t total = (uint32_t)(n * kRowPieces);
+    const unsigned grid = (total + kThreads - 1) / kThreads;
+    if (interleaved) latent_write_kernel<true><<<grid, kThreads, 0, st>>>(a, t, total);
+    else latent_write_kernel<false><<<grid, kThreads, 0, st>>>(a, t, total);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace moba
