@@ -5,6 +5,7 @@
 #include "rope_internal.h"
 
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 using namespace moba;
@@ -81,6 +82,17 @@ bool may_share(const Rows3& a, const Rows3& b) {
     }
   }
   return false;
+}
+
+// Whether one of the outputs may share memory with an input or another output.
+moba_status check_apart(std::initializer_list<const Rows3*> outs, std::initializer_list<const Rows3*> ins) {
+  for (auto o = outs.begin(); o != outs.end(); o++) {
+    for (const Rows3* i : ins)
+      if (may_share(**o, *i)) return MOBA_ERR_LAYOUT;
+    for (auto p = o + 1; p != outs.end(); p++)
+      if (may_share(**o, **p)) return MOBA_ERR_LAYOUT;
+  }
+  return MOBA_OK;
 }
 
 // Rotation of T rows with heads of D dims.
@@ -196,8 +208,8 @@ moba_status check_latent_pages(const moba_tensor* t, __hip_bfloat16** data, int6
 
 // q, k, k_rope, v and cu_seqlens of the expanded form
 moba_status check_latent(const moba_tensor* q, const moba_tensor* k, const moba_tensor* kr, const moba_tensor* v,
-                         const moba_tensor* cu, float scale, LatentArgs* a) {
-  Rows3 vq, vk, vr, vv;
+                         const moba_tensor* cu, float scale, LatentArgs* a, Rows3 (&in)[4]) {
+  Rows3 &vq = in[0], &vk = in[1], &vr = in[2], &vv = in[3];
   moba_status st;
   if ((st = check_rows(q, MOBA_BF16, true, kQk, 16, &vq)) != MOBA_OK) return st;
   if ((st = check_rows(k, MOBA_BF16, true, kNope, 16, &vk)) != MOBA_OK) return st;
@@ -290,12 +302,13 @@ moba_status moba_latent_forward(const moba_tensor* q, const moba_tensor* k, cons
                                 const moba_tensor* v, const moba_tensor* cu_seqlens, float scale, moba_tensor* out,
                                 moba_tensor* lse, hipStream_t stream) {
   LatentArgs a{};
-  Rows3 vo;
+  Rows3 in[4], vo;
   moba_status st;
   if (missing(out) || missing(lse)) return MOBA_ERR_NULL;
-  if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a)) != MOBA_OK) return st;
+  if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a, in)) != MOBA_OK) return st;
   if ((st = check_out(out, MOBA_BF16, true, kNope, 16, &vo)) != MOBA_OK) return st;
   if (vo.T != a.T || vo.H != a.H) return MOBA_ERR_SHAPE;
+  if ((st = check_apart({&vo}, {&in[0], &in[1], &in[2], &in[3]})) != MOBA_OK) return st;
   const int64_t ls[2] = {a.H, a.T};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
   if ((st = check_scale(scale)) != MOBA_OK) return st;
@@ -319,10 +332,10 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
                                  moba_tensor* dq, moba_tensor* dk, moba_tensor* dk_rope, moba_tensor* dv,
                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
   LatentArgs a{};
-  Rows3 vo, vd, gq, gk, gr, gv;
+  Rows3 in[4], vo, vd, gq, gk, gr, gv;
   moba_status st;
   if (missing(lse)) return MOBA_ERR_NULL;
-  if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a)) != MOBA_OK) return st;
+  if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a, in)) != MOBA_OK) return st;
   if ((st = check_rows(out, MOBA_BF16, true, kNope, 16, &vo)) != MOBA_OK) return st;
   if ((st = check_rows(dout, MOBA_BF16, true, kNope, 16, &vd)) != MOBA_OK) return st;
   if ((st = check_out(dq, MOBA_BF16, true, kQk, 16, &gq)) != MOBA_OK) return st;
@@ -332,6 +345,7 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
   for (const Rows3* x : {&vo, &vd, &gq, &gk, &gv})
     if (x->T != a.T || x->H != a.H) return MOBA_ERR_SHAPE;
   if (gr.T != a.T) return MOBA_ERR_SHAPE;
+  if ((st = check_apart({&gq, &gk, &gr, &gv}, {&in[0], &in[1], &in[2], &in[3], &vo, &vd})) != MOBA_OK) return st;
   if (vd.st >= int64_t(1) << 24) return MOBA_ERR_UNSUPPORTED;
   const int64_t ls[2] = {a.H, a.T};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
@@ -413,7 +427,7 @@ moba_status moba_latent_decode(const moba_tensor* q_c, const moba_tensor* q_rope
   if ((st = check_out(out, MOBA_BF16, true, kRank, 16, &vo)) != MOBA_OK) return st;
   const int64_t S = vc.T, H = vc.H;
   if (vr.T != S || vr.H != H || vo.T != S || vo.H != H) return MOBA_ERR_SHAPE;
-  if (may_share(vo, vc) || may_share(vo, vr)) return MOBA_ERR_LAYOUT;
+  if ((st = check_apart({&vo}, {&vc, &vr})) != MOBA_OK) return st;
   const int64_t ls[2] = {H, S};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
   if (table->dtype != MOBA_I32) return MOBA_ERR_DTYPE;
