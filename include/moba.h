@@ -517,7 +517,7 @@ moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, c
  * Latent attention of one new query per request over the paged cache, absorbed.
  * table [S, W] i32 (rows contiguous, any row stride), lens [S] i32, as for moba_cache_decode: a request
  * with lens[s] <= 0 gets out 0 and lse -inf; lens[s] above W * P counts as W * P; tokens of a table
- * entry outside [0, N) are left out as if masked.  H <= 4096, S * H < 2^24, S * W * P / 64 < 2^30.
+ * entry outside [0, N) are left out as if masked.  H <= 4096, S * H < 2^23, S * W * P / 64 < 2^30.
  * out [S, H, 512] bf16, lse [H, S] f32.  What pages hold past a request's length is never used, whatever
  * its bits.  fp32 softmax and sums; the weights enter the matrix cores as bf16.  A request's
  * split over work-groups, and with it its rounding, depends on the whole batch.

@@ -261,7 +261,7 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t H, int64_t P, LatentShape
   if (S < 0 || W < 1 || H < 1) return MOBA_ERR_SHAPE;
   if (P < kLatStep || P > 256 || P % kLatStep != 0) return MOBA_ERR_UNSUPPORTED;
   if (H > 4096 || S >= kMost || W >= kMost || S * W >= (int64_t(1) << 30) / (P / kLatStep) ||
-      S * H >= int64_t(1) << 24)
+      S * H >= int64_t(1) << 23)
     return MOBA_ERR_UNSUPPORTED;
   // heads of a group: what a work-group's registers hold, no more than there are
   d->heads = H <= 16 ? 16 : H <= 32 ? 32 : 64;

@@ -10,12 +10,13 @@
 // request) stand in one line, and every share of heads-groups work-groups takes an equal run of it; a
 // request that lies in one run is finished there, the others leave partials that a second kernel joins.
 // Two buffers of 64 rows (72 KiB each), step i + 1 in flight while step i is used.  On
-// v_mfma_f32_16x16x32_bf16, per step:
+// v_mfma_f32_32x32x16_bf16 (M = 64) or v_mfma_f32_16x16x32_bf16, per step:
 //   S^T (tokens x heads) = U . Q^T   the waves share out tokens and heads (M = 64: 2 x 2, else 4 x 1),
 //                                    Q in registers
 //   P^T under the running max, through LDS as bf16, for all waves
 //   O^T (dims x heads) += U^T . P^T  wave w owns dims 128 w .. 128 w + 127
-// The running max is raised only when some weight of the step would pass 2^8.
+// The running max is raised only when some weight of the step passes 2^8; the step's weights are then formed
+// again.
 #include "latent_internal.h"
 #include "latent_tile.h"
 
@@ -33,7 +34,8 @@ constexpr int kStepChunks = kLatStep * kRowChunks;     // 4608
 constexpr int kDma = kStepChunks / (64 * kWaves);      // DMA instructions a wave (18)
 constexpr int kPRow = kLatStep + 8;                    // bf16 of a head's row of P (padded)
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr float kMaxLog2 = 8.0f;                       // weights stay at most 2^8
+constexpr float kMaxWeight = 256.0f;
+constexpr int kAhead = 8;                              // operand reads ahead of their products
 
 // The 72 chunks of a row: two rows to the bank period, as swz_slim in latent_tile.h has it, in
 // groups of 8 chunks.
@@ -41,33 +43,75 @@ __device__ __forceinline__ uint32_t at_row(int r, int c) {
   return (uint32_t)(r * (kRowChunks * 16) + ((c ^ swz_slim(r)) * 16));
 }
 
-__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+__device__ __forceinline__ f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ f32x16 product(bf16x8 a, bf16x8 b, f32x16 c) { return mfma(a, b, c); }
+
+// A product's tile: kT x kT results of kK terms.  Lane c + kT g holds column c, rows row(i); as an
+// operand, 16-byte chunk g of the row or column c.
+template <int T>
+struct Tile;
+template <>
+struct Tile<16> {
+  typedef f32x4 Acc;
+  static constexpr int kN = 4, kK = 32;
+  static __device__ __forceinline__ int row(int i, int g) { return 4 * g + i; }
+  static __device__ __forceinline__ Acc zero() { return Acc{0.0f, 0.0f, 0.0f, 0.0f}; }
+};
+template <>
+struct Tile<32> {
+  typedef f32x16 Acc;
+  static constexpr int kN = 16, kK = 16;
+  static __device__ __forceinline__ int row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
+  static __device__ __forceinline__ Acc zero() {
+    Acc a;
+#pragma unroll
+    for (int i = 0; i < 16; i++) a[i] = 0.0f;
+    return a;
+  }
+};
 
 __device__ __forceinline__ int steps_of(const LatentDecodeArgs& a, int s) {
   const int64_t n = a.lens[s], most = (int64_t)a.W * a.P;
   return (int)(((n < 0 ? 0 : n > most ? most : n) + kLatStep - 1) / kLatStep);
 }
 
-// Of the line of steps, share w's run: [n w / shares, n (w + 1) / shares)
-__device__ __forceinline__ int64_t run_begin(int64_t n, int64_t w, int shares) { return n * w / shares; }
+// The line of n steps (below 2^30) in runs, one a share: the first n % shares of them are a step longer.
+struct Runs {
+  uint32_t q, r;
+  __device__ __forceinline__ Runs(uint32_t n, uint32_t shares) : q(n / shares), r(n - n / shares * shares) {}
+  __device__ __forceinline__ uint32_t begin(uint32_t w) const { return w * q + min(w, r); }
+  // the share that holds step y
+  __device__ __forceinline__ uint32_t share(uint32_t y) const {
+    const uint32_t x = r * (q + 1);
+    return y < x ? y / (q + 1) : r + (y - x) / max(q, 1u);
+  }
+};
 
 template <int M>
 __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecodeArgs a) {
-  constexpr int kHt = M / 16;                  // head tiles of the group
-  constexpr int kWh = M == 64 ? 2 : 1;         // waves over heads in the first product
-  constexpr int kWt = kWaves / kWh;            // and over tokens
-  constexpr int kTt = 4 / kWt, kHw = kHt / kWh;  // token and head tiles of a wave
+  constexpr int T = M == 64 ? 32 : 16;
+  using Tl = Tile<T>;
+  using Acc = typename Tl::Acc;
+  constexpr int kHt = M / T;                     // head tiles of the group
+  constexpr int kWh = M == 64 ? 2 : 1;           // waves over heads in the first product
+  constexpr int kWt = kWaves / kWh;              // and over tokens
+  constexpr int kTt = kLatStep / T / kWt, kHw = kHt / kWh;  // token and head tiles of a wave
+  static_assert(kTt == 1, "a wave scores one tile of tokens");
+  constexpr int kNk = kRow / Tl::kK;             // terms of a score, in products
+  constexpr int kPk = T / 8;                     // of them, those of 8 chunks (2 or 4)
+  constexpr int kDt = 128 / T, kPd = 64 / T;     // dim tiles of a wave; those of 8 chunks (4 or 2)
+  constexpr int kKs = kLatStep / Tl::kK;         // products over a step's tokens
   __shared__ u32x4 lds[2 * kStepChunks];
   __shared__ __align__(16) __hip_bfloat16 pl[M * kPRow];
   __shared__ float red[kWt][M];
   __shared__ int flag[2];
-  __shared__ int64_t scan[kWaves + 2];
+  __shared__ uint32_t scan[kWaves + 1];
   __shared__ int begin_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c16 = lane & 15, g4 = lane >> 4;
+  const int c = lane % T, g = lane / T;
   const int wt = wave % kWt, wh = wave / kWt;
 
   // work-groups go round-robin to the 8 XCDs: those of one run sit on one of them
@@ -79,34 +123,34 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
   // ---- where the run begins: every thread sums the steps of a range of requests
   const int span = (a.S + kThreads - 1) / kThreads;
   const int sb = min(a.S, tid * span), se = min(a.S, sb + span);
-  int64_t mine = 0;
+  uint32_t mine = 0;
   for (int s = sb; s < se; s++) mine += steps_of(a, s);
-  int64_t upto = mine;
+  uint32_t upto = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t x = __shfl_up(upto, d, 64);
+    const uint32_t x = __shfl_up(upto, d, 64);
     if (lane >= d) upto += x;
   }
   if (lane == 63) scan[wave] = upto;
   __syncthreads();
-  int64_t base = 0, total = 0;
+  uint32_t base = 0, total = 0;
 #pragma unroll
   for (int i = 0; i < kWaves; i++) {
     if (i < wave) base += scan[i];
     total += scan[i];
   }
   upto += base;
-  const int64_t x0 = w < a.shares ? run_begin(total, w, a.shares) : 0;
-  const int64_t x1 = w < a.shares ? run_begin(total, w + 1, a.shares) : 0;
+  const Runs runs(total, a.shares);
+  const uint32_t x0 = w < a.shares ? runs.begin(w) : 0, x1 = w < a.shares ? runs.begin(w + 1) : 0;
   if (tid == 0) {
     flag[0] = flag[1] = 0;
     if (blockIdx.x == 0) a.first[a.S] = total;
   }
   if (x0 < x1 && upto - mine <= x0 && x0 < upto) {  // one thread
-    int64_t y = upto - mine;
+    uint32_t y = upto - mine;
     int s = sb;
     for (;; s++) {
-      const int n = steps_of(a, s);
+      const uint32_t n = steps_of(a, s);
       if (x0 < y + n) break;
       y += n;
     }
@@ -115,7 +159,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
   }
   // requests that begin in the share's run leave where (for the join)
   if (hg == 0) {
-    int64_t y = upto - mine;
+    uint32_t y = upto - mine;
     for (int s = sb; s < se && y < x1; s++) {
       if (y >= x0) a.first[s] = y;
       y += steps_of(a, s);
@@ -124,7 +168,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
   __syncthreads();
   if (x0 >= x1) return;
   int s = __builtin_amdgcn_readfirstlane(begin_s);
-  int64_t sx = uniform64(scan[kWaves]);  // the step at which request s begins
+  uint32_t sx = __builtin_amdgcn_readfirstlane(scan[kWaves]);  // the step at which request s begins
 
   // ---- lanes' parts of the DMA and the operands
   // DMA instruction wave + 4 x: nine of a wave's fill 32 rows, the other nine the same chunks 32 rows on
@@ -134,56 +178,81 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     const int j = 64 * (wave + kWaves * x) + lane;
     doff[x] = at_row(j / kRowChunks, j % kRowChunks);  // (the swizzle is its own inverse)
   }
-  const auto entry = [&](int s_, int step_) {
-    return a.table[(int64_t)s_ * a.t_ss + (int)((int64_t)step_ * kLatStep / a.P)];
+  const uint32_t tp = (uint32_t)a.P / kLatStep;  // steps of a page
+  struct Src {
+    int id, at;  // a step's page and its place there
+  };
+  // Lane l holds entry p0 + l of the request's table row: a load of its own at every step would be waited for
+  // together with the DMA in flight.
+  uint32_t p0 = 0;
+  int ids = 0;
+  const auto entries = [&](int s_, uint32_t from) {
+    return a.table[(int64_t)s_ * a.t_ss + min(from + lane, (uint32_t)a.W - 1)];
+  };
+  const auto source = [&](int s_, int step_) {
+    const uint32_t pg = (uint32_t)step_ / tp;
+    if (pg - p0 >= 64) {
+      p0 = pg;
+      ids = entries(s_, pg);
+      asm volatile("" : "+v"(ids));  // (used here: so waited for here, not after the branch)
+    }
+    return Src{__builtin_amdgcn_readlane(ids, pg - p0), (int)((uint32_t)step_ - pg * tp)};
   };
   const auto held = [&](int id) { return id >= 0 && id < a.N; };
-  const auto stage = [&](int id, int step_, u32x4* buf) {
+  const auto stage = [&](const Src& x_, u32x4* buf) {
     // (where there is no page its rows are cleared before they are used)
-    const int at = (int)((int64_t)step_ * kLatStep % a.P);
-    const char* src = scalar_ptr(a.pages + (held(id) ? (int64_t)id : 0) * a.p_sp + at * kRow);
+    const char* src = scalar_ptr(a.pages + (held(x_.id) ? (int64_t)x_.id : 0) * a.p_sp + x_.at * (kLatStep * kRow));
 #pragma unroll
     for (int x = 0; x < kDma; x++)
       dma16_at(src + (x / (kDma / 2)) * (kLatStep / 2 * kRow * 2), doff[x % (kDma / 2)],
                buf + 64 * (wave + kWaves * x));
   };
-  // row operand: row 16 t + c16, chunk 4 k + g4 at orow[t][k % 2] + 128 (k / 2)
-  uint32_t orow[kTt][2];
+  // row operand: row T wt + c, chunk (64 / T) k + g at orow[k % kPk] + 128 (k / kPk)
+  uint32_t orow[kPk];
 #pragma unroll
-  for (int t = 0; t < kTt; t++)
-#pragma unroll
-    for (int k = 0; k < 2; k++) orow[t][k] = at_row(16 * (kTt * wt + t) + c16, 4 * k + g4);
-  // transposed: lane's group g4 holds tokens 32 ks + 8 g4 + 4 x + (0 .. 3) of dim 16 dt + c16 of the
-  // wave's: otr[x][dt % 4] + 128 (dt / 4)
-  uint32_t otr[2][4];
+  for (int k = 0; k < kPk; k++) orow[k] = at_row(T * wt + c, (64 / T) * k + g);
+  // transposed: lane's group g holds tokens kK ks + 8 g + 4 x + (0 .. 3) of dim T dt + c of the
+  // wave's: otr[x][dt % kPd] + 128 (dt / kPd)
+  uint32_t otr[2][kPd];
 #pragma unroll
   for (int x = 0; x < 2; x++)
 #pragma unroll
-    for (int dt = 0; dt < 4; dt++)
-      otr[x][dt] = at_row(8 * g4 + 4 * x + (c16 >> 2), 16 * wave + 2 * dt + ((c16 & 3) >> 1)) + 8 * (c16 & 1);
+    for (int dt = 0; dt < kPd; dt++) {
+      const int i = lane & 15;
+      otr[x][dt] = at_row(8 * g + 4 * x + (i >> 2), 16 * wave + (T / 8) * dt + 2 * (c >> 4) + ((i & 3) >> 1)) + 8 * (i & 1);
+    }
 
   const float c2 = a.scale_log2;
   int step = (int)(x0 - sx), par = 0;
-  int id = entry(s, step);  // the page of the step that is staged
-  stage(id, step, lds);
-  for (int64_t x = x0; x < x1;) {
+  p0 = (uint32_t)step / tp;
+  ids = entries(s, p0);
+  Src at = source(s, step);  // where the staged step stands
+  stage(at, lds);
+  for (uint32_t x = x0; x < x1;) {
     // ---------------------------------------------------------- one request
     const int64_t len = min((int64_t)a.lens[s], (int64_t)a.W * a.P);
     const int ns = steps_of(a, s);
-    const int last = (int)min((int64_t)ns, x1 - sx);  // steps step .. last - 1 are the run's
+    const int last = (int)min((uint32_t)ns, x1 - sx);  // steps step .. last - 1 are the run's
     const bool whole = step == 0 && last == ns;
     const int64_t pslot = ((int64_t)w * 2 + (x == x0 ? 0 : 1)) * a.groups + hg;
-    bf16x8 qf[kHw][kRow / 32];
+    u32x4 qf[kHw][kNk];
 #pragma unroll
     for (int t = 0; t < kHw; t++) {
-      const int h = min(h0 + 16 * (kHw * wh + t) + c16, a.H - 1);
-      const __hip_bfloat16* qc = a.qc + (int64_t)s * a.qc_ss + (int64_t)h * a.qc_sh + 8 * g4;
-      const __hip_bfloat16* qr = a.qr + (int64_t)s * a.qr_ss + (int64_t)h * a.qr_sh + 8 * g4;
+      const int h = min(h0 + T * (kHw * wh + t) + c, a.H - 1);
+      const __hip_bfloat16* qc = a.qc + (int64_t)s * a.qc_ss + (int64_t)h * a.qc_sh + 8 * g;
+      const __hip_bfloat16* qr = a.qr + (int64_t)s * a.qr_ss + (int64_t)h * a.qr_sh + 8 * g;
 #pragma unroll
-      for (int k = 0; k < kRow / 32; k++)
-        qf[t][k] = as_bf16x8(*reinterpret_cast<const u32x4*>(k < kRank / 32 ? qc + 32 * k : qr + 32 * (k - kRank / 32)));
+      for (int k = 0; k < kNk; k++)
+        qf[t][k] = *reinterpret_cast<const u32x4*>(
+            k < kRank / Tl::kK ? qc + Tl::kK * k : qr + Tl::kK * (k - kRank / Tl::kK));
     }
-    f32x4 o[8][kHt];
+    // (into the accumulation registers, where the matrix cores read them as well as anywhere: the
+    // others are full)
+#pragma unroll
+    for (int t = 0; t < kHw; t++)
+#pragma unroll
+      for (int k = 0; k < kNk; k++) asm volatile("" : "+a"(qf[t][k]));
+    Acc o[kDt][kHt];
     float m[kHw], l[kHw];
 #pragma unroll
     for (int t = 0; t < kHw; t++) {
@@ -191,188 +260,215 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
       l[t] = 0.0f;
     }
 #pragma unroll
-    for (int dt = 0; dt < 8; dt++)
+    for (int dt = 0; dt < kDt; dt++)
 #pragma unroll
-      for (int t = 0; t < kHt; t++) o[dt][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int t = 0; t < kHt; t++) o[dt][t] = Tl::zero();
 
     // the request after this one, if the run goes on
     int s2 = s;
-    int64_t sx2 = sx;
+    uint32_t sx2 = sx;
     if (sx + ns < x1) {
       sx2 = sx + ns;
       do s2++;
       while (steps_of(a, s2) == 0);
     }
-    // the page of the step after, loaded a step ahead of its use
-    int next = step + 1 < last ? entry(s, step + 1) : s2 != s ? entry(s2, 0) : 0;
+    int ids2 = s2 != s ? entries(s2, 0) : 0;
+    asm volatile("" : "+v"(ids2));
+    const Src first2 = Src{__builtin_amdgcn_readfirstlane(ids2), 0};
+    // where the step after stands
+    Src next = step + 1 < last ? source(s, step + 1) : first2;
 
     for (; step < last; step++, x++, par ^= 1) {
       u32x4* lb = lds + par * kStepChunks;
       const char* buf = reinterpret_cast<const char*>(lb);
       dma_wait();
       // ---- rows that are not to be seen: past the request's end, or of no page
-      const int live = held(id) ? (int)min((int64_t)kLatStep, len - (int64_t)step * kLatStep) : 0;
+      const int live = held(at.id) ? (int)min((int64_t)kLatStep, len - (int64_t)step * kLatStep) : 0;
       __syncthreads();
       if (live < kLatStep) {
         for (int j = live * kRowChunks + tid; j < kStepChunks; j += kThreads) lb[j] = u32x4{0, 0, 0, 0};
         __syncthreads();
       }
-      id = next;
-      if (step + 1 < last) stage(id, step + 1, lds + (par ^ 1) * kStepChunks);
-      else if (s2 != s) stage(id, 0, lds + (par ^ 1) * kStepChunks);
-      if (step + 2 < last) next = entry(s, step + 2);
-      else if (step + 2 == last && s2 != s) next = entry(s2, 0);
+      at = next;
+      if (step + 1 < last || s2 != s) stage(at, lds + (par ^ 1) * kStepChunks);
+      next = step + 2 < last ? source(s, step + 2) : first2;
 
-      // ---- scores
-      f32x4 z[kTt][kHw];
+      // ---- scores: two sums, of even and of odd products
+      Acc z[kHw];
+      {
+        Acc z1[kHw];
 #pragma unroll
-      for (int t = 0; t < kTt; t++)
+        for (int u = 0; u < kHw; u++) z[u] = z1[u] = Tl::zero();
+        u32x4 op[kNk];
 #pragma unroll
-        for (int u = 0; u < kHw; u++) z[t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k = 0; k < kNk; k++) op[k] = *reinterpret_cast<const u32x4*>(buf + orow[k % kPk] + 128 * (k / kPk));
 #pragma unroll
-      for (int k = 0; k < kRow / 32; k++)
+        for (int k = 0; k < kNk; k++)
 #pragma unroll
-        for (int t = 0; t < kTt; t++) {
-          const bf16x8 op = as_bf16x8(*reinterpret_cast<const u32x4*>(buf + orow[t][k & 1] + 128 * (k >> 1)));
+          for (int u = 0; u < kHw; u++) {
+            if (k % 2) z1[u] = product(as_bf16x8(op[k]), as_bf16x8(qf[u][k]), z1[u]);
+            else z[u] = product(as_bf16x8(op[k]), as_bf16x8(qf[u][k]), z[u]);
+          }
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
-          for (int u = 0; u < kHw; u++) z[t][u] = mfma16(op, qf[u][k], z[t][u]);
+        for (int k = 0; k < kNk - kAhead; k++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, kHw, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_group_barrier(0x008, kHw * kAhead, 0);
+#pragma unroll
+        for (int u = 0; u < kHw; u++)
+#pragma unroll
+          for (int i = 0; i < Tl::kN; i++) z[u][i] = (z[u][i] + z1[u][i]) * c2;
+      }
       if (live < kLatStep) {
 #pragma unroll
-        for (int t = 0; t < kTt; t++)
+        for (int u = 0; u < kHw; u++)
 #pragma unroll
-          for (int u = 0; u < kHw; u++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-              if (16 * (kTt * wt + t) + 4 * g4 + i >= live) z[t][u][i] = -INFINITY;
+          for (int i = 0; i < Tl::kN; i++)
+            if (T * wt + Tl::row(i, g) >= live) z[u][i] = -INFINITY;
       }
-      // ---- weights under the running max
-      bool high = false;
+      // ---- weights under the running max, as bf16 into LDS; the lane's sums
+      float ts[kHw];
+      const auto weigh = [&]() {
 #pragma unroll
-      for (int u = 0; u < kHw; u++) {
-        float mx = -INFINITY;
+        for (int u = 0; u < kHw; u++) {
+          const float mu = m[u] == -INFINITY ? 0.0f : m[u];
+          ts[u] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < kTt; t++)
+          for (int i = 0; i < Tl::kN; i += 4) {
+            float p[4];
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            z[t][u][i] *= c2;
-            mx = fmaxf(mx, z[t][u][i]);
+            for (int j = 0; j < 4; j++) {
+              p[j] = __builtin_amdgcn_exp2f(z[u][i + j] - mu);
+              ts[u] += p[j];
+            }
+            *reinterpret_cast<uint2*>(&pl[(T * (kHw * wh + u) + c) * kPRow + T * wt + Tl::row(i, g)]) =
+                make_uint2(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
           }
-        high |= mx > m[u] + kMaxLog2;
-      }
+        }
+      };
+      weigh();
+      bool high = false;  // (a sum past the limit: a weight may be; a first step has no max yet)
+#pragma unroll
+      for (int u = 0; u < kHw; u++) high |= ts[u] > kMaxWeight || m[u] == -INFINITY;
       if (high) flag[par] = 1;
       __syncthreads();
-      const bool raise = flag[par] != 0;
-      if (raise) {
+      if (flag[par] != 0) {
         // the step's max of every head, over the waves that hold its tokens
 #pragma unroll
         for (int u = 0; u < kHw; u++) {
           float mx = -INFINITY;
 #pragma unroll
-          for (int t = 0; t < kTt; t++)
+          for (int i = 0; i < Tl::kN; i++) mx = fmaxf(mx, z[u][i]);
 #pragma unroll
-            for (int i = 0; i < 4; i++) mx = fmaxf(mx, z[t][u][i]);
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          if (g4 == 0) red[wt][16 * (kHw * wh + u) + c16] = fmaxf(mx, m[u]);
+          for (int d = T; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+          if (g == 0) red[wt][T * (kHw * wh + u) + c] = fmaxf(mx, m[u]);
         }
         __syncthreads();
-        // (every wave rescales its dims of all heads: the old max of a head is what all waves that
-        // score it hold; those of the other heads come through LDS as their ratio)
-        float mo[kHw];
+        float al[kHw];
 #pragma unroll
         for (int u = 0; u < kHw; u++) {
-          float mx = red[0][16 * (kHw * wh + u) + c16];
+          float mx = red[0][T * (kHw * wh + u) + c];
 #pragma unroll
-          for (int i = 1; i < kWt; i++) mx = fmaxf(mx, red[i][16 * (kHw * wh + u) + c16]);
-          mo[u] = m[u];
+          for (int i = 1; i < kWt; i++) mx = fmaxf(mx, red[i][T * (kHw * wh + u) + c]);
+          al[u] = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[u] - mx);
+          l[u] *= al[u];
           m[u] = mx;
         }
         __syncthreads();
+        // a wave rescales its dims of all heads: their ratios come from the waves that score them
 #pragma unroll
-        for (int u = 0; u < kHw; u++) {
-          const float al = m[u] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mo[u] - m[u]);
-          l[u] *= al;
-          if (wt == 0 && g4 == 0) red[0][16 * (kHw * wh + u) + c16] = al;
-        }
+        for (int u = 0; u < kHw; u++)
+          if (wt == 0 && g == 0) red[0][T * (kHw * wh + u) + c] = al[u];
+        weigh();
         __syncthreads();
+        if (tid == 0) flag[par] = 0;  // (read again two steps on, behind that step's barriers)
 #pragma unroll
         for (int t = 0; t < kHt; t++) {
-          const float al = red[0][16 * t + c16];
+          const float f = red[0][T * t + c];
 #pragma unroll
-          for (int dt = 0; dt < 8; dt++) o[dt][t] *= al;
+          for (int dt = 0; dt < kDt; dt++)
+#pragma unroll
+            for (int i = 0; i < Tl::kN; i++) o[dt][t][i] *= f;
         }
       }
 #pragma unroll
-      for (int u = 0; u < kHw; u++) {
-        const float mu = m[u] == -INFINITY ? 0.0f : m[u];
-#pragma unroll
-        for (int t = 0; t < kTt; t++) {
-          float p[4];
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            p[i] = __builtin_amdgcn_exp2f(z[t][u][i] - mu);
-            l[u] += p[i];
-          }
-          *reinterpret_cast<uint2*>(&pl[(16 * (kHw * wh + u) + c16) * kPRow + 16 * (kTt * wt + t) + 4 * g4]) =
-              make_uint2(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
-        }
-      }
-      __syncthreads();
-      if (tid == 0) flag[par] = 0;  // (read again two steps on, behind that step's barriers)
+      for (int u = 0; u < kHw; u++) l[u] += ts[u];
       // ---- values
+      {
+        s16x4 t0[kKs * kDt], t1[kKs * kDt];
+        bf16x8 pb[kKs * kHt];
 #pragma unroll
-      for (int ks = 0; ks < 2; ks++) {
-        bf16x8 pb[kHt];
+        for (int ks = 0; ks < kKs; ks++) {
 #pragma unroll
-        for (int t = 0; t < kHt; t++)
-          pb[t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(16 * t + c16) * kPRow + 32 * ks + 8 * g4]));
+          for (int t = 0; t < kHt; t++)
+            pb[ks * kHt + t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(T * t + c) * kPRow + Tl::kK * ks + 8 * g]));
 #pragma unroll
-        for (int dt = 0; dt < 8; dt++) {
-          const char* b = buf + 32 * ks * (kRowChunks * 16) + 128 * (dt >> 2);
-          const bf16x8 v = join16(tr16(b + otr[0][dt & 3]), tr16(b + otr[1][dt & 3]));
-#pragma unroll
-          for (int t = 0; t < kHt; t++) o[dt][t] = mfma16(v, pb[t], o[dt][t]);
+          for (int dt = 0; dt < kDt; dt++) {
+            const char* b = buf + Tl::kK * ks * (kRowChunks * 16) + 128 * (dt / kPd);
+            t0[ks * kDt + dt] = tr16(b + otr[0][dt % kPd]);
+            t1[ks * kDt + dt] = tr16(b + otr[1][dt % kPd]);
+          }
         }
+#pragma unroll
+        for (int y = 0; y < kKs * kDt; y++)
+#pragma unroll
+          for (int t = 0; t < kHt; t++)
+            o[y % kDt][t] = product(join16(t0[y], t1[y]), pb[y / kDt * kHt + t], o[y % kDt][t]);
+        constexpr int kReads = kKs * (2 * kDt + kHt), kPer = kReads / (kKs * kDt);
+        __builtin_amdgcn_sched_group_barrier(0x100, kReads - kPer * (kKs * kDt - kAhead / 2), 0);
+#pragma unroll
+        for (int y = 0; y < kKs * kDt - kAhead / 2; y++) {
+          __builtin_amdgcn_sched_group_barrier(0x008, kHt, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kHt * kAhead / 2, 0);
       }
     }
 
     // ------------------------------------------------- the request's result
     // sums of the weights, over the lanes and waves that hold a head's tokens; and its max
     __syncthreads();
+    float* mrow = reinterpret_cast<float*>(pl);
 #pragma unroll
     for (int u = 0; u < kHw; u++) {
       float y = l[u];
-      y += __shfl_xor(y, 16, 64);
-      y += __shfl_xor(y, 32, 64);
-      if (g4 == 0) red[wt][16 * (kHw * wh + u) + c16] = y;
-    }
-    float* mrow = reinterpret_cast<float*>(pl);
 #pragma unroll
-    for (int u = 0; u < kHw; u++)
-      if (wt == 0 && g4 == 0) mrow[16 * (kHw * wh + u) + c16] = m[u];
+      for (int d = T; d < 64; d <<= 1) y += __shfl_xor(y, d, 64);
+      if (g == 0) red[wt][T * (kHw * wh + u) + c] = y;
+      if (g == 0 && wt == 0) mrow[T * (kHw * wh + u) + c] = m[u];
+    }
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < kHt; t++) {
-      const int hl = 16 * t + c16, h = h0 + hl;
+      const int hl = T * t + c, h = h0 + hl;
       float lt = red[0][hl];
 #pragma unroll
       for (int i = 1; i < kWt; i++) lt += red[i][hl];
       const float mt = mrow[hl];
       if (h < a.H) {
+        const int d0 = 128 * wave;
         if (whole) {
           const float inv = lt > 0.0f || lt != lt ? 1.0f / lt : 0.0f;  // (nothing attended: 0; NaN stays)
-          __hip_bfloat16* dst = a.out + (int64_t)s * a.o_ss + (int64_t)h * a.o_sh + 128 * wave + 4 * g4;
+          __hip_bfloat16* dst = a.out + (int64_t)s * a.o_ss + (int64_t)h * a.o_sh + d0;
 #pragma unroll
-          for (int dt = 0; dt < 8; dt++)
-            *reinterpret_cast<uint2*>(dst + 16 * dt) =
-                make_uint2(pack_bf16(o[dt][t][0] * inv, o[dt][t][1] * inv), pack_bf16(o[dt][t][2] * inv, o[dt][t][3] * inv));
-          if (wave == 0 && g4 == 0) a.lse[(int64_t)h * a.S + s] = (mt + __builtin_amdgcn_logf(lt)) * kLn2;
+          for (int dt = 0; dt < kDt; dt++)
+#pragma unroll
+            for (int i = 0; i < Tl::kN; i += 4)
+              *reinterpret_cast<uint2*>(dst + T * dt + Tl::row(i, g)) =
+                  make_uint2(pack_bf16(o[dt][t][i] * inv, o[dt][t][i + 1] * inv),
+                             pack_bf16(o[dt][t][i + 2] * inv, o[dt][t][i + 3] * inv));
+          if (wave == 0 && g == 0) a.lse[(int64_t)h * a.S + s] = (mt + __builtin_amdgcn_logf(lt)) * kLn2;
         } else {
-          float* dst = a.part_o + (pslot * M + hl) * kRank + 128 * wave + 4 * g4;
+          float* dst = a.part_o + (pslot * M + hl) * kRank + d0;
 #pragma unroll
-          for (int dt = 0; dt < 8; dt++) *reinterpret_cast<f32x4*>(dst + 16 * dt) = o[dt][t];
-          if (wave == 0 && g4 == 0) a.part_ml[pslot * M + hl] = make_float2(mt, lt);
+          for (int dt = 0; dt < kDt; dt++)
+#pragma unroll
+            for (int i = 0; i < Tl::kN; i += 4)
+              *reinterpret_cast<f32x4*>(dst + T * dt + Tl::row(i, g)) =
+                  f32x4{o[dt][t][i], o[dt][t][i + 1], o[dt][t][i + 2], o[dt][t][i + 3]};
+          if (wave == 0 && g == 0) a.part_ml[pslot * M + hl] = make_float2(mt, lt);
         }
       }
     }
@@ -380,56 +476,83 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     s = s2;
     sx = sx2;
     step = 0;
+    p0 = 0;
+    ids = ids2;
   }
 }
 
-// Joins a request's partials, in the order of its steps: a work-group per (request, head), two dims a
-// thread.  Requests of one run are finished already; empty ones get 0 and -inf here.
+// Joins a request's partials, in the order of its steps: a work-group per (request, head).  Its four quarters sum a
+// quarter of the partials each, four dims a thread, and are added up in order.  Requests of one run are finished
+// already; empty ones get 0 and -inf here.
+constexpr int kJoinThreads = 512, kJoinLanes = kRank / 4, kJoinParts = kJoinThreads / kJoinLanes;
 template <int M>
-__global__ __launch_bounds__(256) void latent_join_kernel(LatentDecodeArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void latent_join_kernel(LatentDecodeArgs a) {
+  __shared__ float2 ml[kLatGroups + 2];  // of every partial: its factor and sum
+  __shared__ f32x4 part[kJoinParts][kJoinLanes];
+  __shared__ float wave_max[kJoinThreads / 64];
   const int s = (int)(blockIdx.x / (uint32_t)a.H), h = (int)(blockIdx.x % (uint32_t)a.H);
-  const int d = 2 * threadIdx.x;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + (int64_t)s * a.o_ss + (int64_t)h * a.o_sh + d);
+  const int tid = threadIdx.x, lane = tid % kJoinLanes, p = tid / kJoinLanes;
+  uint2* dst = reinterpret_cast<uint2*>(a.out + (int64_t)s * a.o_ss + (int64_t)h * a.o_sh) + lane;
   const int ns = steps_of(a, s);
   if (ns == 0) {
-    *dst = 0;
-    if (threadIdx.x == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
+    if (p == 0) *dst = make_uint2(0, 0);
+    if (tid == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
     return;
   }
-  const int64_t total = a.first[a.S], y0 = a.first[s], y1 = y0 + ns;
-  // share w holds steps [total w / shares, ...): the one of step y is the last whose run begins at or before
-  // y and is not empty
-  const auto share_of = [&](int64_t y) {
-    int64_t w = y * a.shares / total;
-    while (run_begin(total, w + 1, a.shares) <= y) w++;
-    while (run_begin(total, w, a.shares) > y) w--;
-    return (int)w;
-  };
-  const int w0 = share_of(y0), w1 = share_of(y1 - 1);
+  const Runs runs(a.first[a.S], a.shares);
+  const uint32_t y0 = a.first[s];
+  const int w0 = (int)runs.share(y0), w1 = (int)runs.share(y0 + ns - 1);
   if (w0 == w1) return;  // finished by its work-group
-  const int hg = h / M, hl = h % M;
-  const auto slot = [&](int w) {
-    const int second = run_begin(total, w, a.shares) < y0;  // the run began with another request
-    return (((int64_t)w * 2 + second) * a.groups + hg) * M + hl;
-  };
-  float m = -INFINITY;
-  for (int w = w0; w <= w1; w++)
-    if (run_begin(total, w, a.shares) < run_begin(total, w + 1, a.shares)) m = fmaxf(m, a.part_ml[slot(w)].x);
+  const int n = w1 - w0 + 1, hg = h / M, hl = h % M;
+  // the first partial may be a run's second one: the run began with another request
+  const int64_t stride = (int64_t)2 * a.groups * M;
+  const int64_t row0 = ((int64_t)w0 * 2 * a.groups + hg) * M + hl;
+  const int64_t first = row0 + (runs.begin(w0) < y0 ? (int64_t)a.groups * M : 0);
+  const auto row = [&](int i) { return i == 0 ? first : row0 + i * stride; };
+  float mx = -INFINITY;
+  float2 v = make_float2(-INFINITY, 0.0f);
+  const bool mine = tid < n;
+  if (mine) v = a.part_ml[row(tid)];
+  mx = v.x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+  if (tid % 64 == 0) wave_max[tid / 64] = mx;
+  __syncthreads();
+  float m = wave_max[0];
+#pragma unroll
+  for (int i = 1; i < kJoinThreads / 64; i++) m = fmaxf(m, wave_max[i]);
   const float mu = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int w = w0; w <= w1; w++) {
-    if (run_begin(total, w, a.shares) >= run_begin(total, w + 1, a.shares)) continue;
-    const int64_t at = slot(w);
-    const float2 ml = a.part_ml[at];
-    const float f = __builtin_amdgcn_exp2f(ml.x - mu);
-    const float2 x = *reinterpret_cast<const float2*>(a.part_o + at * kRank + d);
-    l = fmaf(ml.y, f, l);
-    o0 = fmaf(x.x, f, o0);
-    o1 = fmaf(x.y, f, o1);
+  if (tid < n) ml[tid] = make_float2(__builtin_amdgcn_exp2f(v.x - mu), v.y);
+  __syncthreads();
+  const int per = (n + kJoinParts - 1) / kJoinParts, i0 = p * per, i1 = min(n, i0 + per);
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = i0; i < i1; i += 8) {
+    f32x4 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) x[j] = reinterpret_cast<const f32x4*>(a.part_o + row(min(i + j, i1 - 1)) * kRank)[lane];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+      const float f = ml[min(i + j, i1 - 1)].x;
+#pragma unroll
+      for (int e = 0; e < 4; e++) acc[e] = i + j < i1 ? fmaf(x[j][e], f, acc[e]) : acc[e];
+    }
   }
+  part[p][lane] = acc;
+  float l = 0.0f;
+  if (tid < 64) {
+    for (int i = tid; i < n; i += 64) l = fmaf(ml[i].x, ml[i].y, l);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
+    if (tid == 0) wave_max[0] = l;
+  }
+  __syncthreads();
+  if (p != 0) return;
+  l = wave_max[0];
+#pragma unroll
+  for (int i = 1; i < kJoinParts; i++) acc += part[i][lane];
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  *dst = pack_bf16(o0 * inv, o1 * inv);
-  if (threadIdx.x == 0) a.lse[(int64_t)h * a.S + s] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  *dst = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+  if (tid == 0) a.lse[(int64_t)h * a.S + s] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <int M>
@@ -441,7 +564,7 @@ hipError_t decode(const LatentDecodeArgs& a, hipStream_t st) {
 
 template <int M>
 hipError_t join(const LatentDecodeArgs& a, hipStream_t st) {
-  latent_join_kernel<M><<<(unsigned)((int64_t)a.S * a.H), 256, 0, st>>>(a);
+  latent_join_kernel<M><<<(unsigned)((int64_t)a.S * a.H), kJoinThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -65,7 +65,7 @@ struct LatentDecodeArgs {
   // workspace
   float* part_o;     // [shares, 2, groups, heads of a group, 512]: unnormalised partials
   float2* part_ml;   // [shares, 2, groups, heads of a group]: their max (log2 domain) and sum
-  int64_t* first;    // [S + 1]: the batch's step at which a request begins; the batch's steps
+  uint32_t* first;   // [S + 1]: the batch's step at which a request begins; the batch's steps
 };
 // heads: of a group, 16, 32 or 64
 hipError_t launch_latent_decode(int heads, const LatentDecodeArgs& a, hipStream_t st);

@@ -333,8 +333,8 @@ def test_workspaces():
     # two partials of a group's heads (512 sums, max and sum) a share, at most as many as steps; the requests'
     # first steps
     pad = lambda n: (n + 15) // 16 * 16  # noqa: E731
-    assert need(3, 4, 8, 64) == 12 * 2 * 16 * (512 * 4 + 8) + pad(8 * 4)
-    assert need(1, 1 << 14, 128, 64) == 128 * 2 * 2 * 64 * (512 * 4 + 8) + pad(8 * 2)
+    assert need(3, 4, 8, 64) == 12 * 2 * 16 * (512 * 4 + 8) + pad(4 * 4)
+    assert need(1, 1 << 14, 128, 64) == 128 * 2 * 2 * 64 * (512 * 4 + 8) + pad(4 * 2)
     back = binding.latent_backward_workspace_bytes
     assert back(0, 3) == back(5, 0) == back(1 << 28, 1) == back(2 ** 40, 1) == 0
     assert back(100, 3) == 300 * (8 + 64 * 4)
