@@ -35,7 +35,9 @@ constexpr int kDma = kStepChunks / (64 * kWaves);      // DMA instructions a wav
 constexpr int kPRow = kLatStep + 8;                    // bf16 of a head's row of P (padded)
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kMaxWeight = 256.0f;
-constexpr int kAhead = 8;                              // operand reads ahead of their products
+constexpr int kInAcc = 62;                             // 16-byte operands of the queries in accumulation registers
+constexpr int kDmaFirst = 13;                          // DMA instructions beside the first product
+constexpr int kAhead = 6;                              // operand reads ahead of their products
 
 // The 72 chunks of a row: two rows to the bank period, as swz_slim in latent_tile.h has it, in
 // groups of 8 chunks.
@@ -89,30 +91,35 @@ struct Runs {
   }
 };
 
+// dma16_at with the LDS address in a scalar register.
+__device__ __forceinline__ void dma16_to(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "{m0}"(to) : "memory");
+}
+
 template <int M>
 __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecodeArgs a) {
+  // first product: a wave scores 16 tokens for all heads, tiles of 16 x 16
+  using S = Tile<16>;
+  constexpr int kHs = M / 16;                    // head tiles
+  constexpr int kNk = kRow / S::kK;              // products of a score
+  static_assert(kNk == kDma, "a DMA instruction goes out beside each product");
+  // second product: a wave sums 128 dims of all heads, tiles of T x T
   constexpr int T = M == 64 ? 32 : 16;
-  using Tl = Tile<T>;
-  using Acc = typename Tl::Acc;
-  constexpr int kHt = M / T;                     // head tiles of the group
-  constexpr int kWh = M == 64 ? 2 : 1;           // waves over heads in the first product
-  constexpr int kWt = kWaves / kWh;              // and over tokens
-  constexpr int kTt = kLatStep / T / kWt, kHw = kHt / kWh;  // token and head tiles of a wave
-  static_assert(kTt == 1, "a wave scores one tile of tokens");
-  constexpr int kNk = kRow / Tl::kK;             // terms of a score, in products
-  constexpr int kPk = T / 8;                     // of them, those of 8 chunks (2 or 4)
+  using V = Tile<T>;
+  using Acc = typename V::Acc;
+  constexpr int kHt = M / T;                     // head tiles
   constexpr int kDt = 128 / T, kPd = 64 / T;     // dim tiles of a wave; those of 8 chunks (4 or 2)
-  constexpr int kKs = kLatStep / Tl::kK;         // products over a step's tokens
+  constexpr int kKs = kLatStep / V::kK;          // products over a step's tokens
   __shared__ u32x4 lds[2 * kStepChunks];
   __shared__ __align__(16) __hip_bfloat16 pl[M * kPRow];
-  __shared__ float red[kWt][M];
+  __shared__ float red[kWaves][M];
   __shared__ int flag[2];
   __shared__ uint32_t scan[kWaves + 1];
   __shared__ int begin_s;
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c = lane % T, g = lane / T;
-  const int wt = wave % kWt, wh = wave / kWt;
+  const int cs = lane % 16, gs = lane / 16;  // lane's place in a tile of the first product
+  const int c = lane % T, g = lane / T;      // and of the second
 
   // work-groups go round-robin to the 8 XCDs: those of one run sit on one of them
   const int per = 8 * a.groups;
@@ -199,18 +206,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     return Src{__builtin_amdgcn_readlane(ids, pg - p0), (int)((uint32_t)step_ - pg * tp)};
   };
   const auto held = [&](int id) { return id >= 0 && id < a.N; };
-  const auto stage = [&](const Src& x_, u32x4* buf) {
-    // (where there is no page its rows are cleared before they are used)
-    const char* src = scalar_ptr(a.pages + (held(x_.id) ? (int64_t)x_.id : 0) * a.p_sp + x_.at * (kLatStep * kRow));
-#pragma unroll
-    for (int x = 0; x < kDma; x++)
-      dma16_at(src + (x / (kDma / 2)) * (kLatStep / 2 * kRow * 2), doff[x % (kDma / 2)],
-               buf + 64 * (wave + kWaves * x));
+  const auto origin = [&](const Src& x_) {  // (where there is no page its rows are cleared before they are used)
+    return scalar_ptr(a.pages + (held(x_.id) ? (int64_t)x_.id : 0) * a.p_sp + x_.at * (kLatStep * kRow));
   };
-  // row operand: row T wt + c, chunk (64 / T) k + g at orow[k % kPk] + 128 (k / kPk)
-  uint32_t orow[kPk];
+  // DMA instruction x of a step whose rows begin at src; where mask is 0, of one 16-byte piece for all lanes
+  const auto stage = [&](int x, const char* src, uint32_t to, uint32_t mask) {
+    dma16_to(src + (x / (kDma / 2)) * (kLatStep / 2 * kRow * 2), doff[x % (kDma / 2)] & mask, to + kWaves * 1024 * x);
+  };
+  // where this wave's DMA begins in each buffer
+  const uint32_t to0 = lds_addr(lds) + 1024 * wave, to1 = to0 + kStepChunks * 16;
+  // row operand: row 16 wave + cs, chunk 4 k + gs at orow[k % 2] + 128 (k / 2)
+  uint32_t orow[2];
 #pragma unroll
-  for (int k = 0; k < kPk; k++) orow[k] = at_row(T * wt + c, (64 / T) * k + g);
+  for (int k = 0; k < 2; k++) orow[k] = at_row(16 * wave + cs, 4 * k + gs);
   // transposed: lane's group g holds tokens kK ks + 8 g + 4 x + (0 .. 3) of dim T dt + c of the
   // wave's: otr[x][dt % kPd] + 128 (dt / kPd)
   uint32_t otr[2][kPd];
@@ -227,42 +235,59 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
   p0 = (uint32_t)step / tp;
   ids = entries(s, p0);
   Src at = source(s, step);  // where the staged step stands
-  stage(at, lds);
+  {
+    const char* src = origin(at);
+#pragma unroll
+    for (int x = 0; x < kDma; x++) stage(x, src, to0, ~0u);
+  }
   for (uint32_t x = x0; x < x1;) {
     // ---------------------------------------------------------- one request
-    const int64_t len = min((int64_t)a.lens[s], (int64_t)a.W * a.P);
-    const int ns = steps_of(a, s);
+    const int len = __builtin_amdgcn_readfirstlane((int)min((int64_t)a.lens[s], (int64_t)a.W * a.P));
+    const int ns = (int)(((uint32_t)len + kLatStep - 1) / kLatStep);
     const int last = (int)min((uint32_t)ns, x1 - sx);  // steps step .. last - 1 are the run's
     const bool whole = step == 0 && last == ns;
     const int64_t pslot = ((int64_t)w * 2 + (x == x0 ? 0 : 1)) * a.groups + hg;
-    u32x4 qf[kHw][kNk];
+    // the queries of the group's heads, through the buffer that no step is staged in, as 64 rows
+    u32x4* lq = lds + (par ^ 1) * kStepChunks;
+    {
+      const __hip_bfloat16* qc = a.qc + (int64_t)s * a.qc_ss;
+      const __hip_bfloat16* qr = a.qr + (int64_t)s * a.qr_ss;
+      int ln = lane;
+      asm volatile("" : "+v"(ln));  // (else the places below are held in registers for the whole run)
 #pragma unroll
-    for (int t = 0; t < kHw; t++) {
-      const int h = min(h0 + T * (kHw * wh + t) + c, a.H - 1);
-      const __hip_bfloat16* qc = a.qc + (int64_t)s * a.qc_ss + (int64_t)h * a.qc_sh + 8 * g;
-      const __hip_bfloat16* qr = a.qr + (int64_t)s * a.qr_ss + (int64_t)h * a.qr_sh + 8 * g;
-#pragma unroll
-      for (int k = 0; k < kNk; k++)
-        qf[t][k] = *reinterpret_cast<const u32x4*>(
-            k < kRank / Tl::kK ? qc + Tl::kK * k : qr + Tl::kK * (k - kRank / Tl::kK));
+      for (int x0_ = 0; x0_ < (M * kRowChunks / 64 + kWaves - 1) / kWaves; x0_++) {
+        const int j = wave + kWaves * x0_;
+        if (j >= M * kRowChunks / 64) break;
+        const int y = 64 * j + ln, r = y / kRowChunks, ch = (y % kRowChunks) ^ swz_slim(r);
+        const int64_t h = min(h0 + r, a.H - 1);
+        dma16(ch < kRank / 8 ? qc + h * a.qc_sh + 8 * ch : qr + h * a.qr_sh + 8 * (ch - kRank / 8), lq + 64 * j);
+      }
+      dma_wait();
+      __syncthreads();
     }
-    // (into the accumulation registers, where the matrix cores read them as well as anywhere: the
-    // others are full)
+    // Into the accumulation registers, where the matrix cores read them as well as anywhere, as many as
+    // those hold (the others are full); a few at a time, which is all that fits on the way.
+    u32x4 qf[kHs][kNk];
 #pragma unroll
-    for (int t = 0; t < kHw; t++)
-#pragma unroll
-      for (int k = 0; k < kNk; k++) asm volatile("" : "+a"(qf[t][k]));
+    for (int y = 0; y < kHs * kNk; y++) {
+      const int t = y / kNk, k = y % kNk;
+      qf[t][k] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(lq) + at_row(16 * t + cs, 4 * (k % 2) + gs) +
+                                                 128 * (k / 2));
+      if (y < kInAcc) asm volatile("" : "+a"(qf[t][k]));
+      if (y % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();  // (the next step is staged there)
     Acc o[kDt][kHt];
-    float m[kHw], l[kHw];
+    float m[kHs], l[kHs];
 #pragma unroll
-    for (int t = 0; t < kHw; t++) {
+    for (int t = 0; t < kHs; t++) {
       m[t] = -INFINITY;
       l[t] = 0.0f;
     }
 #pragma unroll
     for (int dt = 0; dt < kDt; dt++)
 #pragma unroll
-      for (int t = 0; t < kHt; t++) o[dt][t] = Tl::zero();
+      for (int t = 0; t < kHt; t++) o[dt][t] = V::zero();
 
     // the request after this one, if the run goes on
     int s2 = s;
@@ -270,7 +295,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     if (sx + ns < x1) {
       sx2 = sx + ns;
       do s2++;
-      while (steps_of(a, s2) == 0);
+      while (__builtin_amdgcn_readfirstlane(steps_of(a, s2)) == 0);
     }
     int ids2 = s2 != s ? entries(s2, 0) : 0;
     asm volatile("" : "+v"(ids2));
@@ -283,104 +308,97 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
       const char* buf = reinterpret_cast<const char*>(lb);
       dma_wait();
       // ---- rows that are not to be seen: past the request's end, or of no page
-      const int live = held(at.id) ? (int)min((int64_t)kLatStep, len - (int64_t)step * kLatStep) : 0;
+      const int live = held(at.id) ? min(kLatStep, len - step * kLatStep) : 0;
       __syncthreads();
       if (live < kLatStep) {
         for (int j = live * kRowChunks + tid; j < kStepChunks; j += kThreads) lb[j] = u32x4{0, 0, 0, 0};
         __syncthreads();
       }
       at = next;
-      if (step + 1 < last || s2 != s) stage(at, lds + (par ^ 1) * kStepChunks);
+      // the next step's DMA goes out piece by piece, between the products: 18 at once would hold the wave up for
+      // as long as all products take
+      const char* src = origin(at);
+      const uint32_t to = par ? to0 : to1;
+      // (with no step to come they fetch next to nothing, into a buffer that nothing reads)
+      const uint32_t on = step + 1 < last || s2 != s ? ~0u : 0;
       next = step + 2 < last ? source(s, step + 2) : first2;
 
-      // ---- scores: two sums, of even and of odd products
-      Acc z[kHw];
+      // ---- scores
+      f32x4 z[kHs];
       {
-        Acc z1[kHw];
 #pragma unroll
-        for (int u = 0; u < kHw; u++) z[u] = z1[u] = Tl::zero();
+        for (int u = 0; u < kHs; u++) z[u] = S::zero();
         u32x4 op[kNk];
+        const auto fetch = [&](int k) { op[k] = *reinterpret_cast<const u32x4*>(buf + orow[k % 2] + 128 * (k / 2)); };
 #pragma unroll
-        for (int k = 0; k < kNk; k++) op[k] = *reinterpret_cast<const u32x4*>(buf + orow[k % kPk] + 128 * (k / kPk));
+        for (int k = 0; k < kAhead; k++) fetch(k);
 #pragma unroll
-        for (int k = 0; k < kNk; k++)
+        for (int k = 0; k < kNk; k++) {
 #pragma unroll
-          for (int u = 0; u < kHw; u++) {
-            if (k % 2) z1[u] = product(as_bf16x8(op[k]), as_bf16x8(qf[u][k]), z1[u]);
-            else z[u] = product(as_bf16x8(op[k]), as_bf16x8(qf[u][k]), z[u]);
-          }
-        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
-#pragma unroll
-        for (int k = 0; k < kNk - kAhead; k++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, kHw, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          for (int u = 0; u < kHs; u++) z[u] = product(as_bf16x8(op[k]), as_bf16x8(qf[u][k]), z[u]);
+          if (k + kAhead < kNk) fetch(k + kAhead);
+          if (k < kDmaFirst) stage(k, src, to, on);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, kHw * kAhead, 0);
 #pragma unroll
-        for (int u = 0; u < kHw; u++)
+        for (int u = 0; u < kHs; u++)
 #pragma unroll
-          for (int i = 0; i < Tl::kN; i++) z[u][i] = (z[u][i] + z1[u][i]) * c2;
+          for (int i = 0; i < 4; i++) z[u][i] *= c2;
       }
       if (live < kLatStep) {
 #pragma unroll
-        for (int u = 0; u < kHw; u++)
+        for (int u = 0; u < kHs; u++)
 #pragma unroll
-          for (int i = 0; i < Tl::kN; i++)
-            if (T * wt + Tl::row(i, g) >= live) z[u][i] = -INFINITY;
+          for (int i = 0; i < 4; i++)
+            if (16 * wave + S::row(i, gs) >= live) z[u][i] = -INFINITY;
       }
       // ---- weights under the running max, as bf16 into LDS; the lane's sums
-      float ts[kHw];
+      float ts[kHs];
       const auto weigh = [&]() {
 #pragma unroll
-        for (int u = 0; u < kHw; u++) {
+        for (int u = 0; u < kHs; u++) {
           const float mu = m[u] == -INFINITY ? 0.0f : m[u];
+          float p[4];
           ts[u] = 0.0f;
 #pragma unroll
-          for (int i = 0; i < Tl::kN; i += 4) {
-            float p[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-              p[j] = __builtin_amdgcn_exp2f(z[u][i + j] - mu);
-              ts[u] += p[j];
-            }
-            *reinterpret_cast<uint2*>(&pl[(T * (kHw * wh + u) + c) * kPRow + T * wt + Tl::row(i, g)]) =
-                make_uint2(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
+          for (int j = 0; j < 4; j++) {
+            p[j] = __builtin_amdgcn_exp2f(z[u][j] - mu);
+            ts[u] += p[j];
           }
+          *reinterpret_cast<uint2*>(&pl[(16 * u + cs) * kPRow + 16 * wave + 4 * gs]) =
+              make_uint2(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]));
         }
       };
       weigh();
       bool high = false;  // (a sum past the limit: a weight may be; a first step has no max yet)
 #pragma unroll
-      for (int u = 0; u < kHw; u++) high |= ts[u] > kMaxWeight || m[u] == -INFINITY;
+      for (int u = 0; u < kHs; u++) high |= ts[u] > kMaxWeight || m[u] == -INFINITY;
       if (high) flag[par] = 1;
       __syncthreads();
       if (flag[par] != 0) {
-        // the step's max of every head, over the waves that hold its tokens
+        // the step's max of every head, over the waves
 #pragma unroll
-        for (int u = 0; u < kHw; u++) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < Tl::kN; i++) mx = fmaxf(mx, z[u][i]);
-#pragma unroll
-          for (int d = T; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-          if (g == 0) red[wt][T * (kHw * wh + u) + c] = fmaxf(mx, m[u]);
+        for (int u = 0; u < kHs; u++) {
+          float mx = fmaxf(fmaxf(z[u][0], z[u][1]), fmaxf(z[u][2], z[u][3]));
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          if (gs == 0) red[wave][16 * u + cs] = fmaxf(mx, m[u]);
         }
         __syncthreads();
-        float al[kHw];
+        float al[kHs];
 #pragma unroll
-        for (int u = 0; u < kHw; u++) {
-          float mx = red[0][T * (kHw * wh + u) + c];
+        for (int u = 0; u < kHs; u++) {
+          float mx = red[0][16 * u + cs];
 #pragma unroll
-          for (int i = 1; i < kWt; i++) mx = fmaxf(mx, red[i][T * (kHw * wh + u) + c]);
+          for (int i = 1; i < kWaves; i++) mx = fmaxf(mx, red[i][16 * u + cs]);
           al[u] = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[u] - mx);
           l[u] *= al[u];
           m[u] = mx;
         }
         __syncthreads();
-        // a wave rescales its dims of all heads: their ratios come from the waves that score them
+        // (the sums' tiles hold other heads a lane: the ratios go through LDS)
 #pragma unroll
-        for (int u = 0; u < kHw; u++)
-          if (wt == 0 && g == 0) red[0][T * (kHw * wh + u) + c] = al[u];
+        for (int u = 0; u < kHs; u++)
+          if (wave == 0 && gs == 0) red[0][16 * u + cs] = al[u];
         weigh();
         __syncthreads();
         if (tid == 0) flag[par] = 0;  // (read again two steps on, behind that step's barriers)
@@ -390,40 +408,36 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 #pragma unroll
           for (int dt = 0; dt < kDt; dt++)
 #pragma unroll
-            for (int i = 0; i < Tl::kN; i++) o[dt][t][i] *= f;
+            for (int i = 0; i < V::kN; i++) o[dt][t][i] *= f;
         }
       }
 #pragma unroll
-      for (int u = 0; u < kHw; u++) l[u] += ts[u];
+      for (int u = 0; u < kHs; u++) l[u] += ts[u];
       // ---- values
       {
-        s16x4 t0[kKs * kDt], t1[kKs * kDt];
+        constexpr int kY = kKs * kDt;
+        s16x4 t0[kY], t1[kY];
         bf16x8 pb[kKs * kHt];
+        const auto fetch = [&](int y) {
+          const int ks = y / kDt, dt = y % kDt;
+          if (dt == 0) {
 #pragma unroll
-        for (int ks = 0; ks < kKs; ks++) {
-#pragma unroll
-          for (int t = 0; t < kHt; t++)
-            pb[ks * kHt + t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(T * t + c) * kPRow + Tl::kK * ks + 8 * g]));
-#pragma unroll
-          for (int dt = 0; dt < kDt; dt++) {
-            const char* b = buf + Tl::kK * ks * (kRowChunks * 16) + 128 * (dt / kPd);
-            t0[ks * kDt + dt] = tr16(b + otr[0][dt % kPd]);
-            t1[ks * kDt + dt] = tr16(b + otr[1][dt % kPd]);
+            for (int t = 0; t < kHt; t++)
+              pb[ks * kHt + t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(T * t + c) * kPRow + V::kK * ks + 8 * g]));
           }
+          const char* b = buf + V::kK * ks * (kRowChunks * 16) + 128 * (dt / kPd);
+          t0[y] = tr16(b + otr[0][dt % kPd]);
+          t1[y] = tr16(b + otr[1][dt % kPd]);
+        };
+#pragma unroll
+        for (int y = 0; y < kAhead / 2; y++) fetch(y);
+#pragma unroll
+        for (int y = 0; y < kY; y++) {
+#pragma unroll
+          for (int t = 0; t < kHt; t++) o[y % kDt][t] = product(join16(t0[y], t1[y]), pb[y / kDt * kHt + t], o[y % kDt][t]);
+          if (y + kAhead / 2 < kY) fetch(y + kAhead / 2);
+          if (y < kDma - kDmaFirst) stage(kDmaFirst + y, src, to, on);
         }
-#pragma unroll
-        for (int y = 0; y < kKs * kDt; y++)
-#pragma unroll
-          for (int t = 0; t < kHt; t++)
-            o[y % kDt][t] = product(join16(t0[y], t1[y]), pb[y / kDt * kHt + t], o[y % kDt][t]);
-        constexpr int kReads = kKs * (2 * kDt + kHt), kPer = kReads / (kKs * kDt);
-        __builtin_amdgcn_sched_group_barrier(0x100, kReads - kPer * (kKs * kDt - kAhead / 2), 0);
-#pragma unroll
-        for (int y = 0; y < kKs * kDt - kAhead / 2; y++) {
-          __builtin_amdgcn_sched_group_barrier(0x008, kHt, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, kPer, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, kHt * kAhead / 2, 0);
       }
     }
 
@@ -432,12 +446,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     __syncthreads();
     float* mrow = reinterpret_cast<float*>(pl);
 #pragma unroll
-    for (int u = 0; u < kHw; u++) {
+    for (int u = 0; u < kHs; u++) {
       float y = l[u];
-#pragma unroll
-      for (int d = T; d < 64; d <<= 1) y += __shfl_xor(y, d, 64);
-      if (g == 0) red[wt][T * (kHw * wh + u) + c] = y;
-      if (g == 0 && wt == 0) mrow[T * (kHw * wh + u) + c] = m[u];
+      y += __shfl_xor(y, 16, 64);
+      y += __shfl_xor(y, 32, 64);
+      if (gs == 0) red[wave][16 * u + cs] = y;
+      if (gs == 0 && wave == 0) mrow[16 * u + cs] = m[u];
     }
     __syncthreads();
 #pragma unroll
@@ -445,7 +459,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
       const int hl = T * t + c, h = h0 + hl;
       float lt = red[0][hl];
 #pragma unroll
-      for (int i = 1; i < kWt; i++) lt += red[i][hl];
+      for (int i = 1; i < kWaves; i++) lt += red[i][hl];
       const float mt = mrow[hl];
       if (h < a.H) {
         const int d0 = 128 * wave;
@@ -455,18 +469,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 #pragma unroll
           for (int dt = 0; dt < kDt; dt++)
 #pragma unroll
-            for (int i = 0; i < Tl::kN; i += 4)
-              *reinterpret_cast<uint2*>(dst + T * dt + Tl::row(i, g)) =
+            for (int i = 0; i < V::kN; i += 4)
+              *reinterpret_cast<uint2*>(dst + T * dt + V::row(i, g)) =
                   make_uint2(pack_bf16(o[dt][t][i] * inv, o[dt][t][i + 1] * inv),
                              pack_bf16(o[dt][t][i + 2] * inv, o[dt][t][i + 3] * inv));
           if (wave == 0 && g == 0) a.lse[(int64_t)h * a.S + s] = (mt + __builtin_amdgcn_logf(lt)) * kLn2;
         } else {
-          float* dst = a.part_o + (pslot * M + hl) * kRank + d0;
+          // as the lanes hold it
+          f32x4* dst = reinterpret_cast<f32x4*>(a.part_o) + pslot * (M * kRank / 4) + lane;
 #pragma unroll
           for (int dt = 0; dt < kDt; dt++)
 #pragma unroll
-            for (int i = 0; i < Tl::kN; i += 4)
-              *reinterpret_cast<f32x4*>(dst + T * dt + Tl::row(i, g)) =
+            for (int i = 0; i < V::kN; i += 4)
+              dst[(((wave * kDt + dt) * kHt + t) * (V::kN / 4) + i / 4) * 64] =
                   f32x4{o[dt][t][i], o[dt][t][i + 1], o[dt][t][i + 2], o[dt][t][i + 3]};
           if (wave == 0 && g == 0) a.part_ml[pslot * M + hl] = make_float2(mt, lt);
         }
@@ -479,80 +494,94 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     p0 = 0;
     ids = ids2;
   }
+  dma_wait();  // (LDS is another work-group's after the end)
 }
 
-// Joins a request's partials, in the order of its steps: a work-group per (request, head).  Its four quarters sum a
-// quarter of the partials each, four dims a thread, and are added up in order.  Requests of one run are finished
-// already; empty ones get 0 and -inf here.
-constexpr int kJoinThreads = 512, kJoinLanes = kRank / 4, kJoinParts = kJoinThreads / kJoinLanes;
-template <int M>
-__global__ __launch_bounds__(kJoinThreads) void latent_join_kernel(LatentDecodeArgs a) {
-  __shared__ float2 ml[kLatGroups + 2];  // of every partial: its factor and sum
-  __shared__ f32x4 part[kJoinParts][kJoinLanes];
-  __shared__ float wave_max[kJoinThreads / 64];
-  const int s = (int)(blockIdx.x / (uint32_t)a.H), h = (int)(blockIdx.x % (uint32_t)a.H);
-  const int tid = threadIdx.x, lane = tid % kJoinLanes, p = tid / kJoinLanes;
-  uint2* dst = reinterpret_cast<uint2*>(a.out + (int64_t)s * a.o_ss + (int64_t)h * a.o_sh) + lane;
+// Joins a request's partials, in the order of its steps.  A work-group takes 256 pieces of four dims of a head, as
+// the decode kernel's lanes held them, of one request; PARTS threads share a piece's partials, in runs whose sums
+// are added up in order.  Requests of one run are finished already; empty ones get 0 and -inf here.
+template <int M, int PARTS>
+__global__ __launch_bounds__(256 * PARTS) void latent_join_kernel(LatentDecodeArgs a) {
+  constexpr int T = M == 64 ? 32 : 16;
+  using V = Tile<T>;
+  constexpr int kHt = M / T, kDt = 128 / T, kI = V::kN / 4, kBlocks = M * kRank / 4 / 256;
+  constexpr int kHeads = M == 16 ? 16 : 32;  // of a work-group's pieces
+  constexpr int kRowsAt = 256 * PARTS / kHeads;  // threads that share a head's partials below
+  __shared__ float fac[kLatGroups + 1][kHeads];
+  __shared__ float2 red[kRowsAt][kHeads];
+  __shared__ f32x4 part[PARTS][256];
+  const int blk = (int)(blockIdx.x % kBlocks);
+  const int hg = (int)(blockIdx.x / kBlocks % (uint32_t)a.groups), s = (int)(blockIdx.x / kBlocks / (uint32_t)a.groups);
+  const int tid = threadIdx.x, piece = tid % 256, p = tid / 256;
+  // the piece: tile t of the heads and dt of a wave's dims, rows 4 i ..
+  const int lane = piece % 64;
+  const int y = (blk * 256 + piece) / 64, i4 = y % kI, t = y / kI % kHt, dt = y / kI / kHt % kDt, wv = y / kI / kHt / kDt;
+  const int hl = T * t + lane % T, h = hg * M + hl;
+  const int d = 128 * wv + T * dt + V::row(4 * i4, lane / T);
+  uint2* dst = reinterpret_cast<uint2*>(a.out + (int64_t)s * a.o_ss + (int64_t)min(h, a.H - 1) * a.o_sh + d);
+  // (the pieces of dims 0 .. 3 write the head's lse)
+  const bool lead = p == 0 && d == 0 && h < a.H;
   const int ns = steps_of(a, s);
   if (ns == 0) {
-    if (p == 0) *dst = make_uint2(0, 0);
-    if (tid == 0) a.lse[(int64_t)h * a.S + s] = -INFINITY;
+    if (p == 0 && h < a.H) *dst = make_uint2(0, 0);
+    if (lead) a.lse[(int64_t)h * a.S + s] = -INFINITY;
     return;
   }
   const Runs runs(a.first[a.S], a.shares);
   const uint32_t y0 = a.first[s];
   const int w0 = (int)runs.share(y0), w1 = (int)runs.share(y0 + ns - 1);
   if (w0 == w1) return;  // finished by its work-group
-  const int n = w1 - w0 + 1, hg = h / M, hl = h % M;
+  const int n = w1 - w0 + 1;
   // the first partial may be a run's second one: the run began with another request
-  const int64_t stride = (int64_t)2 * a.groups * M;
-  const int64_t row0 = ((int64_t)w0 * 2 * a.groups + hg) * M + hl;
-  const int64_t first = row0 + (runs.begin(w0) < y0 ? (int64_t)a.groups * M : 0);
-  const auto row = [&](int i) { return i == 0 ? first : row0 + i * stride; };
-  float mx = -INFINITY;
-  float2 v = make_float2(-INFINITY, 0.0f);
-  const bool mine = tid < n;
-  if (mine) v = a.part_ml[row(tid)];
-  mx = v.x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-  if (tid % 64 == 0) wave_max[tid / 64] = mx;
+  const int64_t slot0 = (int64_t)w0 * 2 * a.groups + hg;
+  const auto slot = [&](int i) { return slot0 + (i == 0 ? (runs.begin(w0) < y0 ? a.groups : 0) : (int64_t)i * 2 * a.groups); };
+  // the heads' maxima, and each partial's factor
+  const int hb = M == 64 ? 32 * (blk % 2) : 0, eh = tid % kHeads, er = tid / kHeads;
+  float m = -INFINITY;
+  for (int i = er; i < n; i += kRowsAt) m = fmaxf(m, a.part_ml[slot(i) * M + hb + eh].x);
+  red[er][eh].x = m;
   __syncthreads();
-  float m = wave_max[0];
-#pragma unroll
-  for (int i = 1; i < kJoinThreads / 64; i++) m = fmaxf(m, wave_max[i]);
+  for (int i = 0; i < kRowsAt; i++) m = fmaxf(m, red[i][eh].x);
   const float mu = m == -INFINITY ? 0.0f : m;
-  if (tid < n) ml[tid] = make_float2(__builtin_amdgcn_exp2f(v.x - mu), v.y);
+  float l = 0.0f;
+  for (int i = er; i < n; i += kRowsAt) {
+    const float2 v = a.part_ml[slot(i) * M + hb + eh];
+    const float f = __builtin_amdgcn_exp2f(v.x - mu);
+    fac[i][eh] = f;
+    l = fmaf(v.y, f, l);
+  }
   __syncthreads();
-  const int per = (n + kJoinParts - 1) / kJoinParts, i0 = p * per, i1 = min(n, i0 + per);
+  red[er][eh] = make_float2(m, l);
+  __syncthreads();
+  const int me = hl - hb;
+  m = red[0][me].x;
+  l = 0.0f;
+  for (int i = 0; i < kRowsAt; i++) l += red[i][me].y;
+  const int per = (n + PARTS - 1) / PARTS, i0 = p * per, i1 = min(n, i0 + per);
+  const f32x4* src = reinterpret_cast<const f32x4*>(a.part_o) + blk * 256 + piece;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i = i0; i < i1; i += 8) {
     f32x4 x[8];
 #pragma unroll
-    for (int j = 0; j < 8; j++) x[j] = reinterpret_cast<const f32x4*>(a.part_o + row(min(i + j, i1 - 1)) * kRank)[lane];
+    for (int j = 0; j < 8; j++) x[j] = src[slot(min(i + j, i1 - 1)) * (M * kRank / 4)];
 #pragma unroll
     for (int j = 0; j < 8; j++) {
-      const float f = ml[min(i + j, i1 - 1)].x;
+      const float f = fac[min(i + j, i1 - 1)][me];
 #pragma unroll
       for (int e = 0; e < 4; e++) acc[e] = i + j < i1 ? fmaf(x[j][e], f, acc[e]) : acc[e];
     }
   }
-  part[p][lane] = acc;
-  float l = 0.0f;
-  if (tid < 64) {
-    for (int i = tid; i < n; i += 64) l = fmaf(ml[i].x, ml[i].y, l);
+  if constexpr (PARTS > 1) {
+    part[p][piece] = acc;
+    __syncthreads();
+    if (p != 0) return;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
-    if (tid == 0) wave_max[0] = l;
+    for (int i = 1; i < PARTS; i++) acc += part[i][piece];
   }
-  __syncthreads();
-  if (p != 0) return;
-  l = wave_max[0];
-#pragma unroll
-  for (int i = 1; i < kJoinParts; i++) acc += part[i][lane];
+  if (h >= a.H) return;
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   *dst = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
-  if (tid == 0) a.lse[(int64_t)h * a.S + s] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  if (lead) a.lse[(int64_t)h * a.S + s] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <int M>
@@ -564,7 +593,10 @@ hipError_t decode(const LatentDecodeArgs& a, hipStream_t st) {
 
 template <int M>
 hipError_t join(const LatentDecodeArgs& a, hipStream_t st) {
-  latent_join_kernel<M><<<(unsigned)((int64_t)a.S * a.H), kJoinThreads, 0, st>>>(a);
+  const unsigned grid = (unsigned)((int64_t)a.S * a.groups * (M * kRank / 4 / 256));
+  // few requests: many partials each
+  if (a.S <= 8) latent_join_kernel<M, 4><<<grid, 1024, 0, st>>>(a);
+  else latent_join_kernel<M, 1><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
