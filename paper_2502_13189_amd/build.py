@@ -28,9 +28,10 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# A running maximum rescales the decode kernel's accumulators with vector instructions now and then: in the
-# accumulation registers, which those cannot reach, they would be copied to and fro at every step.
-FILE_FLAGS = {"latent_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# Where vector instructions work on what the matrix cores made, it is kept out of the accumulation registers, which
+# those cannot reach: it would be copied to and fro at every step.
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+FILE_FLAGS = {"latent_decode.hip": _VGPR_FORM, "latent_bwd.hip": _VGPR_FORM}
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-I" + INCLUDE, "-I" + CSRC,
           "-Wall", "-Wno-unused-result"]
 

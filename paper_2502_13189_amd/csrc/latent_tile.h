@@ -12,6 +12,9 @@
 #include "latent_internal.h"
 #include "mfma_tile.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace moba {
 
 constexpr int kWide = kLatTile * kNope / 8;     // 16-byte chunks of a wide tile (1024)
@@ -47,21 +50,23 @@ struct Rows {
 };
 
 // Lane's part of the DMA of tile i (64 rows; those past the sequence repeat its last one) by NW
-// waves.  WIDE: 16 instructions of four rows, else 8 of eight rows; wave w issues w, w + NW, ...
+// waves.  WIDE: 16 instructions of four rows, else 8 of eight rows; wave w issues w, w + NW, ..., here its x-th.
 template <int NW, bool WIDE>
-__device__ __forceinline__ void stage_tile(const Rows& R, int i, u32x4* buf, int wave, int lane) {
-  constexpr int kCh = WIDE ? 16 : 8, kN = WIDE ? 16 : 8;
+__device__ __forceinline__ void stage_part(const Rows& R, int i, u32x4* buf, int wave, int lane, int x) {
+  constexpr int kCh = WIDE ? 16 : 8;
   const int r0 = i * kLatTile;
   const char* tile = R.base + (int64_t)r0 * R.st;
   const int last = R.len - 1 - r0;  // (a staged tile begins in the sequence)
+  const int j = wave + NW * x, row = (64 / kCh) * j + lane / kCh;
+  const int c = (lane % kCh) ^ (WIDE ? swz_wide(row) : swz_slim(row));
+  dma16_at(tile, (uint32_t)min(row, last) * R.st + (uint32_t)c * 16, buf + 64 * j);
+}
+
+template <int NW, bool WIDE>
+__device__ __forceinline__ void stage_tile(const Rows& R, int i, u32x4* buf, int wave, int lane) {
+  static_assert((WIDE ? 16 : 8) % NW == 0, "whole instructions");
 #pragma unroll
-  for (int x = 0; x < (kN + NW - 1) / NW; x++) {
-    const int j = wave + NW * x;
-    if (kN % NW != 0 && j >= kN) break;
-    const int row = (64 / kCh) * j + lane / kCh;
-    const int c = (lane % kCh) ^ (WIDE ? swz_wide(row) : swz_slim(row));
-    dma16_at(tile, (uint32_t)min(row, last) * R.st + (uint32_t)c * 16, buf + 64 * j);
-  }
+  for (int x = 0; x < (WIDE ? 16 : 8) / NW; x++) stage_part<NW, WIDE>(R, i, buf, wave, lane, x);
 }
 
 // Row operand: chunk c of row r (bytes).
@@ -85,6 +90,26 @@ __device__ __forceinline__ uint32_t tr_slim(const TrLane& t, int dt, int x) {
   return at_slim(t.row + 8 * x, 4 * dt + t.chunk) + t.half;
 }
 
+// f(0), f(1), ... f(N - 1), the index a constant of the compiler.
+template <int N>
+using Index = std::integral_constant<int, N>;
+template <typename F, int... X>
+__device__ __forceinline__ void each_of(F& f, std::integer_sequence<int, X...>) {
+  (f(Index<X>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {
+  each_of(f, std::make_integer_sequence<int, N>());
+}
+
+// ---- the backward's kernels: work-groups of 4 waves, one on a CU
+constexpr int kLatBwdWaves = 4;
+constexpr int kLatBwdDma = 10;     // DMA instructions a wave and tile: 4 + 4 + 2
+constexpr int kSlicesAhead = 6;    // slices from an operand's reads to its product
+
+// The end of a slice: nothing is moved over it.
+__device__ __forceinline__ void slice_end() { __builtin_amdgcn_sched_barrier(0); }
+
 // Places of work.  Sequence s's tiles of `rows` tokens begin at place cu[s] / rows + s, so that
 // no table is needed: places(T, S) of them, some empty.
 __host__ __device__ inline int64_t latent_places(int64_t T, int S, int rows) { return T / rows + S; }
@@ -95,11 +120,16 @@ struct Place {
   int t0;        // the tile's first token within the sequence
 };
 __device__ __forceinline__ bool latent_place(const LatentArgs& a, int64_t x, int rows, Place* p) {
-  int lo = 0, hi = a.S - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.cu[mid] / rows + mid <= x) lo = mid; else hi = mid - 1;
+  // the last sequence whose first place is at or before x: 64 of them looked at together
+  int lo = 0;
+  for (int n = a.S; n > 1;) {
+    const int step = (n + 63) / 64, lane = threadIdx.x & 63, at = lo + lane * step;
+    const bool before = lane * step < n && a.cu[min(at, a.S)] / rows + at <= x;
+    const int k = max(0, __popcll(__builtin_amdgcn_ballot_w64(before)) - 1);
+    lo += k * step;
+    n = min(step, n - k * step);
   }
+  lo = __builtin_amdgcn_readfirstlane(lo);
   // (whatever cu holds, rows stay within [0, T))
   const int64_t c0 = a.cu[lo], c1 = a.cu[lo + 1];
   const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
