@@ -1,37 +1,37 @@
 // Causal latent attention, expanded form: z_ij = scale (<q_i[0:128], k_j> + <q_i[128:192], kr_j>),
 // out_i = sum_j softmax(z_i)_j v_j, where kr is one rotary key for all heads.
 //
-// Bound by the matrix cores: 640 operations a scored pair and 640 bytes a (head, token).  Work-group = 8
-// waves = 256 queries of one head; wave w owns queries 32w .. 32w + 31, one per lane column.  Keys come
-// in tiles of 64: k and v (128 dims each) and kr (64) are staged row-major in LDS by DMA, two
-// buffers each (80 KiB), tile i + 1 in flight while tile i is used, one barrier a tile.  On
+// Bound by the matrix cores: 640 operations a scored pair and 640 bytes a (head, token).  Work-group = NW
+// waves (8, or 4 for small batches) = 32 NW queries of one head; wave w owns queries 32w .. 32w + 31, one per
+// lane column.  Keys come in tiles of 64: k and v (128 dims each) and kr (64) are staged row-major in LDS by
+// DMA, two buffers each (80 KiB), tile i + 1 in flight while tile i is used, one barrier a tile.  On
 // v_mfma_f32_32x32x16_bf16, per tile and wave:
 //   S^T (keys x queries) = K . Q^T    2 halves x 12 k-steps, Q in registers
 //   online softmax in 32 bits: a lane holds one query and 32 of the 64 keys.  Weights are formed
 //     under the running max, which is raised only when a lane's weights sum to more than 2^8
 //   O^T (dims x queries) += V^T . P^T  4 dim tiles x 4 k-steps, V^T by transposed LDS reads
+// Queries and keys are cut at the same multiples of 32, so of a wave's halves of tiles one is masked, the
+// diagonal one; those before it are whole, those behind it are left out.
 // The weights enter the second product as bf16 (2^-9 of each, independent of each other: it adds
 // to the result about what its own rounding to bf16 does); all sums are fp32.
 #include "latent_tile.h"
 
 #include <math.h>
 
-#include <type_traits>
-
 namespace moba {
 namespace {
 
-constexpr int kWaves = kLatRows / 32;
 constexpr int kBufChunks = 2 * kWide + kSlim;  // k, v, kr
 constexpr float kSumLimit = 256.0f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kStageRow = kNope / 8 + 1;  // 16-byte chunks of a staged result row (one pad)
 
-// P^T operands of the tile under the running max m; returns the lane's sum of weights.
-__device__ __forceinline__ float weights(const f32x16 (&s)[2], float m, bf16x8 (&pb)[4], float c2) {
+// P^T operands of NH halves of a tile under the running max m; returns the lane's sum of weights.
+template <int NH>
+__device__ __forceinline__ float weights(const f32x16 (&s)[NH], float m, bf16x8 (&pb)[2 * NH], float c2) {
   float ts = 0.0f;
 #pragma unroll
-  for (int th = 0; th < 2; th++)
+  for (int th = 0; th < NH; th++)
 #pragma unroll
     for (int s2 = 0; s2 < 2; s2++) {
       uint32_t w[4];
@@ -47,10 +47,9 @@ __device__ __forceinline__ float weights(const f32x16 (&s)[2], float m, bf16x8 (
   return ts;
 }
 
-template <bool EDGE>
-__device__ __forceinline__ void softmax(f32x16 (&s)[2], float& m, float& l, f32x16 (&o)[4],
-                                        bf16x8 (&pb)[4], int hi, float c2) {
-  if (EDGE) mask_keys(s, -4, hi);
+template <int NH>
+__device__ __forceinline__ void softmax(const f32x16 (&s)[NH], float& m, float& l, f32x16 (&o)[4],
+                                        bf16x8 (&pb)[2 * NH], float c2) {
   float ts = 0.0f;
   bool redo = __builtin_amdgcn_ballot_w64(m == -INFINITY) != 0;
   if (!redo) {
@@ -60,7 +59,7 @@ __device__ __forceinline__ void softmax(f32x16 (&s)[2], float& m, float& l, f32x
   if (redo) {
     float mx = -INFINITY;
 #pragma unroll
-    for (int th = 0; th < 2; th++)
+    for (int th = 0; th < NH; th++)
 #pragma unroll
       for (int r = 0; r < 16; r++) mx = fmaxf(mx, s[th][r]);
     mx = fmaxf(mx, xor32(mx)) * c2;
@@ -77,12 +76,12 @@ __device__ __forceinline__ void softmax(f32x16 (&s)[2], float& m, float& l, f32x
   l += ts;
 }
 
-// Whether a wide tile holds a value that is not finite (all lanes alike).
+// Whether 32 rows of a wide tile hold a value that is not finite (all lanes alike).
 __device__ __forceinline__ bool holds_odd(const char* vb, int lane) {
   typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
   u16x8 most = 0;
 #pragma unroll
-  for (int j = 0; j < kWide / 64; j++) {
+  for (int j = 0; j < kWide / 128; j++) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(vb + (64 * j + lane) * 16) & 0x7f807f80u;
     most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x8, w));
   }
@@ -92,13 +91,13 @@ __device__ __forceinline__ bool holds_odd(const char* vb, int lane) {
   return __builtin_amdgcn_ballot_w64(odd != 0) != 0;
 }
 
-// O^T += V^T . P^T of an edge tile that holds values that are not finite: a weight of 0 must not
+// O^T += V^T . P^T of a diagonal half that holds values that are not finite: a weight of 0 must not
 // meet them, since a row may not see what it does not attend.  One key at a time, and a row takes
-// the product of those that it attends.  hi: keys of the tile that the lane's row attends.
+// the product of those that it attends.  hi: keys of the half that the lane's row attends.
 __device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const uint32_t (&ov)[2][4],
-                                          const bf16x8 (&pb)[4], int hi, int hh) {
+                                          const bf16x8 (&pb)[2], int hi, int hh) {
 #pragma unroll
-  for (int ks = 0; ks < 4; ks++)
+  for (int ks = 0; ks < 2; ks++)
 #pragma unroll 1
     for (int kk = 0; kk < 16; kk++) {
       u32x4 only;  // element e of an operand: key 16 ks + 8 (e / 4) + 4 hh + e % 4
@@ -122,20 +121,23 @@ __device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const 
     }
 }
 
-__global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentArgs a) {
+template <int NW>
+__global__ __launch_bounds__(64 * NW, 8 / NW) void latent_forward_kernel(LatentArgs a) {
+  constexpr int kRows = 32 * NW;
   __shared__ u32x4 lds[2 * kBufChunks];
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qc = lane & 31, hh = lane >> 5;
 
   Work wk;
-  if (!latent_work<true>(a, latent_places(a.T, a.S, kLatRows), &wk)) return;
+  if (!latent_work<true>(a, latent_places(a.T, a.S, kRows), &wk)) return;
   Place pl;
-  if (!latent_place(a, wk.place, kLatRows, &pl)) return;
+  if (!latent_place(a, wk.place, kRows, &pl)) return;
   const int h = __builtin_amdgcn_readfirstlane(wk.h);
   const int row = pl.t0 + 32 * wave + qc;         // this lane's query, within the sequence
   const int rc = min(row, pl.len - 1);
-  const int kend = min(pl.t0 + kLatRows, pl.len);
+  const int kend = min(pl.t0 + kRows, pl.len);
+  const int base = pl.t0 + 32 * wave;             // the wave's first query
 
   bf16x8 qf[12];
   {
@@ -148,9 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
   };
   const Rows rk = rows(a.k, a.k_st, a.k_sh), rv = rows(a.v, a.v_st, a.v_sh), rr = rows(a.kr, a.kr_st, 0);
   const auto stage = [&](int i, u32x4* buf) {
-    stage_tile<kWaves, true>(rk, i, buf, wave, lane);
-    stage_tile<kWaves, true>(rv, i, buf + kWide, wave, lane);
-    stage_tile<kWaves, false>(rr, i, buf + 2 * kWide, wave, lane);
+    stage_tile<NW, true>(rk, i, buf, wave, lane);
+    stage_tile<NW, true>(rv, i, buf + kWide, wave, lane);
+    stage_tile<NW, false>(rr, i, buf + 2 * kWide, wave, lane);
   };
 
   // operand offsets: rows qc (+ 32: the same swizzle, 32 rows on), chunk 2 kk + hh
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
   stage(0, lds);
   dma_wait();
   __syncthreads();
-  const auto step = [&](auto masked, int i) {
-    constexpr bool edge = decltype(masked)::value;
+  const int nfull = pl.t0 / kLatTile;  // tiles before the diagonal's
+  for (int i = 0; i < nfull; i++) {
     const char* buf = reinterpret_cast<const char*>(lds + (i & 1) * kBufChunks);
     if (i + 1 < n) stage(i + 1, lds + ((i + 1) & 1) * kBufChunks);
     f32x16 s[2];
@@ -206,14 +208,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
       }
       __builtin_amdgcn_sched_group_barrier(0x008, kPre, 0);
     }
-    const int u0 = i * kLatTile;
-    const int hi = row + 1 - u0 - 4 * hh;
     bf16x8 pb[4];
-    softmax<edge>(s, m, l, o, pb, hi, c2);
-    const char* bv = buf + kWide * 16;
-    if (edge && holds_odd(bv, lane)) {
-      pv_by_key(o, bv, ov, pb, row + 1 - u0, hh);
-    } else {
+    softmax(s, m, l, o, pb, c2);
+    {
+      const char* bv = buf + kWide * 16;
       s16x4 t0[16], t1[16];
 #pragma unroll
       for (int j = 0; j < 16; j++) {
@@ -233,10 +231,52 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
     }
     dma_wait();
     __syncthreads();
-  };
-  const int nfull = pl.t0 / kLatTile;  // tiles before the diagonal's
-  for (int i = 0; i < nfull; i++) step(std::false_type(), i);
-  for (int i = nfull; i < n; i++) step(std::true_type(), i);
+  }
+  // the diagonal's tiles, by halves: each wave those up to its own rows' (and none if it has no rows)
+  const int stop = base < pl.len ? base : -1;
+  for (int i = nfull; i < n; i++) {
+    if (i + 1 < n) stage(i + 1, lds + ((i + 1) & 1) * kBufChunks);
+#pragma unroll 1
+    for (int th = 0; th < 2; th++) {
+      const int u0 = i * kLatTile + 32 * th;
+      if (u0 > stop) break;
+      const char* bk = reinterpret_cast<const char*>(lds + (i & 1) * kBufChunks) + 8192 * th;
+      const char* bv = bk + kWide * 16;
+      const char* br = reinterpret_cast<const char*>(lds + (i & 1) * kBufChunks) + 2 * kWide * 16 + 4096 * th;
+      f32x16 s[1];
+#pragma unroll
+      for (int r = 0; r < 16; r++) s[0][r] = 0.0f;
+      u32x4 op[12];
+#pragma unroll
+      for (int j = 0; j < 12; j++)
+        op[j] = j < 8 ? *reinterpret_cast<const u32x4*>(bk + ok[j & 7]) : *reinterpret_cast<const u32x4*>(br + orr[(j - 8) & 3]);
+#pragma unroll
+      for (int j = 0; j < 12; j++) s[0] = mfma(as_bf16x8(op[j]), qf[j], s[0]);
+      const bool diagonal = u0 == stop;
+      if (diagonal) {
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+          if (8 * (r >> 2) + 4 * hh + (r & 3) > qc) s[0][r] = -INFINITY;
+      }
+      bf16x8 pb[2];
+      softmax(s, m, l, o, pb, c2);
+      if (diagonal && holds_odd(bv, lane)) {
+        pv_by_key(o, bv, ov, pb, qc + 1, hh);
+      } else {
+        s16x4 t0[8], t1[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const char* b = bv + 16 * (j >> 2) * 256;
+          t0[j] = tr16(b + ov[0][j & 3]);
+          t1[j] = tr16(b + ov[1][j & 3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) o[j & 3] = mfma(join16(t0[j], t1[j]), pb[j >> 2], o[j & 3]);
+      }
+    }
+    dma_wait();
+    __syncthreads();
+  }
 
   // the buffers are free: each wave stages its 32 rows and writes them whole
   const float lt = l + xor32(l);
@@ -256,7 +296,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int j = 0; j < 8; j++) {
-    const int rr2 = 4 * j + (lane >> 4), t = pl.t0 + 32 * wave + rr2;
+    const int rr2 = 4 * j + (lane >> 4), t = base + rr2;
     if (t < pl.len)
       reinterpret_cast<u32x4*>(a.out + (pl.tok0 + t) * a.o_st + (int64_t)h * a.o_sh)[lane & 15] =
           stg[rr2 * kStageRow + (lane & 15)];
@@ -265,8 +305,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_forward_kernel(LatentAr
 
 }  // namespace
 
+// Queries of a work-group: 128 where twice as many work-groups still all find a CU of their own, and 256
+// otherwise, which reads k and v half as often.
 hipError_t launch_latent_forward(const LatentArgs& a, hipStream_t st) {
-  latent_forward_kernel<<<latent_grid(a, kLatRows), 64 * kWaves, 0, st>>>(a);
+  if (latent_places(a.T, a.S, kLatRows) * a.H <= kLatSmall)
+    latent_forward_kernel<4><<<latent_grid(a, 128), 256, 0, st>>>(a);
+  else
+    latent_forward_kernel<8><<<latent_grid(a, 256), 512, 0, st>>>(a);
   return hipGetLastError();
 }
 
