@@ -508,7 +508,9 @@ size_t moba_latent_backward_workspace_bytes(int64_t T, int32_t num_heads);
  * c [T, 512], k_rope [T, 64] bf16, any token stride; slots [T] i64 contiguous as moba_cache_plan
  *        writes them: page * P + offset; a token whose slot is negative or not of the pool is left
  *        out.  No slot may come twice
- * rot    NULL: k_rope is stored as it is; else it is turned first (R = 64), and rounded once
+ * rot    NULL: k_rope is stored as it is; else it is turned first (R = 64), and rounded once; rows of no
+ *        sequence (positions from cu_seqlens) are then left out
+ * T < 2^28.
  */
 moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, const moba_tensor* slots,
                               const moba_rotation* rot, moba_tensor* pages, hipStream_t stream);

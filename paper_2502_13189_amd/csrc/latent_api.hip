@@ -394,13 +394,13 @@ moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, c
     if ((st = check_rotation(rot, T, kRopeDim, &a.r)) != MOBA_OK) return st;
     if (a.r.half != kRopeDim / 2) return MOBA_ERR_SHAPE;
   }
-  if (T >= kMost) return MOBA_ERR_UNSUPPORTED;
-  if (T == 0) return MOBA_OK;
+  if (T >= int64_t(1) << 28) return MOBA_ERR_UNSUPPORTED;  // (8 threads a token, 2^32 of a launch)
+  if (T == 0 || (a.r.cu && a.r.S == 0)) return MOBA_OK;
   a.c = reinterpret_cast<const __hip_bfloat16*>(vc.data); a.c_st = vc.st;
   a.kr = reinterpret_cast<const __hip_bfloat16*>(vr.data); a.kr_st = vr.st;
   a.slots = static_cast<const int64_t*>(slots->data);
   a.T = T;
-  a.rotate = rot != nullptr && !(a.r.cu && a.r.S == 0);
+  a.rotate = rot != nullptr;
   Phase ph("latent_write", stream);
   MOBA_LAUNCH(launch_latent_write(rot && rot->interleaved != 0, a, stream));
   return MOBA_OK;

@@ -156,10 +156,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
   if (x0 < x1 && upto - mine <= x0 && x0 < upto) {  // one thread
     uint32_t y = upto - mine;
     int s = sb;
-    for (;; s++) {
+    while (span > 1) {
       const uint32_t n = steps_of(a, s);
       if (x0 < y + n) break;
       y += n;
+      s++;
     }
     begin_s = s;
     scan[kWaves] = y;
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     uint32_t y = upto - mine;
     for (int s = sb; s < se && y < x1; s++) {
       if (y >= x0) a.first[s] = y;
-      y += steps_of(a, s);
+      if (span > 1) y += steps_of(a, s);
     }
   }
   __syncthreads();
@@ -522,13 +523,13 @@ __global__ __launch_bounds__(256 * PARTS) void latent_join_kernel(LatentDecodeAr
   // (the pieces of dims 0 .. 3 write the head's lse)
   const bool lead = p == 0 && d == 0 && h < a.H;
   const int ns = steps_of(a, s);
+  const uint32_t y0 = a.first[s], total = a.first[a.S];  // (y0 of an empty request: anything)
   if (ns == 0) {
     if (p == 0 && h < a.H) *dst = make_uint2(0, 0);
     if (lead) a.lse[(int64_t)h * a.S + s] = -INFINITY;
     return;
   }
-  const Runs runs(a.first[a.S], a.shares);
-  const uint32_t y0 = a.first[s];
+  const Runs runs(total, a.shares);
   const int w0 = (int)runs.share(y0), w1 = (int)runs.share(y0 + ns - 1);
   if (w0 == w1) return;  // finished by its work-group
   const int n = w1 - w0 + 1;

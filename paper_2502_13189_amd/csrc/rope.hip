@@ -107,48 +107,65 @@ hipError_t rope_layout(bool interleaved, const RopeArgs& a, hipStream_t st) {
 }
 
 // ================================================================ latent write
-// A token's row of the cache: 512 numbers as they are, then the 64 of the rotary key, turned.  72
-// threads a token, 16 bytes each: a copy, bound by memory.
-constexpr int kRank = 512, kRot = 64, kRowLen = kRank + kRot, kRowPieces = kRowLen / 8;
+// A token's row of the cache: 512 numbers as they are, then the 64 of the rotary key, turned.  A copy, bound by
+// memory.  A wave takes 8 tokens: their 512 numbers a lane's 16 bytes of each, their rotary keys 8 lanes each
+// with 4 pairs; all loads go out before the first is used.
+constexpr int kRank = 512, kRot = 64, kRowLen = kRank + kRot, kTokens = 8;
 
 template <bool INTERLEAVED>
-__global__ __launch_bounds__(kThreads) void latent_write_kernel(LatentWriteArgs a, int64_t t0, uint32_t total) {
-  const uint32_t x = blockIdx.x * kThreads + threadIdx.x;
-  if (x >= total) return;
-  const uint32_t row = x / kRowPieces;
-  const int piece = (int)(x - row * kRowPieces);
-  const int64_t t = t0 + row;
-  const int64_t slot = a.slots[t];
-  if (slot < 0 || slot >= (int64_t)a.N * a.P) return;
-  const int64_t page = slot / a.P;
-  __hip_bfloat16* dst = a.pages + page * a.p_sp + (slot - page * a.P) * kRowLen;
-  if (piece < kRank / 8) {
-    reinterpret_cast<uint4*>(dst)[piece] = reinterpret_cast<const uint4*>(a.c + t * a.c_st)[piece];
-    return;
+__global__ __launch_bounds__(kThreads) void latent_write_kernel(LatentWriteArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t0 = ((int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64) * kTokens;
+  if (t0 >= a.T) return;
+  // what a token has is loaded before it is known whether it has a slot
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 c[kTokens];
+#pragma unroll
+  for (int j = 0; j < kTokens; j++) {
+    const int64_t at = t0 + j < a.T ? t0 + j : a.T - 1;
+    c[j] = reinterpret_cast<const u32x4*>(a.c + at * a.c_st)[lane];
   }
-  const int i = piece - kRank / 8;  // 4 pairs of the rotary key
-  const __hip_bfloat16* src = a.kr + t * a.kr_st;
-  dst += kRank;
+  // lane 8 j + i: 4 pairs of token j's rotary key
+  const int i = lane & 7;
+  const bool real = t0 + (lane >> 3) < a.T;
+  const int64_t t = real ? t0 + (lane >> 3) : a.T - 1;
   using P = Piece<__hip_bfloat16, 4>;
   const int d0 = INTERLEAVED ? 8 * i : 4 * i, d1 = INTERLEAVED ? d0 + 4 : d0 + kRot / 2;
-  P u = *reinterpret_cast<const P*>(src + d0), w = *reinterpret_cast<const P*>(src + d1);
-  int64_t p;
-  if (a.rotate) {
-    if (!row_position(a.r, t, &p)) p = 0;  // (a row of no sequence that has a slot: as it is)
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      float c, s;
-      cos_sin_at(a.r, 4 * i + j, p, &c, &s);
-      __hip_bfloat16& e0 = INTERLEAVED ? (j < 2 ? u.e[(2 * j) % 4] : w.e[(2 * j) % 4]) : u.e[j];
-      __hip_bfloat16& e1 = INTERLEAVED ? (j < 2 ? u.e[(2 * j + 1) % 4] : w.e[(2 * j + 1) % 4]) : w.e[j];
-      float f0 = to_f32(e0), f1 = to_f32(e1);
-      turn_pair(f0, f1, c, s);
-      e0 = from_f32<__hip_bfloat16>(f0);
-      e1 = from_f32<__hip_bfloat16>(f1);
-    }
+  P u = *reinterpret_cast<const P*>(a.kr + t * a.kr_st + d0), w = *reinterpret_cast<const P*>(a.kr + t * a.kr_st + d1);
+  const int64_t slot = a.slots[t];
+  // its row in the pool; null: none
+  __hip_bfloat16* dst = nullptr;
+  int64_t p = 0;
+  const bool placed = !a.rotate || row_position(a.r, t, &p);  // (a row of no sequence is left out)
+  if (real && placed && slot >= 0 && slot < (int64_t)a.N * a.P) {
+    const uint64_t page = (uint64_t)slot / (uint32_t)a.P;
+    dst = a.pages + (int64_t)page * a.p_sp + (slot - (int64_t)page * a.P) * kRowLen;
   }
-  *reinterpret_cast<P*>(dst + d0) = u;
-  *reinterpret_cast<P*>(dst + d1) = w;
+  if (dst) {
+    if (a.rotate) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        float cs, sn;
+        cos_sin_at(a.r, 4 * i + j, p, &cs, &sn);
+        __hip_bfloat16& e0 = INTERLEAVED ? (j < 2 ? u.e[(2 * j) % 4] : w.e[(2 * j) % 4]) : u.e[j];
+        __hip_bfloat16& e1 = INTERLEAVED ? (j < 2 ? u.e[(2 * j + 1) % 4] : w.e[(2 * j + 1) % 4]) : w.e[j];
+        float f0 = to_f32(e0), f1 = to_f32(e1);
+        turn_pair(f0, f1, cs, sn);
+        e0 = from_f32<__hip_bfloat16>(f0);
+        e1 = from_f32<__hip_bfloat16>(f1);
+      }
+    }
+    *reinterpret_cast<P*>(dst + kRank + d0) = u;
+    *reinterpret_cast<P*>(dst + kRank + d1) = w;
+  }
+#pragma unroll
+  for (int j = 0; j < kTokens; j++) {
+    const uint64_t x = reinterpret_cast<uint64_t>(dst);
+    __hip_bfloat16* to = reinterpret_cast<__hip_bfloat16*>(
+        ((uint64_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), 8 * j) << 32) |
+        (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, 8 * j));
+    if (to) reinterpret_cast<u32x4*>(to)[lane] = c[j];
+  }
 }
 
 }  // namespace
@@ -172,17 +189,11 @@ hipError_t launch_rope(bool bf16, bool interleaved, int vec, const RopeArgs& a, 
 }
 
 hipError_t launch_latent_write(bool interleaved, const LatentWriteArgs& a, hipStream_t st) {
-  constexpr int64_t most = ((int64_t(1) << 31) - 1) / kRowPieces;
-  for (int64_t t = 0; t < a.T; t += most) {
-    const int64_t n = a.T - t < most ? a.T - t : most;
-    const uint32_t total = (uint32_t)(n * kRowPieces);
-    const unsigned grid = (total + kThreads - 1) / kThreads;
-    if (interleaved) latent_write_kernel<true><<<grid, kThreads, 0, st>>>(a, t, total);
-    else latent_write_kernel<false><<<grid, kThreads, 0, st>>>(a, t, total);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  constexpr int kPer = kThreads / 64 * kTokens;
+  const unsigned grid = (unsigned)((a.T + kPer - 1) / kPer);
+  if (interleaved) latent_write_kernel<true><<<grid, kThreads, 0, st>>>(a);
+  else latent_write_kernel<false><<<grid, kThreads, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace moba

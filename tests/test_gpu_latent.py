@@ -387,6 +387,25 @@ def test_write(interleaved):
     assert bool((flat[rest] == 7.0).all()) and bool((pflat[rest] == 7.0).all())
 
 
+def test_write_by_sequences():
+    """Positions from packed sequences; a row of no sequence is left out though it has a slot."""
+    r = binding.rotation(64)
+    T = 21
+    c, kr = randn(T, 512, seed=1), randn(T, 64, seed=2)
+    pages = torch.full((2, 64, 576), 7.0, dtype=BF, device=DEV)
+    cu = torch.tensor([2, 12, 12, 19], dtype=torch.int32, device=DEV)
+    start = torch.tensor([5, 0, 1000], dtype=torch.int32, device=DEV)
+    slots = torch.arange(T, device=DEV) + 50
+    binding.latent_write(c, kr, slots, pages, r, cu_seqlens=cu, start=start)
+    pos = torch.cat([torch.arange(5, 15, device=DEV), torch.arange(1000, 1007, device=DEV)])
+    want = torch.full((128, 576), 7.0, dtype=BF, device=DEV)
+    want[52:69] = torch.cat([c[2:19], binding.rope(kr[2:19, None], None, r, pos=pos)[0][:, 0]], 1)
+    assert torch.equal(pages.view(-1, 576), want)
+    binding.latent_write(c, kr, slots, pages, r, cu_seqlens=cu[:1])
+    torch.cuda.synchronize()
+    assert torch.equal(pages.view(-1, 576), want)
+
+
 def test_write_page_stride():
     """A layer's slice of a pool of several layers."""
     pool = torch.full((4, 3, 64, 576), 7.0, dtype=BF, device=DEV)
