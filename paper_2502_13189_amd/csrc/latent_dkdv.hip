@@ -106,7 +106,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
     // products 0 .. 39: S and dP of the two halves of the rows, in turn; 40 .. 79: dV^T and dK^T
     constexpr int kN = 80;
     u32x4 op[kN];
-    uint32_t wp[2][8], wd[2][8];  // P and dS of the halves, bf16 pairs
+    uint32_t wp[2][8], wd[2][8], wl[2][8];  // P and dS of the halves, bf16 pairs; and what dS's leave out
     float2 lv[16], dl[16];
     const auto fetch = [&](auto n_) __attribute__((always_inline)) {
       constexpr int x = decltype(n_)::value;
@@ -134,6 +134,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
         const bf16x8 b = as_bf16x8(u32x4{w[e], w[e + 1], w[e + 2], w[e + 3]});
         if constexpr (z < 4) dv[z] = mfma(as_bf16x8(op[x]), b, dv[z]);
         else dk[z - 4] = mfma(as_bf16x8(op[x]), b, dk[z - 4]);
+        if constexpr (edge && z >= 4)
+          dk[z - 4] = mfma(as_bf16x8(op[x]), as_bf16x8(u32x4{wl[st][e], wl[st][e + 1], wl[st][e + 2], wl[st][e + 3]}), dk[z - 4]);
       }
     };
     // elements 2 e, 2 e + 1 of a half: rows r, r + 1
@@ -156,6 +158,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
       }
       wp[st][e] = pack_bf16(p0, p1);
       wd[st][e] = pack_bf16(d0, d1);
+      if (edge) wl[st][e] = rest_bf16(wd[st][e], d0, d1);
       asm volatile("" : "+v"(wp[st][e]), "+v"(wd[st][e]));  // (formed here, not where they are used)
     };
     each<kSlicesAhead>(fetch);

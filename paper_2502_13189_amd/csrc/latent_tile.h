@@ -102,6 +102,11 @@ __device__ __forceinline__ void each(F f) {
   each_of(f, std::make_integer_sequence<int, N>());
 }
 
+// What a packed pair of bf16 leaves out of a and b, as such a pair.
+__device__ __forceinline__ uint32_t rest_bf16(uint32_t pair, float a, float b) {
+  return pack_bf16(a - __uint_as_float(pair << 16), b - __uint_as_float(pair & 0xffff0000u));
+}
+
 // ---- the backward's kernels: work-groups of 4 waves, one on a CU
 constexpr int kLatBwdWaves = 4;
 constexpr int kLatBwdDma = 10;     // DMA instructions a wave and tile: 4 + 4 + 2
