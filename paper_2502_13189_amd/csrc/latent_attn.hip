@@ -305,10 +305,12 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void latent_forward_kernel(LatentA
 
 }  // namespace
 
-// Queries of a work-group: 128 where twice as many work-groups still all find a CU of their own, and 256
-// otherwise, which reads k and v half as often.
+// Queries of a work-group: 256, which reads k and v half as often, where many long sequences' work fills the chip; else
+// 128, two work-groups on a CU, which leaves fewer waves without rows and the last ones alone for less long.  256 and
+// 128, us: 1 x 256 tokens, 32 heads 17.3, 12.6; 8 x 1000, 4 heads 37.2, 32.4; 4096, 8 heads 115, 89; 100 x 100, 32
+// heads 39, 30; 4096, 32 heads 206, 191; 2048, 128 heads 218, 212; 8192, 32 heads 628, 664.
 hipError_t launch_latent_forward(const LatentArgs& a, hipStream_t st) {
-  if (latent_places(a.T, a.S, kLatRows) * a.H <= kLatSmall)
+  if (latent_places(a.T, a.S, kLatRows) * a.H <= kLatFew || a.T < kLatLong * (int64_t)a.S)
     latent_forward_kernel<4><<<latent_grid(a, 128), 256, 0, st>>>(a);
   else
     latent_forward_kernel<8><<<latent_grid(a, 256), 512, 0, st>>>(a);

@@ -169,15 +169,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dq_kernel(LatentArgs a)
     for (int th = 0; th < 2; th++)
 #pragma unroll
       for (int r = 0; r < 16; r++) s[th][r] = dp[th][r] = 0.0f;
-    // products 0 .. 39: S^T and dP^T of the two halves of the keys, in turn; 40 .. 63: dQ^T
+    // products 0 .. 39: S^T (12) and dP^T (8) of the two halves of the keys; 40 .. 63: dQ^T
     constexpr int kN = 64;
     u32x4 op[kN];
     uint32_t w[2][8], wl[2][8];  // dS of the halves, bf16 pairs; on the diagonal also what they leave out
     const auto fetch = [&](auto at) __attribute__((always_inline)) {
       constexpr int x = decltype(at)::value;
       if constexpr (x < 40) {
-        constexpr int th = x / 20, y = x % 20, kk = y < 16 ? y / 2 : y - 8;
-        if constexpr (y < 16 && y % 2) op[x] = *reinterpret_cast<const u32x4*>(bv + 8192 * th + ow[kk]);
+        constexpr int th = x / 20, y = x % 20, kk = y < 12 ? y : y - 12;
+        if constexpr (y >= 12) op[x] = *reinterpret_cast<const u32x4*>(bv + 8192 * th + ow[kk]);
         else if constexpr (kk < 8) op[x] = *reinterpret_cast<const u32x4*>(bk + 8192 * th + ow[kk]);
         else op[x] = *reinterpret_cast<const u32x4*>(br + 4096 * th + os[kk - 8]);
       } else {
@@ -190,8 +190,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dq_kernel(LatentArgs a)
     const auto use = [&](auto at) __attribute__((always_inline)) {
       constexpr int x = decltype(at)::value;
       if constexpr (x < 40) {
-        constexpr int th = x / 20, y = x % 20, kk = y < 16 ? y / 2 : y - 8;
-        if constexpr (y < 16 && y % 2) dp[th] = mfma(as_bf16x8(op[x]), df[kk], dp[th]);
+        constexpr int th = x / 20, y = x % 20, kk = y < 12 ? y : y - 12;
+        if constexpr (y >= 12) dp[th] = mfma(as_bf16x8(op[x]), df[kk], dp[th]);
         else s[th] = mfma(as_bf16x8(op[x]), qf[kk], s[th]);
       } else {
         constexpr int ks = (x - 40) / 6, dt = (x - 40) % 6, th = ks / 2, e = 4 * (ks % 2);
@@ -200,18 +200,18 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dq_kernel(LatentArgs a)
           acc[dt] = mfma(as_bf16x8(op[x]), as_bf16x8(u32x4{wl[th][e], wl[th][e + 1], wl[th][e + 2], wl[th][e + 3]}), acc[dt]);
       }
     };
-    const auto weigh = [&](int th, int e) __attribute__((always_inline)) {  // elements 2 e, 2 e + 1 of a half
-      float d[2];
-#pragma unroll
-      for (int u = 0; u < 2; u++) {
-        const int j = 2 * e + u, key = 32 * th + 8 * (j >> 2) + (j & 3);
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[th][j], c2, -ld.x));
-        d[u] = p * (dp[th][j] - ld.y);
-        if (edge) d[u] = key < hi ? d[u] : 0.0f;
-      }
-      w[th][e] = pack_bf16(d[0], d[1]);
-      if (edge) wl[th][e] = rest_bf16(w[th][e], d[0], d[1]);
-      asm volatile("" : "+v"(w[th][e]));  // (formed here, not where it is used)
+    // elements 2 e, 2 e + 1 of a half: P, then dS
+    float p[2][16];
+    const auto weigh = [&](int th, int j) __attribute__((always_inline)) {  // element j
+      p[th][j] = __builtin_amdgcn_exp2f(fmaf(s[th][j], c2, -ld.x));
+      if (edge) p[th][j] = 32 * th + 8 * (j >> 2) + (j & 3) < hi ? p[th][j] : 0.0f;
+      asm volatile("" : "+v"(p[th][j]));  // (formed here, not where it is used)
+    };
+    const auto slope = [&](int th, int e) __attribute__((always_inline)) {
+      const float d0 = p[th][2 * e] * (dp[th][2 * e] - ld.y), d1 = p[th][2 * e + 1] * (dp[th][2 * e + 1] - ld.y);
+      w[th][e] = pack_bf16(d0, d1);
+      if (edge) wl[th][e] = rest_bf16(w[th][e], d0, d1);
+      asm volatile("" : "+v"(w[th][e]));
     };
     each<kSlicesAhead>(fetch);
     each<kN>([&](auto at) __attribute__((always_inline)) {
@@ -219,8 +219,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dq_kernel(LatentArgs a)
       use(at);
       if constexpr (x + kSlicesAhead < kN) fetch(Index<x + kSlicesAhead>());
       if constexpr (x % 5 == 3 && x / 5 < kLatBwdDma) stage_piece(nt, nbuf, x / 5);
-      if constexpr (x >= 22 && x < 38 && x % 2 == 0) weigh(0, (x - 22) / 2);
-      if constexpr (x >= 42 && x < 50) weigh(1, x - 42);
+      // one exponential to a slice, which with the operand reads is about what fits beside its product
+      if constexpr (x >= 13 && x < 29) weigh(0, x - 13);
+      if constexpr (x >= 25 && x < 33) slope(0, x - 25);
+      if constexpr (x >= 33 && x < 49) weigh(1, x - 33);
+      if constexpr (x >= 44 && x < 52) slope(1, x - 44);
       slice_end();
     });
     dma_wait();

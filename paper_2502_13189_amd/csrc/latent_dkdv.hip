@@ -103,7 +103,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
     for (int st = 0; st < 2; st++)
 #pragma unroll
       for (int r = 0; r < 16; r++) s[st][r] = dp[st][r] = 0.0f;
-    // products 0 .. 39: S and dP of the two halves of the rows, in turn; 40 .. 79: dV^T and dK^T
+    // products 0 .. 39: S (12) and dP (8) of the two halves of the rows; 40 .. 79: dV^T and dK^T
     constexpr int kN = 80;
     u32x4 op[kN];
     uint32_t wp[2][8], wd[2][8], wl[2][8];  // P and dS of the halves, bf16 pairs; and what dS's leave out
@@ -111,8 +111,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
     const auto fetch = [&](auto n_) __attribute__((always_inline)) {
       constexpr int x = decltype(n_)::value;
       if constexpr (x < 40) {
-        constexpr int st = x / 20, y = x % 20, kk = y < 16 ? y / 2 : y - 8;
-        if constexpr (y < 16 && y % 2) op[x] = *reinterpret_cast<const u32x4*>(bd + 8192 * st + ow[kk]);
+        constexpr int st = x / 20, y = x % 20, kk = y < 12 ? y : y - 12;
+        if constexpr (y >= 12) op[x] = *reinterpret_cast<const u32x4*>(bd + 8192 * st + ow[kk]);
         else if constexpr (kk < 8) op[x] = *reinterpret_cast<const u32x4*>(bq + 8192 * st + ow[kk]);
         else op[x] = *reinterpret_cast<const u32x4*>(br + 4096 * st + os[kk - 8]);
       } else {
@@ -125,8 +125,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
     const auto use = [&](auto n_) __attribute__((always_inline)) {
       constexpr int x = decltype(n_)::value;
       if constexpr (x < 40) {
-        constexpr int st = x / 20, y = x % 20, kk = y < 16 ? y / 2 : y - 8;
-        if constexpr (y < 16 && y % 2) dp[st] = mfma(as_bf16x8(op[x]), vf[kk], dp[st]);
+        constexpr int st = x / 20, y = x % 20, kk = y < 12 ? y : y - 12;
+        if constexpr (y >= 12) dp[st] = mfma(as_bf16x8(op[x]), vf[kk], dp[st]);
         else s[st] = mfma(as_bf16x8(op[x]), kf[kk], s[st]);
       } else {
         constexpr int y = x - 40, st = y / 20, e = 4 * (y / 10 % 2), z = y % 10;
@@ -138,28 +138,30 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
           dk[z - 4] = mfma(as_bf16x8(op[x]), as_bf16x8(u32x4{wl[st][e], wl[st][e + 1], wl[st][e + 2], wl[st][e + 3]}), dk[z - 4]);
       }
     };
-    // elements 2 e, 2 e + 1 of a half: rows r, r + 1
-    const auto fetch_ld = [&](int st, int e) __attribute__((always_inline)) {
-      const int r = 32 * st + 8 * (e >> 1) + 4 * hh + 2 * (e & 1);
-      lv[8 * st + e] = *reinterpret_cast<const float2*>(&lse2[cur][r]);
-      dl[8 * st + e] = *reinterpret_cast<const float2*>(&dlt[cur][r]);
+    // elements 2 e, 2 e + 1 of a half, rows r and r + 1: P, then dS
+    float p[2][16];
+    const auto row_at = [&](int st, int e) { return 32 * st + 8 * (e >> 1) + 4 * hh + 2 * (e & 1); };
+    const auto fetch_lse = [&](int st, int e) __attribute__((always_inline)) {
+      lv[8 * st + e] = *reinterpret_cast<const float2*>(&lse2[cur][row_at(st, e)]);
     };
-    const auto weigh = [&](int st, int e) __attribute__((always_inline)) {
-      const int r = 32 * st + 8 * (e >> 1) + 4 * hh + 2 * (e & 1);
-      const float2 l = lv[8 * st + e], d = dl[8 * st + e];
-      float p0 = __builtin_amdgcn_exp2f(fmaf(s[st][2 * e], c2, -l.x)), p1 = __builtin_amdgcn_exp2f(fmaf(s[st][2 * e + 1], c2, -l.y));
-      float d0 = p0 * (dp[st][2 * e] - d.x), d1 = p1 * (dp[st][2 * e + 1] - d.y);
-      if (edge) {
-        const int at = i * kLatTile + r;
-        p0 = at >= key ? p0 : 0.0f;
-        d0 = at >= key ? d0 : 0.0f;
-        p1 = at + 1 >= key ? p1 : 0.0f;
-        d1 = at + 1 >= key ? d1 : 0.0f;
-      }
-      wp[st][e] = pack_bf16(p0, p1);
+    const auto fetch_delta = [&](int st, int e) __attribute__((always_inline)) {
+      dl[8 * st + e] = *reinterpret_cast<const float2*>(&dlt[cur][row_at(st, e)]);
+    };
+    const auto weigh = [&](int st, int j) __attribute__((always_inline)) {  // element j
+      const float2 l = lv[8 * st + j / 2];
+      float x = __builtin_amdgcn_exp2f(fmaf(s[st][j], c2, j % 2 ? -l.y : -l.x));
+      if (edge) x = i * kLatTile + row_at(st, j / 2) + j % 2 >= key ? x : 0.0f;
+      p[st][j] = x;
+      if (j % 2) wp[st][j / 2] = pack_bf16(p[st][j - 1], x);
+      asm volatile("" : "+v"(p[st][j]));  // (formed here, not where it is used)
+      if (j % 2) asm volatile("" : "+v"(wp[st][j / 2]));
+    };
+    const auto slope = [&](int st, int e) __attribute__((always_inline)) {
+      const float2 d = dl[8 * st + e];
+      const float d0 = p[st][2 * e] * (dp[st][2 * e] - d.x), d1 = p[st][2 * e + 1] * (dp[st][2 * e + 1] - d.y);
       wd[st][e] = pack_bf16(d0, d1);
       if (edge) wl[st][e] = rest_bf16(wd[st][e], d0, d1);
-      asm volatile("" : "+v"(wp[st][e]), "+v"(wd[st][e]));  // (formed here, not where they are used)
+      asm volatile("" : "+v"(wd[st][e]));
     };
     each<kSlicesAhead>(fetch);
     each<kN>([&](auto n_) __attribute__((always_inline)) {
@@ -167,10 +169,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
       use(n_);
       if constexpr (x + kSlicesAhead < kN) fetch(Index<x + kSlicesAhead>());
       if constexpr (x % 6 == 4 && x / 6 < kLatBwdDma) stage_piece(nt, nbuf, x / 6);
-      if constexpr (x >= 18 && x < 34 && x % 2 == 0) fetch_ld(0, (x - 18) / 2);
-      if constexpr (x >= 22 && x < 38 && x % 2 == 0) weigh(0, (x - 22) / 2);
-      if constexpr (x >= 38 && x < 54 && x % 2 == 0) fetch_ld(1, (x - 38) / 2);
-      if constexpr (x >= 42 && x < 58 && x % 2 == 0) weigh(1, (x - 42) / 2);
+      // one exponential or one pair of dS to a slice, which is about what fits beside its product
+      if constexpr (x >= 9 && x < 25 && x % 2 == 1) fetch_lse(0, (x - 9) / 2);
+      if constexpr (x >= 13 && x < 29) weigh(0, x - 13);
+      if constexpr (x >= 25 && x < 33) fetch_delta(0, x - 25);
+      if constexpr (x >= 29 && x < 37) slope(0, x - 29);
+      if constexpr (x >= 33 && x < 49 && x % 2 == 1) fetch_lse(1, (x - 33) / 2);
+      if constexpr (x >= 37 && x < 53) weigh(1, x - 37);
+      if constexpr (x >= 49 && x < 57) fetch_delta(1, x - 49);
+      if constexpr (x >= 53 && x < 61) slope(1, x - 53);
       slice_end();
     });
     dma_wait();

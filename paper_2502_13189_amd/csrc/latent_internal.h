@@ -13,7 +13,8 @@ constexpr int kRow = kRank + kRopeDim;  // numbers a token has in the cache
 
 // ------------------------------------------------------------- expanded form
 constexpr int kLatRows = 256;   // query rows of a forward work-group (or half of it)
-constexpr int kLatSmall = 256;  // work-groups up to which half of it is better
+constexpr int kLatFew = 1024;   // half of it: up to so many work-groups,
+constexpr int kLatLong = 4096;  // or for sequences shorter than this, on average
 constexpr int kLatRowsDq = 128; // of a dQ work-group
 constexpr int kLatKeys = 128;   // keys of a dK/dV work-group
 constexpr int kLatTile = 64;    // tokens of a staged tile
