@@ -303,6 +303,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     const Src first2 = Src{__builtin_amdgcn_readfirstlane(ids2), 0};
     // where the step after stands
     Src next = step + 1 < last ? source(s, step + 1) : first2;
+    const char* src = origin(next);
 
     for (; step < last; step++, x++, par ^= 1) {
       u32x4* lb = lds + par * kStepChunks;
@@ -318,7 +319,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
       at = next;
       // the next step's DMA goes out piece by piece, between the products: 18 at once would hold the wave up for
       // as long as all products take
-      const char* src = origin(at);
       const uint32_t to = par ? to0 : to1;
       // (with no step to come they fetch next to nothing, into a buffer that nothing reads)
       const uint32_t on = step + 1 < last || s2 != s ? ~0u : 0;
@@ -340,10 +340,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
           if (k + kAhead < kNk) fetch(k + kAhead);
           if (k < kDmaFirst) stage(k, src, to, on);
         }
-#pragma unroll
-        for (int u = 0; u < kHs; u++)
-#pragma unroll
-          for (int i = 0; i < 4; i++) z[u][i] *= c2;
       }
       if (live < kLatStep) {
 #pragma unroll
@@ -362,7 +358,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
           ts[u] = 0.0f;
 #pragma unroll
           for (int j = 0; j < 4; j++) {
-            p[j] = __builtin_amdgcn_exp2f(z[u][j] - mu);
+            p[j] = __builtin_amdgcn_exp2f(fmaf(z[u][j], c2, -mu));
             ts[u] += p[j];
           }
           *reinterpret_cast<uint2*>(&pl[(16 * u + cs) * kPRow + 16 * wave + 4 * gs]) =
@@ -375,11 +371,29 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
       for (int u = 0; u < kHs; u++) high |= ts[u] > kMaxWeight || m[u] == -INFINITY;
       if (high) flag[par] = 1;
       __syncthreads();
-      if (flag[par] != 0) {
+      // (the first operands of the values are on their way while the flag is looked at)
+      const int raise = flag[par];
+      constexpr int kY = kKs * kDt;
+      s16x4 t0[kY], t1[kY];
+      bf16x8 pb[kKs * kHt];
+      const auto value = [&](int y) {
+        const int ks = y / kDt, dt = y % kDt;
+        if (dt == 0) {
+#pragma unroll
+          for (int t = 0; t < kHt; t++)
+            pb[ks * kHt + t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(T * t + c) * kPRow + V::kK * ks + 8 * g]));
+        }
+        const char* b = buf + V::kK * ks * (kRowChunks * 16) + 128 * (dt / kPd);
+        t0[y] = tr16(b + otr[0][dt % kPd]);
+        t1[y] = tr16(b + otr[1][dt % kPd]);
+      };
+#pragma unroll
+      for (int y = 0; y < kAhead / 2; y++) value(y);
+      if (raise != 0) {
         // the step's max of every head, over the waves
 #pragma unroll
         for (int u = 0; u < kHs; u++) {
-          float mx = fmaxf(fmaxf(z[u][0], z[u][1]), fmaxf(z[u][2], z[u][3]));
+          float mx = fmaxf(fmaxf(z[u][0], z[u][1]), fmaxf(z[u][2], z[u][3])) * c2;
           mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
           mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
           if (gs == 0) red[wave][16 * u + cs] = fmaxf(mx, m[u]);
@@ -411,34 +425,22 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 #pragma unroll
             for (int i = 0; i < V::kN; i++) o[dt][t][i] *= f;
         }
+#pragma unroll
+        for (int y = 0; y < kAhead / 2; y++) value(y);  // (the weights are others now)
       }
 #pragma unroll
       for (int u = 0; u < kHs; u++) l[u] += ts[u];
       // ---- values
       {
-        constexpr int kY = kKs * kDt;
-        s16x4 t0[kY], t1[kY];
-        bf16x8 pb[kKs * kHt];
-        const auto fetch = [&](int y) {
-          const int ks = y / kDt, dt = y % kDt;
-          if (dt == 0) {
-#pragma unroll
-            for (int t = 0; t < kHt; t++)
-              pb[ks * kHt + t] = as_bf16x8(*reinterpret_cast<const u32x4*>(&pl[(T * t + c) * kPRow + V::kK * ks + 8 * g]));
-          }
-          const char* b = buf + V::kK * ks * (kRowChunks * 16) + 128 * (dt / kPd);
-          t0[y] = tr16(b + otr[0][dt % kPd]);
-          t1[y] = tr16(b + otr[1][dt % kPd]);
-        };
-#pragma unroll
-        for (int y = 0; y < kAhead / 2; y++) fetch(y);
+        const char* src2 = origin(next);
 #pragma unroll
         for (int y = 0; y < kY; y++) {
 #pragma unroll
           for (int t = 0; t < kHt; t++) o[y % kDt][t] = product(join16(t0[y], t1[y]), pb[y / kDt * kHt + t], o[y % kDt][t]);
-          if (y + kAhead / 2 < kY) fetch(y + kAhead / 2);
+          if (y + kAhead / 2 < kY) value(y + kAhead / 2);
           if (y < kDma - kDmaFirst) stage(kDmaFirst + y, src, to, on);
         }
+        src = src2;
       }
     }
 
