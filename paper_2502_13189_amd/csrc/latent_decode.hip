@@ -74,10 +74,13 @@ struct Tile<32> {
   }
 };
 
-__device__ __forceinline__ int steps_of(const LatentDecodeArgs& a, int s) {
+// Tokens of a request, and its steps.
+__device__ __forceinline__ int tokens_of(const LatentDecodeArgs& a, int s) {
   const int64_t n = a.lens[s], most = (int64_t)a.W * a.P;
-  return (int)(((n < 0 ? 0 : n > most ? most : n) + kLatStep - 1) / kLatStep);
+  return (int)(n < 0 ? 0 : n > most ? most : n);
 }
+__device__ __forceinline__ int steps_in(int tokens) { return (int)(((uint32_t)tokens + kLatStep - 1) / kLatStep); }
+__device__ __forceinline__ int steps_of(const LatentDecodeArgs& a, int s) { return steps_in(tokens_of(a, s)); }
 
 // The line of n steps (below 2^30) in runs, one a share: the first n % shares of them are a step longer.
 struct Runs {
@@ -241,10 +244,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 #pragma unroll
     for (int x = 0; x < kDma; x++) stage(x, src, to0, ~0u);
   }
+  int len = __builtin_amdgcn_readfirstlane(tokens_of(a, s));
   for (uint32_t x = x0; x < x1;) {
     // ---------------------------------------------------------- one request
-    const int len = __builtin_amdgcn_readfirstlane((int)min((int64_t)a.lens[s], (int64_t)a.W * a.P));
-    const int ns = (int)(((uint32_t)len + kLatStep - 1) / kLatStep);
+    const int ns = steps_in(len);
     const int last = (int)min((uint32_t)ns, x1 - sx);  // steps step .. last - 1 are the run's
     const bool whole = step == 0 && last == ns;
     const int64_t pslot = ((int64_t)w * 2 + (x == x0 ? 0 : 1)) * a.groups + hg;
@@ -263,9 +266,20 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
         const int64_t h = min(h0 + r, a.H - 1);
         dma16(ch < kRank / 8 ? qc + h * a.qc_sh + 8 * ch : qr + h * a.qr_sh + 8 * (ch - kRank / 8), lq + 64 * j);
       }
-      dma_wait();
-      __syncthreads();
     }
+    // the request after this one, if the run goes on
+    int s2 = s, len2 = 0;
+    uint32_t sx2 = sx;
+    if (sx + ns < x1) {
+      sx2 = sx + ns;
+      do len2 = __builtin_amdgcn_readfirstlane(tokens_of(a, ++s2));
+      while (len2 == 0);
+    }
+    int ids2 = s2 != s ? entries(s2, 0) : 0;
+    asm volatile("" : "+v"(ids2));
+    const Src first2 = Src{__builtin_amdgcn_readfirstlane(ids2), 0};
+    dma_wait();
+    __syncthreads();
     // Into the accumulation registers, where the matrix cores read them as well as anywhere, as many as
     // those hold (the others are full); a few at a time, which is all that fits on the way.
     u32x4 qf[kHs][kNk];
@@ -290,17 +304,6 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 #pragma unroll
       for (int t = 0; t < kHt; t++) o[dt][t] = V::zero();
 
-    // the request after this one, if the run goes on
-    int s2 = s;
-    uint32_t sx2 = sx;
-    if (sx + ns < x1) {
-      sx2 = sx + ns;
-      do s2++;
-      while (__builtin_amdgcn_readfirstlane(steps_of(a, s2)) == 0);
-    }
-    int ids2 = s2 != s ? entries(s2, 0) : 0;
-    asm volatile("" : "+v"(ids2));
-    const Src first2 = Src{__builtin_amdgcn_readfirstlane(ids2), 0};
     // where the step after stands
     Src next = step + 1 < last ? source(s, step + 1) : first2;
     const char* src = origin(next);
@@ -494,6 +497,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     s = s2;
     sx = sx2;
     step = 0;
+    len = len2;
     p0 = 0;
     ids = ids2;
   }
