@@ -94,9 +94,9 @@ struct Runs {
   }
 };
 
-// dma16_at with the LDS address in a scalar register.
+// dma16_at with the LDS address in a scalar register (the s_nop: see there).
 __device__ __forceinline__ void dma16_to(const char* base, uint32_t off, uint32_t to) {
-  asm volatile("global_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "{m0}"(to) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "{m0}"(to) : "memory");
 }
 
 template <int M>

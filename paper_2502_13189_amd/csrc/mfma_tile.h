@@ -105,7 +105,8 @@ __device__ __forceinline__ void dma_lanes(Dma<NW>& D, int wave, int lane, int64_
 // before any later LDS read it cannot prove disjoint from the DMA's target
 // (which it cannot for buffers chosen at run time), defeating the prefetch.
 // Every caller therefore waits for its DMA explicitly (dma_wait) before the
-// barrier that publishes the data.
+// barrier that publishes the data.  A write to M0 asks for one wait state before an LDS DMA reads it,
+// which the compiler does not count into inline assembly either: hence the s_nop.
 __device__ __forceinline__ uint32_t lds_addr(const u32x4* p) {
   return __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p);
@@ -113,14 +114,14 @@ __device__ __forceinline__ uint32_t lds_addr(const u32x4* p) {
 
 // A per-lane 64-bit source address (gathered rows).
 __device__ __forceinline__ void dma16(const void* gsrc, u32x4* ldst) {
-  asm volatile("global_load_lds_dwordx4 %0, off" : : "v"(gsrc), "{m0}"(lds_addr(ldst)) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(gsrc), "{m0}"(lds_addr(ldst)) : "memory");
 }
 
 // A wave-uniform base (scalar registers) plus a 32-bit per-lane byte offset:
 // one vector register per address instead of two, which keeps the attention
 // kernels' register allocation free of spills.
 __device__ __forceinline__ void dma16_at(const char* base, uint32_t off, u32x4* ldst) {
-  asm volatile("global_load_lds_dwordx4 %0, %1"
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                : : "v"(off), "s"(base), "{m0}"(lds_addr(ldst)) : "memory");
 }
 
