@@ -197,6 +197,77 @@ def test_gradient_against_differences():
         assert abs(got - want) <= float((tol[i] * d.abs()).sum()) + 1e-4, i
 
 
+def test_far_rows():
+    """Token strides that put rows beyond 2^31 elements; inputs, outputs and gradients apart in one buffer."""
+    T, H, st = 300, 2, 1 << 23
+    big = torch.empty(T * st, dtype=BF, device=DEV)
+    q, k, kr, v = inputs(T, H, seed=6)
+    dout = randn(T, H, 128, seed=7)
+    cu = cu_of((299, 1))
+
+    def place(x, at):
+        y = big.as_strided(x.shape, (st, 192, 1) if x.dim() == 3 else (st, 1), at)
+        y.copy_(x)
+        return y
+
+    q2, k2, v2, kr2, g2 = place(q, 0), place(k, 512), place(v, 1024), place(kr, 1536), place(dout, 2048)
+    blank = lambda x, at: place(torch.zeros_like(x, memory_format=torch.contiguous_format), at)  # noqa: E731
+    out, dq, dk, dv, dkr = (blank(x, 2560 + 512 * i) for i, x in enumerate((v, q, k, v, kr)))
+    _, lse = binding.latent_forward(q2, k2, kr2, v2, cu, out=out)
+    check_forward(q, k, kr, v, cu, out, lse)
+    grads = binding.latent_backward(q2, k2, kr2, v2, cu, out, lse, g2, dq=dq, dk=dk, dk_rope=dkr, dv=dv)
+    check_backward(q, k, kr, v, cu, dout, grads)
+
+
+def test_side_streams():
+    """Calls on several streams at once, outputs and workspaces allocated for the stream of their call."""
+    lens, H = (150, 333), 3
+    T = sum(lens)
+    sets = [(*inputs(T, H, seed=10 * i), randn(T, H, 128, seed=10 * i + 5)) for i in range(3)]
+    cu = cu_of(lens)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = []
+    for (q, k, kr, v, dout), st in zip(sets, streams):
+        for _ in range(4):
+            out, lse = binding.latent_forward(q, k, kr, v, cu, stream=st)
+            grads = binding.latent_backward(q, k, kr, v, cu, out, lse, dout, stream=st)
+        got.append((out, lse, *grads))
+    torch.cuda.synchronize()
+    for (q, k, kr, v, dout), x in zip(sets, got):
+        out, lse = binding.latent_forward(q, k, kr, v, cu)
+        for a, b in zip(x, (out, lse, *binding.latent_backward(q, k, kr, v, cu, out, lse, dout))):
+            assert torch.equal(a, b)
+
+
+def test_backward_workspace():
+    """A workspace of the exact size, holding NaN; one too small is refused."""
+    T, H = 100, 3
+    q, k, kr, v = inputs(T, H)
+    cu, dout = cu_of((60, 40)), randn(T, H, 128, seed=5)
+    out, lse = binding.latent_forward(q, k, kr, v, cu)
+    want = binding.latent_backward(q, k, kr, v, cu, out, lse, dout)
+    need = binding.latent_backward_workspace_bytes(T, H)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device=DEV)
+    for _ in range(2):
+        for a, b in zip(want, binding.latent_backward(q, k, kr, v, cu, out, lse, dout, workspace=ws)):
+            assert torch.equal(a, b)
+    with pytest.raises(binding.MobaError, match="NO_MEMORY"):
+        binding.latent_backward(q, k, kr, v, cu, out, lse, dout, workspace=ws[:need - 1])
+
+
+def test_long_sequences():
+    """The forward's work-groups of 256 queries (many long sequences): rows of each of them."""
+    T, H = 8300, 33
+    q, k, kr, v = inputs(T, H, seed=8)
+    cu = cu_of((T,))
+    out, lse = binding.latent_forward(q, k, kr, v, cu)
+    for h in (0, 17, 32):
+        r = ref.Attention(q[:, h:h + 1], k[:, h:h + 1], kr, v[:, h:h + 1])
+        assert ref.worst(out[:, h:h + 1].transpose(0, 1), r.out, r.out_bound()) <= 1.0
+        assert ref.worst(lse[h:h + 1], r.lse, r.lse_bound()) <= 1.0
+
+
 def test_graph_of_forward_and_backward():
     """Captured together, replayed on new inputs beside eager calls of the same shapes."""
     lens, H = (200, 57), 3
