@@ -421,8 +421,8 @@ size_t moba_cache_decode_workspace_bytes(int64_t S, int64_t W, int32_t Hq, int32
  * from R on are copied.  To turn the last dims of wider heads, pass views of them.
  *
  *   freqs   [R / 2] f64 contiguous: radians a position, scaled for longer contexts as the caller
- *           wants it.  Angles are formed in 64-bit integers (a fraction of a turn): exact to 2^-53 of a
- *           frequency at any position, of either sign
+ *           wants it.  Angles are formed in 64-bit integers (a fraction of a turn): exact to 2^-52 of a turn
+ *           (or of the frequency's turns a position, where they are more than one) times the position
  *   pos     [T] i32 or i64 contiguous: the rows' positions; or NULL, with
  *   cu_seqlens [S + 1] i32 contiguous, DEVICE memory, non-decreasing: row t of sequence s stands at
  *           position start[s] + t - cu_seqlens[s]; rows outside [cu_seqlens[0], cu_seqlens[S]) are left as they are

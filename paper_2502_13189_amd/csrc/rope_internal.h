@@ -65,10 +65,11 @@ __device__ __forceinline__ bool row_position(const Rotation& r, int64_t t, int64
 
 // A frequency as turns a position, a 64-bit fraction: whole turns do not count, so the angle of
 // any position is that fraction times the position modulo 2^64, exact but for the fraction's own
-// rounding (2^-53 of a frequency: 2^-33 radians at position 2^20).
+// rounding (below 2^-52 of a turn: 2^-30 radians at position 2^20, frequencies up to 1).
 __device__ __forceinline__ uint64_t turns_of(double freq) {
   const double turns = freq * 0.15915494309189533577;  // 1 / (2 pi)
-  return (uint64_t)((turns - floor(turns)) * 18446744073709551616.0);
+  // (a little below 0 rounds to a whole turn, which 64 bits do not hold)
+  return (uint64_t)(fmin(turns - floor(turns), 0x1.fffffffffffffp-1) * 18446744073709551616.0);
 }
 
 // cos and sin of a 64-bit fraction of a turn.  The nearest quarter turn is taken off exactly; the rest, x

@@ -81,6 +81,23 @@ def test_far_positions(p):
     assert bool(((got.cpu().double() - y).abs() <= tol).all()), ref.worst(got.cpu(), y, tol)
 
 
+@pytest.mark.parametrize("p", [1, 2 ** 20, -(2 ** 20), 2 ** 31 - 1])
+def test_frequencies_about_zero(p):
+    """Frequencies of either sign, down to ones whose turn is lost beside 1: a whole turn less almost nothing."""
+    freqs = torch.tensor([-1e-18, -1e-30, -5e-324, 1e-30, -1e-16, -1e-3, -6.5, -0.0], dtype=torch.float64)
+    r = binding.Rotation(freqs.to(DEV))
+    x = randn(1, 1, 16, dtype=F32, seed=4)
+    got, _ = binding.rope(x, None, r, pos=torch.tensor([p], dtype=torch.int64, device=DEV))
+    back, _ = binding.rope_backward(x, None, r, pos=torch.tensor([-p], dtype=torch.int64, device=DEV))
+    y = ref.rotate(x, torch.tensor([p], dtype=torch.int64, device=DEV), r.freqs, 1.0, False)
+    # (the reference's angles: 2^-53 of up to 6.5 p; the kernel's: 2^-52 of a turn a position)
+    extra = abs(p) * (6.5 * 2.0 ** -53 + 2.0 ** -52 * 2 * math.pi)
+    size = x.double().abs()
+    tol = ref.rotate_bound(x, y, 8, 1.0, False, 2.0 ** -24) + extra * (size + size.roll(8, -1))
+    assert bool(((got.double() - y).abs() <= tol).all()), ((got.double() - y).abs() / tol).max()
+    assert bool(((back.double() - y).abs() <= tol).all())
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_views(interleaved):
     """Parts of wider heads, heads outermost, offsets that leave rows aligned to one element only."""
