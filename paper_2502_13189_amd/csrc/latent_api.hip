@@ -263,8 +263,14 @@ moba_status decode_shape(int64_t S, int64_t W, int64_t H, int64_t P, LatentShape
   if (H > 4096 || S >= kMost || W >= kMost || S * W >= (int64_t(1) << 30) / (P / kLatStep) ||
       S * H >= int64_t(1) << 23)
     return MOBA_ERR_UNSUPPORTED;
-  // heads of a group: what a work-group's registers hold, no more than there are
-  d->heads = H <= 16 ? 16 : H <= 32 ? 32 : 64;
+  // heads of a group: 64, what a work-group's registers hold, read a row the fewest times; but fewer where the batch
+  // (as far as the table says) has so little work that a step's length counts, and no more than there are.  16, 32 and
+  // 64, us a call: 8000 tokens, 128 heads 20.0, 26.0, 37.3; 64000, 64 heads 35.7, 35.4, 46.5; 64 x 1000, 64 heads
+  // 31, 33, 37; 64000, 128 heads 52.5, 42.5, 44.4; 192000, 64 heads 73, 59, 66; 128000, 128 heads 88, 65, 60; 64000,
+  // 256 heads 87, 63, 57; 64 x 4000, 64 heads 98 (32), 90 (64).
+  const int64_t work = S * W * P * H;  // (below 2^48)
+  const int most = work <= 3 << 20 ? 16 : work <= 3 << 22 ? 32 : 64;
+  d->heads = H <= 16 ? 16 : H <= 32 ? std::min(most, 32) : most;
   d->groups = (int)ceil_div(H, d->heads);
   const int64_t steps = std::max<int64_t>(1, S * W * (P / kLatStep));  // at most
   d->shares = (int)std::min<int64_t>(std::max(1, kLatGroups / d->groups), steps);

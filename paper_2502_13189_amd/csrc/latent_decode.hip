@@ -2,21 +2,29 @@
 // numbers, 512 of the latent vector and 64 of the rotary key, for all heads.  For a head's query
 // (qc, qr): z_j = scale <(qc, qr), u_j>, out = sum_j softmax(z)_j u_j[0:512].
 //
-// A row is 1152 bytes and 2176 operations a head: 64 heads and more are bound by the matrix cores about as
-// much as by memory, few heads by memory alone.  A row is read once for scores and values: it is staged in
+// A row is 1152 bytes and 2176 operations a head: at 128 heads the matrix cores take about as long as
+// memory does, with fewer heads memory is the bound.  A row is read once for scores and values: it is staged in
 // LDS and serves as the row operand of the first product and, by transposed reads, of the second.
 //
 // Work-group = 4 waves, a group of M = 16, 32 or 64 heads, one on each CU.  The batch's steps (64 tokens of a
-// request) stand in one line, and every share of heads-groups work-groups takes an equal run of it; a
+// request) stand in one line, cut into equal runs, one for each share: a work-group for each group of heads.  A
 // request that lies in one run is finished there, the others leave partials that a second kernel joins.
 // Two buffers of 64 rows (72 KiB each), step i + 1 in flight while step i is used.  On
 // v_mfma_f32_32x32x16_bf16 (M = 64) or v_mfma_f32_16x16x32_bf16, per step:
-//   S^T (tokens x heads) = U . Q^T   the waves share out tokens and heads (M = 64: 2 x 2, else 4 x 1),
-//                                    Q in registers
+//   S^T (tokens x heads) = U . Q^T   wave w scores tokens 16 w .. of all heads, Q in registers
 //   P^T under the running max, through LDS as bf16, for all waves
 //   O^T (dims x heads) += U^T . P^T  wave w owns dims 128 w .. 128 w + 127
 // The running max is raised only when some weight of the step passes 2^8; the step's weights are then formed
-// again.
+// again.  The weights enter the second product as bf16, all sums are fp32.
+//
+// 2^20 tokens, 128 heads: 334 us (6.5 us the join's share of a row, 13 us in all), 3.6 TB/s and 870 TFLOP/s.  A
+// step of M = 64 takes some 5200 cycles at the 2.0 GHz that the chip keeps under this load: scores 2400 (1152 of
+// products; the DMA's 18 instructions a wave go out beside them, and the path from L2 to LDS, 33 bytes a cycle of a
+// CU, needs 2200 for a step's rows), weights 650, values 1500 (1024), flag and barriers 300.  A run's start, the
+// chain lengths - table - rows - queries, takes 11 us.  Groups of 128 heads (a row read once for all, 7700 cycles a step
+// of twice the work) were tried: 2^20 tokens 283 us, but the partials and their join double: 304 in all against 346
+// there, 155 against 136 for 48 requests of 100 to 30000 tokens, 86 against 64 for 128 of 1000.  Two waves a SIMD
+// with half the dims each: 354 against 345 (2^20 tokens, whole call), the registers spill.
 #include "latent_internal.h"
 #include "latent_tile.h"
 
@@ -601,7 +609,8 @@ hipError_t decode(const LatentDecodeArgs& a, hipStream_t st) {
 template <int M>
 hipError_t join(const LatentDecodeArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)((int64_t)a.S * a.groups * (M * kRank / 4 / 256));
-  // few requests: many partials each
+  // few requests: many partials each.  One thread a piece and four, us a call: 131072 tokens, 16 heads 57, 45, 128
+  // heads 71, 61; 8 x 16000 35.6, 35.4 and 63, 66; 16 x 8000 34.7, 35.0 and 63, 72; 64 x 4000 62, 67 and 120, 164.
   if (a.S <= 8) latent_join_kernel<M, 4><<<grid, 1024, 0, st>>>(a);
   else latent_join_kernel<M, 1><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();

@@ -334,6 +334,19 @@ def test_decode(lens, page, H):
     assert torch.equal(out, out2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("H", [17, 33, 40, 64, 128, 130])
+@pytest.mark.parametrize("lens,page", [((1,), 64), ((700, 333, 0), 64), ((0, 64, 65, 63, 0, 128, 1, 0), 128),
+                                       ((5000,), 192), ((1, 20011, 0, 300, 256, 257), 256)])
+def test_decode_wide_tables(lens, page, H):
+    """Tables far wider than the requests, as a captured step has them: the heads go in the largest groups."""
+    pages, table, ln, rows = paged(lens, page, seed=H)
+    more = -(-(1 << 24) // (len(lens) * page * H))
+    table = torch.cat([table, torch.full((len(lens), more), -1, dtype=torch.int32, device=DEV)], 1)
+    qc, qr = randn(len(lens), H, 512, seed=1), randn(len(lens), H, 64, seed=2)
+    out, lse = binding.latent_decode(qc, qr, pages, table, ln)
+    check_decode(qc, qr, rows, out, lse)
+
+
 @pytest.mark.parametrize("H", [8, 20, 128])
 def test_decode_many_requests(H):
     """More requests than work-groups, many in one run, some split over two."""
