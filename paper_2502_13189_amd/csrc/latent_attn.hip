@@ -14,6 +14,8 @@
 // diagonal one; those before it are whole, those behind it are left out.
 // The weights enter the second product as bf16 (2^-9 of each, independent of each other: it adds
 // to the result about what its own rounding to bf16 does); all sums are fp32.
+// 16384 tokens, 32 heads: 2.24 to 2.34 ms, 1.18 to 1.23 PFLOP/s of the 1.23 to 1.39 that large matrix products reach here
+// (the chip's clock falls under either).
 #include "latent_tile.h"
 
 #include <math.h>

@@ -17,14 +17,16 @@
 // The running max is raised only when some weight of the step passes 2^8; the step's weights are then formed
 // again.  The weights enter the second product as bf16, all sums are fp32.
 //
-// 2^20 tokens, 128 heads: 334 us (6.5 us the join's share of a row, 13 us in all), 3.6 TB/s and 870 TFLOP/s.  A
-// step of M = 64 takes some 5200 cycles at the 2.0 GHz that the chip keeps under this load: scores 2400 (1152 of
-// products; the DMA's 18 instructions a wave go out beside them, and the path from L2 to LDS, 33 bytes a cycle of a
-// CU, needs 2200 for a step's rows), weights 650, values 1500 (1024), flag and barriers 300.  A run's start, the
-// chain lengths - table - rows - queries, takes 11 us.  Groups of 128 heads (a row read once for all, 7700 cycles a step
-// of twice the work) were tried: 2^20 tokens 283 us, but the partials and their join double: 304 in all against 346
-// there, 155 against 136 for 48 requests of 100 to 30000 tokens, 86 against 64 for 128 of 1000.  Two waves a SIMD
-// with half the dims each: 354 against 345 (2^20 tokens, whole call), the registers spill.
+// 2^20 tokens, 128 heads: 334 us and the join 13, 3.6 TB/s and 870 TFLOP/s; 48 requests of 100 to 30000 tokens
+// (261732 in all), 128 heads: 124 and 12.  A step of M = 64 takes some 5000 cycles at the 2.0 GHz that the chip keeps
+// under this load: scores 2400 (1152 of products; the DMA's 18 instructions a wave go out beside them, and the path
+// from L2 to LDS, 33 bytes a cycle of a CU, needs 2200 for a step's rows), weights 650, values 1500 (1024), flag and
+// barriers 300.  A run's start, the chain lengths - table - rows - queries, takes 11 us.
+//
+// Tried, whole calls: groups of 128 heads, a row read once for all, 7700 cycles a step of twice the work, but twice
+// the partials to write and join: 2^20 tokens 326 us against 345, the 48 requests 155 against 132, 128 of 1000 tokens
+// 86 against 64, so it pays from some 10^6 tokens a call on alone.  Two waves a SIMD, half the dims each: 354 against
+// 345, since their registers spill.
 #include "latent_internal.h"
 #include "latent_tile.h"
 

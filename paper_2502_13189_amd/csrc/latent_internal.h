@@ -65,7 +65,7 @@ struct LatentDecodeArgs {
   int shares;                                      // of the batch's steps, for each group of heads
   int groups;                                      // groups of heads
   // workspace
-  float* part_o;     // [shares, 2, groups, heads of a group * 512]: unnormalised partials, as the lanes hold them
+  float* part_o;     // [shares, 2, groups, heads of a group * 512]: unnormalised partials, as the join reads them
   float2* part_ml;   // [shares, 2, groups, heads of a group]: their max (log2 domain) and sum
   uint32_t* first;   // [S + 1]: the batch's step at which a request begins; the batch's steps
 };
