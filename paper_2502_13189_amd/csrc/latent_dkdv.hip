@@ -8,9 +8,11 @@ namespace {
 
 constexpr int kWaves = kLatBwdWaves;
 
+constexpr int kStage = 2 * kNope / 8 + 1;   // 16-byte chunks of a staged row of dk and dv (one pad)
 constexpr int kBufKv = 2 * kWide + kSlim;  // q's first 128 dims, dout, q's rotary dims
 
 __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs a) {
+  static_assert(kWaves * 32 * kStage <= 2 * kBufKv, "the staged rows fit");
   __shared__ u32x4 lds[2 * kBufKv];
   __shared__ __align__(16) float lse2[2][kLatTile], dlt[2][kLatTile];
   const int tid = threadIdx.x;
@@ -192,28 +194,46 @@ __global__ __launch_bounds__(64 * kWaves, 1) void latent_dkdv_kernel(LatentArgs 
   for (int i = i0; i < iedge; i++) step(std::true_type(), i);
   for (int i = iedge; i < n; i++) step(std::false_type(), i);
 
-  if (key >= pl.len) return;
+  // each wave stages its 32 rows, dk beside dv and then the part of dkr, and writes them whole
   const float scl = a.scale;
-  __hip_bfloat16* krow = a.dk + kt * a.dk_st + (int64_t)h * a.dk_sh;
-  __hip_bfloat16* vrow = a.dv + kt * a.dv_st + (int64_t)h * a.dv_sh;
-  float* rrow = a.dkr_part + ((int64_t)h * a.T + kt) * kRopeDim;
+  u32x4* stg = lds + wave * 32 * kStage;
+  uint2* srow = reinterpret_cast<uint2*>(stg + qc * kStage);
 #pragma unroll
   for (int dt = 0; dt < 4; dt++)
 #pragma unroll
     for (int r4 = 0; r4 < 4; r4++) {
-      const int d = 32 * dt + 8 * r4 + 4 * hh;
-      *reinterpret_cast<uint2*>(krow + d) = make_uint2(pack_bf16(dk[dt][4 * r4] * scl, dk[dt][4 * r4 + 1] * scl),
-                                                       pack_bf16(dk[dt][4 * r4 + 2] * scl, dk[dt][4 * r4 + 3] * scl));
-      *reinterpret_cast<uint2*>(vrow + d) = make_uint2(pack_bf16(dv[dt][4 * r4], dv[dt][4 * r4 + 1]),
-                                                       pack_bf16(dv[dt][4 * r4 + 2], dv[dt][4 * r4 + 3]));
+      const int d = (32 * dt + 8 * r4 + 4 * hh) >> 2;
+      srow[d] = make_uint2(pack_bf16(dk[dt][4 * r4] * scl, dk[dt][4 * r4 + 1] * scl),
+                           pack_bf16(dk[dt][4 * r4 + 2] * scl, dk[dt][4 * r4 + 3] * scl));
+      srow[d + kNope / 4] = make_uint2(pack_bf16(dv[dt][4 * r4], dv[dt][4 * r4 + 1]),
+                                       pack_bf16(dv[dt][4 * r4 + 2], dv[dt][4 * r4 + 3]));
     }
+  const auto settle = [] {  // a wave's own LDS writes, read by its other lanes
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_wave_barrier();
+  };
+  settle();
+#pragma unroll
+  for (int j = 0; j < 16; j++) {
+    const int y = 64 * j + lane, r = y / 32, c = y % 32, t = pl.t0 + 32 * wave + r;
+    __hip_bfloat16* row = c < 16 ? a.dk + (pl.tok0 + t) * a.dk_st + (int64_t)h * a.dk_sh
+                                 : a.dv + (pl.tok0 + t) * a.dv_st + (int64_t)h * a.dv_sh;
+    if (t < pl.len) reinterpret_cast<u32x4*>(row)[c % 16] = stg[r * kStage + c];
+  }
+  settle();
+  float4* sr = reinterpret_cast<float4*>(stg + qc * kStage);
 #pragma unroll
   for (int dt = 0; dt < 2; dt++)
 #pragma unroll
     for (int r4 = 0; r4 < 4; r4++)
-      *reinterpret_cast<float4*>(rrow + 32 * dt + 8 * r4 + 4 * hh) =
-          make_float4(dk[4 + dt][4 * r4] * scl, dk[4 + dt][4 * r4 + 1] * scl, dk[4 + dt][4 * r4 + 2] * scl,
-                      dk[4 + dt][4 * r4 + 3] * scl);
+      sr[(32 * dt + 8 * r4 + 4 * hh) >> 2] = make_float4(dk[4 + dt][4 * r4] * scl, dk[4 + dt][4 * r4 + 1] * scl,
+                                                         dk[4 + dt][4 * r4 + 2] * scl, dk[4 + dt][4 * r4 + 3] * scl);
+  settle();
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    const int y = 64 * j + lane, r = y / 16, c = y % 16, t = pl.t0 + 32 * wave + r;
+    if (t < pl.len) reinterpret_cast<u32x4*>(a.dkr_part + ((int64_t)h * a.T + pl.tok0 + t) * kRopeDim)[c] = stg[r * kStage + c];
+  }
 }
 
 }  // namespace
