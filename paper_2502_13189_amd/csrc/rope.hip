@@ -111,7 +111,7 @@ hipError_t rope_layout(bool interleaved, const RopeArgs& a, hipStream_t st) {
 // ================================================================ latent write
 // A token's row of the cache: 512 numbers as they are, then the 64 of the rotary key, turned.  A copy, bound by
 // memory.  A wave takes 8 tokens: their 512 numbers a lane's 16 bytes of each, their rotary keys 8 lanes each
-// with 4 pairs; all loads go out before the first is used.  116993 tokens: 44 us a launch, 6.1 TB/s (its rows
+// with 4 pairs; all loads go out before the first is used.  117017 tokens: 44 us a launch, 6.1 TB/s (its rows
 // lie in the last-level cache in part); one token of 62 requests: 3 us, latency.
 constexpr int kRank = 512, kRot = 64, kRowLen = kRank + kRot, kTokens = 8;
 
