@@ -206,6 +206,11 @@ moba_status check_latent_pages(const moba_tensor* t, __hip_bfloat16** data, int6
   return MOBA_OK;
 }
 
+// The pool's rows, as check_apart takes them.
+Rows3 pool_rows(const __hip_bfloat16* data, int64_t sp, int N, int P) {
+  return Rows3{reinterpret_cast<char*>(const_cast<__hip_bfloat16*>(data)), N > 1 ? sp : 0, kRow, N, P, kRow, 2};
+}
+
 // q, k, k_rope, v and cu_seqlens of the expanded form
 moba_status check_latent(const moba_tensor* q, const moba_tensor* k, const moba_tensor* kr, const moba_tensor* v,
                          const moba_tensor* cu, float scale, LatentArgs* a, Rows3 (&in)[4]) {
@@ -396,6 +401,11 @@ moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, c
   const int64_t T = vc.T;
   if (vr.T != T) return MOBA_ERR_SHAPE;
   if ((st = check_contig(slots, MOBA_I64, 1, &T)) != MOBA_OK) return st;
+  if (T > 0) {  // (tokens as the rows of one page: such a view may lie between the pages of a wider pool)
+    const Rows3 pool = pool_rows(a.pages, a.p_sp, a.N, a.P);
+    const Rows3 one_c{vc.data, 0, vc.st, 1, T, kRank, 2}, one_r{vr.data, 0, vr.st, 1, T, kRopeDim, 2};
+    if ((st = check_apart({&pool}, {&one_c, &one_r})) != MOBA_OK) return st;
+  }
   if (rot) {
     if ((st = check_rotation(rot, T, kRopeDim, &a.r)) != MOBA_OK) return st;
     if (a.r.half != kRopeDim / 2) return MOBA_ERR_SHAPE;
@@ -433,7 +443,8 @@ moba_status moba_latent_decode(const moba_tensor* q_c, const moba_tensor* q_rope
   if ((st = check_out(out, MOBA_BF16, true, kRank, 16, &vo)) != MOBA_OK) return st;
   const int64_t S = vc.T, H = vc.H;
   if (vr.T != S || vr.H != H || vo.T != S || vo.H != H) return MOBA_ERR_SHAPE;
-  if ((st = check_apart({&vo}, {&vc, &vr})) != MOBA_OK) return st;
+  const Rows3 pool_r = pool_rows(pool, a.p_sp, a.N, a.P);
+  if ((st = check_apart({&vo}, {&vc, &vr, &pool_r})) != MOBA_OK) return st;
   const int64_t ls[2] = {H, S};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
   if (table->dtype != MOBA_I32) return MOBA_ERR_DTYPE;

@@ -289,6 +289,32 @@ def test_overlap(lib):
     assert c.call(lib) == "MOBA_ERR_LAYOUT"
 
 
+def test_overlap_of_the_pool(lib):
+    """A write from the pool into itself (its work-groups read and write in any order), a result on the pool; rows that
+    lie between the pages of a wider pool are no overlap: such a call gets as far as the next check."""
+    for n, at in (("c", 0), ("c", 2 * 5 * 64 * 576 - 1024), ("kr", 2 * 576 * 64 + 1024)):
+        c = Write()
+        c.t[n].data, c.t[n].stride[0] = c.t["pages"].data + at, 576
+        assert c.call(lib) == "MOBA_ERR_LAYOUT", n
+        c.turn = False
+        assert c.call(lib) == "MOBA_ERR_LAYOUT", n
+    c = Write()  # pages of layer 1 of two, tokens in layer 0's page 2
+    c.t["pages"].stride[0] = 2 * 64 * 576
+    c.t["c"].data, c.t["c"].stride[0] = c.t["pages"].data + 2 * (3 * 64 * 576), 576
+    c.t["freqs"].shape[0] = 31
+    assert c.call(lib) == "MOBA_ERR_SHAPE"
+    c.t["c"].data += 2 * 58 * 576  # its last token in layer 1
+    assert c.call(lib) == "MOBA_ERR_LAYOUT"
+    for at in (0, -2 * 512, 2 * 9 * 64 * 576 - 16):
+        c = Decode()
+        c.t["out"].data = c.t["pages"].data + at
+        assert c.call(lib) == "MOBA_ERR_LAYOUT", at
+    c = Decode()
+    c.t["out"].data = c.t["pages"].data + 2 * 9 * 64 * 576
+    c.scale = 0.0
+    assert c.call(lib) == "MOBA_ERR_UNSUPPORTED"
+
+
 def test_limits(lib):
     for bad in (0.0, -1.0, math.nan, math.inf):
         for make in (Forward, Backward, Decode):
