@@ -376,11 +376,23 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
     Phase ph("latent_delta", stream);
     MOBA_LAUNCH(launch_latent_delta(a, stream));
   }
-  {
-    Phase ph("latent_dq", stream);
-    MOBA_LAUNCH(launch_latent_dq(a, stream));
-  }
-  {
+  // Few work-groups last as long as their longest chain of tiles, and both sides take about that in one launch.  One
+  // after the other and together, us a call: 8192 tokens, 1 head 422, 251; 4096, 10 heads 387, 256; 2048, 32 heads 235,
+  // 210; 256, 4 heads 36, 29; 5 sequences, 4583 tokens, 10 heads 192, 143, 32 heads (1280 work-groups) 402, 407; 8192,
+  // 32 heads 2321, 2597 (the query side is the slower for the other's registers, heads are spread over the XCDs).
+  // Sequences of a tile or so have no chains: 40 x 64 tokens, 4 heads 28, 34.
+  if (a.S <= kLatBothSeqs && a.T >= (int64_t)kLatKeys * a.S && latent_places_bound(a.T, a.S) * a.H <= kLatBoth) {
+    {
+      Phase ph("latent_first", stream);
+      MOBA_LAUNCH(launch_latent_first(a, stream));
+    }
+    Phase ph("latent_both", stream);
+    MOBA_LAUNCH(launch_latent_both(a, stream));
+  } else {
+    {
+      Phase ph("latent_dq", stream);
+      MOBA_LAUNCH(launch_latent_dq(a, stream));
+    }
     Phase ph("latent_dkdv", stream);
     MOBA_LAUNCH(launch_latent_dkdv(a, stream));
   }

@@ -18,6 +18,8 @@ constexpr int kLatLong = 4096;  // or for sequences shorter than this, on averag
 constexpr int kLatRowsDq = 128; // of a dQ work-group
 constexpr int kLatKeys = 128;   // keys of a dK/dV work-group
 constexpr int kLatTile = 64;    // tokens of a staged tile
+constexpr int kLatBoth = 1024;  // work-groups of a side up to which the backward's sides share a launch,
+constexpr int kLatBothSeqs = 64;  // and sequences
 
 struct LatentArgs {
   const __hip_bfloat16* q; int64_t q_st, q_sh;    // [T, H, 192], elements
@@ -43,6 +45,8 @@ struct LatentArgs {
 inline int64_t latent_places_bound(int64_t T, int64_t S) { return T / kLatKeys + S; }
 hipError_t launch_latent_forward(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_delta(const LatentArgs& a, hipStream_t st);
+hipError_t launch_latent_first(const LatentArgs& a, hipStream_t st);
+hipError_t launch_latent_both(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_dq(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_dkdv(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_dkr(const LatentArgs& a, hipStream_t st);

@@ -147,6 +147,56 @@ __device__ __forceinline__ bool latent_place(const LatentArgs& a, int64_t x, int
   return true;
 }
 
+// Sequence s within [0, T), whatever cu holds; its first tile.
+__device__ __forceinline__ bool latent_first(const LatentArgs& a, int s, Place* p) {
+  const int64_t c0 = a.cu[s], c1 = a.cu[s + 1];
+  const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
+  const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
+  p->tok0 = uniform64(b);
+  p->len = __builtin_amdgcn_readfirstlane((int)(e - b));
+  p->t0 = 0;
+  return p->len > 0;
+}
+
+// Rank r of (head, tile of kLatKeys tokens) pairs, those with the most tiles before them in their sequence first; of up to
+// 64 sequences.  more: the tiles behind it.
+__device__ __forceinline__ bool latent_ranked(const LatentArgs& a, uint32_t r, Place* p, int* h, int* more) {
+  const int lane = threadIdx.x & 63;
+  int64_t tok0 = 0;
+  int len = 0;
+  if (lane < a.S) {
+    const int64_t c0 = a.cu[lane], c1 = a.cu[lane + 1];
+    const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
+    const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
+    tok0 = b;
+    len = (int)(e - b);
+  }
+  const int n = (int)(((uint32_t)len + kLatKeys - 1) / kLatKeys);
+  int level = n;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) level = max(level, __shfl_xor(level, d, 64));
+  level = __builtin_amdgcn_readfirstlane(level);
+  r = __builtin_amdgcn_readfirstlane(r);
+  for (; level > 0; level--) {
+    const uint64_t in = __builtin_amdgcn_ballot_w64(n >= level);
+    const uint32_t c = (uint32_t)__popcll(in), all = c * (uint32_t)a.H;
+    if (r >= all) {
+      r -= all;
+      continue;
+    }
+    const uint32_t i = r % c;
+    const uint64_t at = __builtin_amdgcn_ballot_w64(n >= level && (uint32_t)__popcll(in & ((1ull << lane) - 1)) == i);
+    const int s = __ffsll((unsigned long long)at) - 1;
+    *h = (int)(r / c);
+    p->tok0 = uniform64(__shfl(tok0, s, 64));
+    p->len = __builtin_amdgcn_readlane(len, s);
+    p->t0 = (level - 1) * kLatKeys;
+    *more = __builtin_amdgcn_readlane(n, s) - level;
+    return true;
+  }
+  return false;
+}
+
 // Work-group -> (head, place).  Work-groups go round-robin to the 8 XCDs; each XCD takes a
 // contiguous run of (head, place) pairs, so that a head's keys and values stay in one L2.  The places
 // of a head are taken longest first where heads divide among the XCDs, and else from both

@@ -88,6 +88,19 @@ def test_backward(lens, H):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("lens,H", [
+    (tuple(37 * i % 301 for i in range(63)) + (700,), 3), (tuple(37 * i % 301 for i in range(64)) + (700,), 3),
+    ((1100, 30), 100), ((1100, 30), 110), ((200, 55), 2), ((200, 56), 2), ((0, 0, 513, 0), 2)])
+def test_backward_launches(lens, H):
+    """About the limits up to which both sides share a launch: 64 sequences, of 128 tokens on average, 1024 work-groups
+    a side."""
+    q, k, kr, v = inputs(sum(lens), H, seed=sum(lens))
+    cu = cu_of(lens)
+    out, lse = binding.latent_forward(q, k, kr, v, cu)
+    dout = randn(sum(lens), H, 128, seed=78)
+    check_backward(q, k, kr, v, cu, dout, binding.latent_backward(q, k, kr, v, cu, out, lse, dout))
+
+
 @pytest.mark.parametrize("size,scale", [(8.0, ref.SCALE), (0.01, 1.0), (3.0, 0.3)])
 def test_scores_of_other_sizes(size, scale):
     """Peaked and flat softmax: the running max moves often, or never."""
