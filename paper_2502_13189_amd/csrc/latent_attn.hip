@@ -123,6 +123,15 @@ __device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const 
     }
 }
 
+// Whether work-groups are ranked by the length of their chains, so that a chip that is filled a few times over ends
+// with short ones (but a head's work-groups then lie on all XCDs).  As latent_work has them and ranked, us: 8192
+// tokens, 10 heads 344, 227; 4 x 2000, 16 heads 117, 99; 1000 and 40 x 100, 16 heads 45, 32; 4096, 32 heads 189, 181; 8 x
+// 300, 128 heads 105, 100.  Below a work-group a CU there is no order (2048, 4 heads 45, 46), and sequences of a tile have
+// no chains (40 x 64, 32 heads 26, 28).
+__device__ __forceinline__ bool by_rank(const LatentArgs& a, int64_t groups) {
+  return a.S <= kLatBothSeqs && groups > 256 && groups <= kLatRanked && a.T > (int64_t)kLatTile * a.S;
+}
+
 template <int NW>
 __global__ __launch_bounds__(64 * NW, 8 / NW) void latent_forward_kernel(LatentArgs a) {
   constexpr int kRows = 32 * NW;
@@ -131,11 +140,18 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void latent_forward_kernel(LatentA
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qc = lane & 31, hh = lane >> 5;
 
-  Work wk;
-  if (!latent_work<true>(a, latent_places(a.T, a.S, kRows), &wk)) return;
   Place pl;
-  if (!latent_place(a, wk.place, kRows, &pl)) return;
-  const int h = __builtin_amdgcn_readfirstlane(wk.h);
+  int h;
+  const int64_t places = latent_places(a.T, a.S, kRows);
+  if (kRows == kLatKeys && by_rank(a, places * a.H)) {
+    int more;
+    if (!latent_ranked(a, blockIdx.x, &pl, &h, &more)) return;
+  } else {
+    Work wk;
+    if (!latent_work<true>(a, places, &wk)) return;
+    if (!latent_place(a, wk.place, kRows, &pl)) return;
+    h = __builtin_amdgcn_readfirstlane(wk.h);
+  }
   const int row = pl.t0 + 32 * wave + qc;         // this lane's query, within the sequence
   const int rc = min(row, pl.len - 1);
   const int kend = min(pl.t0 + kRows, pl.len);

@@ -20,6 +20,7 @@ constexpr int kLatKeys = 128;   // keys of a dK/dV work-group
 constexpr int kLatTile = 64;    // tokens of a staged tile
 constexpr int kLatBoth = 1024;  // work-groups of a side up to which the backward's sides share a launch,
 constexpr int kLatBothSeqs = 64;  // and sequences
+constexpr int kLatRanked = 4096;  // of a forward: up to which they are ranked by length (and as few sequences)
 
 struct LatentArgs {
   const __hip_bfloat16* q; int64_t q_st, q_sh;    // [T, H, 192], elements

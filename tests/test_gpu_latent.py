@@ -93,10 +93,11 @@ def test_backward(lens, H):
     ((1100, 30), 100), ((1100, 30), 110), ((200, 55), 2), ((200, 56), 2), ((0, 0, 513, 0), 2)])
 def test_backward_launches(lens, H):
     """About the limits up to which both sides share a launch: 64 sequences, of 128 tokens on average, 1024 work-groups
-    a side."""
+    a side; the forward's work-groups, ranked or not."""
     q, k, kr, v = inputs(sum(lens), H, seed=sum(lens))
     cu = cu_of(lens)
     out, lse = binding.latent_forward(q, k, kr, v, cu)
+    check_forward(q, k, kr, v, cu, out, lse)
     dout = randn(sum(lens), H, 128, seed=78)
     check_backward(q, k, kr, v, cu, dout, binding.latent_backward(q, k, kr, v, cu, out, lse, dout))
 
