@@ -1,5 +1,5 @@
-// Backward of causal latent attention (expanded form): its two sides, for the kernels.  With the forward's lse and Delta_i =
-// <dout_i, out_i>:
+// Backward of causal latent attention (expanded form): its two sides, for the kernels.  With the forward's lse and
+// Delta_i = <dout_i, out_i>:
 //   P = exp(z - lse),  dP = dout v^T,  dS = P (dP - Delta)
 //   dq = scale dS [k; kr],  dk = scale dS^T q[0:128],  dkr = scale sum over heads of dS^T q[128:192],
 //   dv = P^T dout

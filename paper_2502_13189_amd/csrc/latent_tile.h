@@ -124,6 +124,16 @@ struct Place {
   int len;       // its tokens
   int t0;        // the tile's first token within the sequence
 };
+
+// Sequence s's first token and tokens: whatever cu holds, within [0, T).
+__device__ __forceinline__ int64_t latent_span(const LatentArgs& a, int s, int* len) {
+  const int64_t c0 = a.cu[s], c1 = a.cu[s + 1];
+  const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
+  const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
+  *len = (int)(e - b);
+  return b;
+}
+
 __device__ __forceinline__ bool latent_place(const LatentArgs& a, int64_t x, int rows, Place* p) {
   // the last sequence whose first place is at or before x: 64 of them looked at together
   int lo = 0;
@@ -135,42 +145,32 @@ __device__ __forceinline__ bool latent_place(const LatentArgs& a, int64_t x, int
     n = min(step, n - k * step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
-  // (whatever cu holds, rows stay within [0, T))
-  const int64_t c0 = a.cu[lo], c1 = a.cu[lo + 1];
-  const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
-  const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
-  const int64_t t0 = (x - (c0 / rows + lo)) * rows;
-  if (t0 < 0 || t0 >= e - b) return false;
+  int len;
+  const int64_t b = latent_span(a, lo, &len);
+  const int64_t t0 = (x - (a.cu[lo] / rows + lo)) * rows;
+  if (t0 < 0 || t0 >= len) return false;
   p->tok0 = uniform64(b);
-  p->len = __builtin_amdgcn_readfirstlane((int)(e - b));
+  p->len = __builtin_amdgcn_readfirstlane(len);
   p->t0 = __builtin_amdgcn_readfirstlane((int)t0);
   return true;
 }
 
-// Sequence s within [0, T), whatever cu holds; its first tile.
+// Sequence s's first tile.
 __device__ __forceinline__ bool latent_first(const LatentArgs& a, int s, Place* p) {
-  const int64_t c0 = a.cu[s], c1 = a.cu[s + 1];
-  const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
-  const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
-  p->tok0 = uniform64(b);
-  p->len = __builtin_amdgcn_readfirstlane((int)(e - b));
+  int len;
+  p->tok0 = uniform64(latent_span(a, s, &len));
+  p->len = __builtin_amdgcn_readfirstlane(len);
   p->t0 = 0;
   return p->len > 0;
 }
 
-// Rank r of (head, tile of kLatKeys tokens) pairs, those with the most tiles before them in their sequence first; of up to
+// Pair r of (head, tile of kLatKeys tokens), those with the most tiles before them in their sequence first; of up to
 // 64 sequences.  more: the tiles behind it.
 __device__ __forceinline__ bool latent_ranked(const LatentArgs& a, uint32_t r, Place* p, int* h, int* more) {
   const int lane = threadIdx.x & 63;
   int64_t tok0 = 0;
   int len = 0;
-  if (lane < a.S) {
-    const int64_t c0 = a.cu[lane], c1 = a.cu[lane + 1];
-    const int64_t b = c0 < 0 ? 0 : c0 > a.T ? a.T : c0;
-    const int64_t e = c1 < b ? b : c1 > a.T ? a.T : c1;
-    tok0 = b;
-    len = (int)(e - b);
-  }
+  if (lane < a.S) tok0 = latent_span(a, lane, &len);
   const int n = (int)(((uint32_t)len + kLatKeys - 1) / kLatKeys);
   int level = n;
 #pragma unroll
@@ -185,7 +185,8 @@ __device__ __forceinline__ bool latent_ranked(const LatentArgs& a, uint32_t r, P
       continue;
     }
     const uint32_t i = r % c;
-    const uint64_t at = __builtin_amdgcn_ballot_w64(n >= level && (uint32_t)__popcll(in & ((1ull << lane) - 1)) == i);
+    const uint32_t before = (uint32_t)__popcll(in & ((1ull << lane) - 1));
+    const uint64_t at = __builtin_amdgcn_ballot_w64(n >= level && before == i);
     const int s = __ffsll((unsigned long long)at) - 1;
     *h = (int)(r / c);
     p->tok0 = uniform64(__shfl(tok0, s, 64));
