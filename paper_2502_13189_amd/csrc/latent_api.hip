@@ -381,7 +381,7 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
   // 210; 256, 4 heads 36, 29; 5 sequences, 4583 tokens, 10 heads 192, 143, 32 heads (1280 work-groups) 402, 407; 8192,
   // 32 heads 2321, 2597 (the query side is the slower for the other's registers, heads are spread over the XCDs).
   // Sequences of a tile or so have no chains: 40 x 64 tokens, 4 heads 28, 34.
-  if (a.S <= kLatBothSeqs && a.T >= (int64_t)kLatKeys * a.S && latent_places_bound(a.T, a.S) * a.H <= kLatBoth) {
+  if (a.S <= kLatRankedSeqs && a.T >= (int64_t)kLatKeys * a.S && latent_places_bound(a.T, a.S) * a.H <= kLatBoth) {
     {
       Phase ph("latent_first", stream);
       MOBA_LAUNCH(launch_latent_first(a, stream));

@@ -129,7 +129,7 @@ __device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const 
 // 300, 128 heads 105, 100.  Below a work-group a CU there is no order (2048, 4 heads 45, 46), and sequences of a tile have
 // no chains (40 x 64, 32 heads 26, 28).
 __device__ __forceinline__ bool by_rank(const LatentArgs& a, int64_t groups) {
-  return a.S <= kLatBothSeqs && groups > 256 && groups <= kLatRanked && a.T > (int64_t)kLatTile * a.S;
+  return a.S <= kLatRankedSeqs && groups > 256 && groups <= kLatRanked && a.T > (int64_t)kLatTile * a.S;
 }
 
 template <int NW>

@@ -18,9 +18,11 @@ constexpr int kLatLong = 4096;  // or for sequences shorter than this, on averag
 constexpr int kLatRowsDq = 128; // of a dQ work-group
 constexpr int kLatKeys = 128;   // keys of a dK/dV work-group
 constexpr int kLatTile = 64;    // tokens of a staged tile
-constexpr int kLatBoth = 1024;  // work-groups of a side up to which the backward's sides share a launch,
-constexpr int kLatBothSeqs = 64;  // and sequences
-constexpr int kLatRanked = 4096;  // of a forward: up to which they are ranked by length (and as few sequences)
+// Few work-groups are ranked by the length of their chains, up to so many sequences (a lane each): the backward's two
+// sides in one launch, up to so many work-groups a side; the forward's.
+constexpr int kLatRankedSeqs = 64;
+constexpr int kLatBoth = 1024;
+constexpr int kLatRanked = 4096;
 
 struct LatentArgs {
   const __hip_bfloat16* q; int64_t q_st, q_sh;    // [T, H, 192], elements
