@@ -518,7 +518,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
 // the decode kernel's lanes held them, of one request; PARTS threads share a piece's partials, in runs whose sums
 // are added up in order.  Requests of one run are finished already; empty ones get 0 and -inf here.
 template <int M, int PARTS>
-__global__ __launch_bounds__(256 * PARTS) void latent_join_kernel(LatentDecodeArgs a) {
+__global__ __launch_bounds__(256 * PARTS) void latent_join_kernel(LatentDecodeArgs a, uint32_t wg0) {
   constexpr int T = M == 64 ? 32 : 16;
   using V = Tile<T>;
   constexpr int kHt = M / T, kDt = 128 / T, kI = V::kN / 4, kBlocks = M * kRank / 4 / 256;
@@ -527,8 +527,9 @@ __global__ __launch_bounds__(256 * PARTS) void latent_join_kernel(LatentDecodeAr
   __shared__ float fac[kLatGroups + 1][kHeads];
   __shared__ float2 red[kRowsAt][kHeads];
   __shared__ f32x4 part[PARTS][256];
-  const int blk = (int)(blockIdx.x % kBlocks);
-  const int hg = (int)(blockIdx.x / kBlocks % (uint32_t)a.groups), s = (int)(blockIdx.x / kBlocks / (uint32_t)a.groups);
+  const uint32_t wg = wg0 + blockIdx.x;
+  const int blk = (int)(wg % kBlocks);
+  const int hg = (int)(wg / kBlocks % (uint32_t)a.groups), s = (int)(wg / kBlocks / (uint32_t)a.groups);
   const int tid = threadIdx.x, piece = tid % 256, p = tid / 256;
   // the piece: tile t of the heads and dt of a wave's dims, rows 4 i ..
   const int lane = piece % 64;
@@ -608,14 +609,19 @@ hipError_t decode(const LatentDecodeArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int M, int PARTS>
+hipError_t join_pieces(const LatentDecodeArgs& a, hipStream_t st) {
+  // (up to three heads still take 16 heads' work-groups: 2^21 requests pass one launch's work items)
+  return launch_pieces((int64_t)a.S * a.groups * (M * kRank / 4 / 256), 256 * PARTS, [&](uint32_t first, unsigned n) {
+    latent_join_kernel<M, PARTS><<<n, 256 * PARTS, 0, st>>>(a, first);
+  });
+}
+
 template <int M>
 hipError_t join(const LatentDecodeArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)((int64_t)a.S * a.groups * (M * kRank / 4 / 256));
   // few requests: many partials each.  One thread a piece and four, us a call: 131072 tokens, 16 heads 57, 45, 128
   // heads 71, 61; 8 x 16000 35.6, 35.4 and 63, 66; 16 x 8000 34.7, 35.0 and 63, 72; 64 x 4000 62, 67 and 120, 164.
-  if (a.S <= 8) latent_join_kernel<M, 4><<<grid, 1024, 0, st>>>(a);
-  else latent_join_kernel<M, 1><<<grid, 256, 0, st>>>(a);
-  return hipGetLastError();
+  return a.S <= 8 ? join_pieces<M, 4>(a, st) : join_pieces<M, 1>(a, st);
 }
 
 }  // namespace
