@@ -469,7 +469,8 @@ moba_status moba_rope_backward(const moba_tensor* dq_out, const moba_tensor* dk_
  * Last dims contiguous, rows 16-byte aligned, any token and head stride (token strides below 2^24
  * elements).  scale is positive and finite (1 / sqrt(192) is usual).  cu_seqlens [S + 1] i32 contiguous
  * is in DEVICE memory, non-decreasing and within [0, T]: nothing is read back, and a padded batch keeps
- * its rows outside [cu_seqlens[0], cu_seqlens[S]) as they are, in all outputs.  T * H < 2^28.
+ * its rows outside [cu_seqlens[0], cu_seqlens[S]) as they are, in all outputs.  T * H < 2^28 (backward: at
+ * most 2^28 - 16).
  * Nothing is allocated or kept between calls: calls can be captured into HIP graphs, and calls that share no
  * memory (workspaces included) may overlap on different streams.  None of the tensors a call writes may overlap
  * another of its tensors.  Results do not depend on timing.

@@ -13,6 +13,8 @@ using namespace moba;
 namespace {
 
 constexpr int64_t kMost = int64_t(1) << 31;
+// Tokens times heads of a backward call: 16 threads each (Delta), in whole work-groups, are below a launch's 2^32.
+constexpr int64_t kMostBackward = (int64_t(1) << 28) - 16;
 
 struct Rows3 {
   char* data;
@@ -332,7 +334,7 @@ moba_status moba_latent_forward(const moba_tensor* q, const moba_tensor* k, cons
 }
 
 size_t moba_latent_backward_workspace_bytes(int64_t T, int32_t H) {
-  if (T < 1 || H < 1 || T >= kMost || T * H >= int64_t(1) << 28) return 0;
+  if (T < 1 || H < 1 || T >= kMost || T * H > kMostBackward) return 0;
   LatentArgs a{};
   return backward_layout(T, H, nullptr, &a);
 }
@@ -357,7 +359,7 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
     if (x->T != a.T || x->H != a.H) return MOBA_ERR_SHAPE;
   if (gr.T != a.T) return MOBA_ERR_SHAPE;
   if ((st = check_apart({&gq, &gk, &gr, &gv}, {&in[0], &in[1], &in[2], &in[3], &vo, &vd})) != MOBA_OK) return st;
-  if (vd.st >= int64_t(1) << 24) return MOBA_ERR_UNSUPPORTED;
+  if (vd.st >= int64_t(1) << 24 || a.T * a.H > kMostBackward) return MOBA_ERR_UNSUPPORTED;
   const int64_t ls[2] = {a.H, a.T};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
   if ((st = check_scale(scale)) != MOBA_OK) return st;

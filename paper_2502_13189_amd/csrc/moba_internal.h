@@ -66,8 +66,9 @@ struct Problem {
 };
 
 // ---------------------------------------------------------------- launches
-// HIP refuses a launch of 2^32 or more work items along x.  Batches of very many
-// short blocks pass that, so launches over (block, kv-head) pairs go through here:
+// HIP refuses a launch of 2^32 or more work items along x, or runs what is left of their number in 32
+// bits without an error.  Batches of very many short blocks pass that, so launches over (block, kv-head) pairs go
+// through here:
 // launch(first, n) enqueues work-groups first .. first + n - 1 of `groups`, each
 // piece a multiple of 64 work-groups but the last (the kernels' maps to the 8 XCDs hold).
 template <typename F>
