@@ -440,9 +440,9 @@ typedef struct {
 /*
  * q [T, Hq, D], k [T, Hk, D] (with k_out, or both NULL) bf16 or f32 (the same), last dim contiguous, any
  * token and head stride, any D from 2 to 4096; q_out, k_out of the same shapes and dtype, may be q and k
- * themselves (with their strides), but share no memory with them otherwise (MOBA_ERR_LAYOUT).  One
- * launch; products in fp32, rounded once.  Nothing is read back or allocated: calls can be
- * captured, and overlap on different streams.
+ * themselves (with their strides), but share no memory with them otherwise, nor with what rot points to
+ * (MOBA_ERR_LAYOUT).  One launch; products in fp32, rounded once.  Nothing is read back or allocated: calls
+ * can be captured, and overlap on different streams.
  */
 moba_status moba_rope(const moba_tensor* q, const moba_tensor* k, const moba_rotation* rot,
                       moba_tensor* q_out, moba_tensor* k_out, hipStream_t stream);
@@ -473,7 +473,7 @@ moba_status moba_rope_backward(const moba_tensor* dq_out, const moba_tensor* dk_
  * most 2^28 - 16).
  * Nothing is allocated or kept between calls: calls can be captured into HIP graphs, and calls that share no
  * memory (workspaces included) may overlap on different streams.  None of the tensors a call writes may overlap
- * another of its tensors.  Results do not depend on timing.
+ * another of its tensors, nor may its workspace (as far as the call needs it): MOBA_ERR_LAYOUT.  Results do not depend on timing.
  */
 
 /*

@@ -59,13 +59,27 @@ bool same_rows(const Rows3& a, const Rows3& b) {
   return a.data == b.data && a.st == b.st && a.sh == b.sh && a.T == b.T && a.H == b.H && a.D == b.D;
 }
 
+// n bytes as one row.
+Rows3 bytes_at(const void* p, int64_t n) {
+  return Rows3{static_cast<char*>(const_cast<void*>(p)), 0, 0, n > 0, 1, n, 1};
+}
+
+// A contiguous tensor as one row of bytes.
+Rows3 flat(const moba_tensor* t) {
+  return bytes_at(t->data, numel(t) * (t->dtype == MOBA_I64 || t->dtype == MOBA_F64 ? 8 : t->dtype == MOBA_BF16 ? 2 : 4));
+}
+
 // Whether two views may share memory.  Views of one wider buffer (equal strides) share none if no
 // row of one lies on a row of the other.
 bool may_share(const Rows3& a, const Rows3& b) {
   if (a.T == 0 || b.T == 0) return false;
   const auto bytes = [](const Rows3& v) { return ((v.T - 1) * v.st + (v.H - 1) * v.sh + v.D) * v.el; };
   if (a.data + bytes(a) <= b.data || b.data + bytes(b) <= a.data) return false;
-  if (a.el != b.el || (b.data - a.data) % a.el != 0) return true;
+  if (a.el != b.el) {
+    const auto in_bytes = [](const Rows3& v) { return Rows3{v.data, v.st * v.el, v.sh * v.el, v.T, v.H, v.D * v.el, 1}; };
+    return may_share(in_bytes(a), in_bytes(b));
+  }
+  if ((b.data - a.data) % a.el != 0) return true;
   const int64_t st = a.T > 1 ? a.st : b.st, sh = a.H > 1 ? a.sh : b.sh;
   if ((a.T > 1 && b.T > 1 && a.st != b.st) || (a.H > 1 && b.H > 1 && a.sh != b.sh)) return true;
   const int64_t d = (b.data - a.data) / a.el;  // row (i, j) of b minus row (k, l) of a: d + (i - k) st + (j - l) sh
@@ -94,6 +108,13 @@ moba_status check_apart(std::initializer_list<const Rows3*> outs, std::initializ
     for (auto p = o + 1; p != outs.end(); p++)
       if (may_share(**o, **p)) return MOBA_ERR_LAYOUT;
   }
+  return MOBA_OK;
+}
+
+// Whether an output may share memory with what says where its rows stand and how fast they turn.
+moba_status check_apart(const Rows3& out, const moba_rotation* r) {
+  for (const moba_tensor* t : {r->freqs, r->pos, r->cu_seqlens, r->start})
+    if (t && may_share(out, flat(t))) return MOBA_ERR_LAYOUT;
   return MOBA_OK;
 }
 
@@ -160,6 +181,8 @@ moba_status rope_impl(const moba_tensor* q, const moba_tensor* k, const moba_rot
     for (int j = 0; j < n; j++)
       if (may_share(vo[i], vi[j]) && !(i == j && same_rows(vo[i], vi[j]))) return MOBA_ERR_LAYOUT;
   if (n == 2 && may_share(vo[0], vo[1])) return MOBA_ERR_LAYOUT;
+  for (int i = 0; i < n; i++)
+    if ((st = check_apart(vo[i], rot)) != MOBA_OK) return st;
   if (T >= kMost) return MOBA_ERR_UNSUPPORTED;
   if (T == 0 || (a.r.cu && a.r.S == 0)) return MOBA_OK;
   // the widest piece that divides the pairs and the head and that every row is aligned to
@@ -213,9 +236,9 @@ Rows3 pool_rows(const __hip_bfloat16* data, int64_t sp, int N, int P) {
   return Rows3{reinterpret_cast<char*>(const_cast<__hip_bfloat16*>(data)), N > 1 ? sp : 0, kRow, N, P, kRow, 2};
 }
 
-// q, k, k_rope, v and cu_seqlens of the expanded form
+// q, k, k_rope, v and cu_seqlens of the expanded form (in: those five)
 moba_status check_latent(const moba_tensor* q, const moba_tensor* k, const moba_tensor* kr, const moba_tensor* v,
-                         const moba_tensor* cu, float scale, LatentArgs* a, Rows3 (&in)[4]) {
+                         const moba_tensor* cu, float scale, LatentArgs* a, Rows3 (&in)[5]) {
   Rows3 &vq = in[0], &vk = in[1], &vr = in[2], &vv = in[3];
   moba_status st;
   if ((st = check_rows(q, MOBA_BF16, true, kQk, 16, &vq)) != MOBA_OK) return st;
@@ -226,6 +249,7 @@ moba_status check_latent(const moba_tensor* q, const moba_tensor* k, const moba_
   if (cu->dtype != MOBA_I32) return MOBA_ERR_DTYPE;
   if (cu->ndim != 1 || cu->shape[0] < 1) return MOBA_ERR_SHAPE;
   if (cu->shape[0] > 1 && cu->stride[0] != 1) return MOBA_ERR_LAYOUT;
+  in[4] = flat(cu);
   const int64_t T = vq.T, H = vq.H, S = cu->shape[0] - 1;
   if (vk.T != T || vr.T != T || vv.T != T || vk.H != H || vv.H != H) return MOBA_ERR_SHAPE;
   // launches of less than 2^32 threads; rows within 32 bits of a tile's first
@@ -315,15 +339,16 @@ moba_status moba_latent_forward(const moba_tensor* q, const moba_tensor* k, cons
                                 const moba_tensor* v, const moba_tensor* cu_seqlens, float scale, moba_tensor* out,
                                 moba_tensor* lse, hipStream_t stream) {
   LatentArgs a{};
-  Rows3 in[4], vo;
+  Rows3 in[5], vo;
   moba_status st;
   if (missing(out) || missing(lse)) return MOBA_ERR_NULL;
   if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a, in)) != MOBA_OK) return st;
   if ((st = check_out(out, MOBA_BF16, true, kNope, 16, &vo)) != MOBA_OK) return st;
   if (vo.T != a.T || vo.H != a.H) return MOBA_ERR_SHAPE;
-  if ((st = check_apart({&vo}, {&in[0], &in[1], &in[2], &in[3]})) != MOBA_OK) return st;
   const int64_t ls[2] = {a.H, a.T};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
+  const Rows3 vl = flat(lse);
+  if ((st = check_apart({&vo, &vl}, {&in[0], &in[1], &in[2], &in[3], &in[4]})) != MOBA_OK) return st;
   if ((st = check_scale(scale)) != MOBA_OK) return st;
   if (a.T == 0 || a.S == 0) return MOBA_OK;
   a.out = reinterpret_cast<__hip_bfloat16*>(vo.data); a.o_st = vo.st; a.o_sh = vo.sh;
@@ -345,7 +370,7 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
                                  moba_tensor* dq, moba_tensor* dk, moba_tensor* dk_rope, moba_tensor* dv,
                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
   LatentArgs a{};
-  Rows3 in[4], vo, vd, gq, gk, gr, gv;
+  Rows3 in[5], vo, vd, gq, gk, gr, gv;
   moba_status st;
   if (missing(lse)) return MOBA_ERR_NULL;
   if ((st = check_latent(q, k, k_rope, v, cu_seqlens, scale, &a, in)) != MOBA_OK) return st;
@@ -358,15 +383,21 @@ moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, con
   for (const Rows3* x : {&vo, &vd, &gq, &gk, &gv})
     if (x->T != a.T || x->H != a.H) return MOBA_ERR_SHAPE;
   if (gr.T != a.T) return MOBA_ERR_SHAPE;
-  if ((st = check_apart({&gq, &gk, &gr, &gv}, {&in[0], &in[1], &in[2], &in[3], &vo, &vd})) != MOBA_OK) return st;
   if (vd.st >= int64_t(1) << 24 || a.T * a.H > kMostBackward) return MOBA_ERR_UNSUPPORTED;
   const int64_t ls[2] = {a.H, a.T};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
+  const Rows3 vl = flat(lse);
+  if ((st = check_apart({&gq, &gk, &gr, &gv}, {&in[0], &in[1], &in[2], &in[3], &in[4], &vo, &vl, &vd})) != MOBA_OK)
+    return st;
   if ((st = check_scale(scale)) != MOBA_OK) return st;
   if (a.T == 0 || a.S == 0) return MOBA_OK;
   if (!workspace) return MOBA_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return MOBA_ERR_LAYOUT;
-  if (workspace_bytes < backward_layout(a.T, a.H, static_cast<char*>(workspace), &a)) return MOBA_ERR_NO_MEMORY;
+  const size_t need = backward_layout(a.T, a.H, static_cast<char*>(workspace), &a);
+  if (workspace_bytes < need) return MOBA_ERR_NO_MEMORY;
+  const Rows3 ws = bytes_at(workspace, (int64_t)need);
+  if ((st = check_apart({&ws}, {&in[0], &in[1], &in[2], &in[3], &in[4], &vo, &vl, &vd, &gq, &gk, &gr, &gv})) != MOBA_OK)
+    return st;
   a.out = reinterpret_cast<__hip_bfloat16*>(vo.data); a.o_st = vo.st; a.o_sh = vo.sh;
   a.lse = static_cast<float*>(lse->data);
   a.dout = reinterpret_cast<const __hip_bfloat16*>(vd.data); a.do_st = vd.st; a.do_sh = vd.sh;
@@ -418,10 +449,12 @@ moba_status moba_latent_write(const moba_tensor* c, const moba_tensor* k_rope, c
   if (T > 0) {  // (tokens as the rows of one page: such a view may lie between the pages of a wider pool)
     const Rows3 pool = pool_rows(a.pages, a.p_sp, a.N, a.P);
     const Rows3 one_c{vc.data, 0, vc.st, 1, T, kRank, 2}, one_r{vr.data, 0, vr.st, 1, T, kRopeDim, 2};
-    if ((st = check_apart({&pool}, {&one_c, &one_r})) != MOBA_OK) return st;
+    const Rows3 vs = flat(slots);
+    if ((st = check_apart({&pool}, {&one_c, &one_r, &vs})) != MOBA_OK) return st;
   }
   if (rot) {
     if ((st = check_rotation(rot, T, kRopeDim, &a.r)) != MOBA_OK) return st;
+    if (T > 0 && (st = check_apart(pool_rows(a.pages, a.p_sp, a.N, a.P), rot)) != MOBA_OK) return st;
     if (a.r.half != kRopeDim / 2) return MOBA_ERR_SHAPE;
   }
   if (T >= int64_t(1) << 28) return MOBA_ERR_UNSUPPORTED;  // (8 threads a token, 2^32 of a launch)
@@ -457,8 +490,6 @@ moba_status moba_latent_decode(const moba_tensor* q_c, const moba_tensor* q_rope
   if ((st = check_out(out, MOBA_BF16, true, kRank, 16, &vo)) != MOBA_OK) return st;
   const int64_t S = vc.T, H = vc.H;
   if (vr.T != S || vr.H != H || vo.T != S || vo.H != H) return MOBA_ERR_SHAPE;
-  const Rows3 pool_r = pool_rows(pool, a.p_sp, a.N, a.P);
-  if ((st = check_apart({&vo}, {&vc, &vr, &pool_r})) != MOBA_OK) return st;
   const int64_t ls[2] = {H, S};
   if ((st = check_contig(lse, MOBA_F32, 2, ls)) != MOBA_OK) return st;
   if (table->dtype != MOBA_I32) return MOBA_ERR_DTYPE;
@@ -466,13 +497,19 @@ moba_status moba_latent_decode(const moba_tensor* q_c, const moba_tensor* q_rope
   if (S > 0 && ((table->shape[1] > 1 && table->stride[1] != 1) || (S > 1 && table->stride[0] < table->shape[1])))
     return MOBA_ERR_LAYOUT;
   if ((st = check_contig(lens, MOBA_I32, 1, &S)) != MOBA_OK) return st;
+  const Rows3 vp = pool_rows(pool, a.p_sp, a.N, a.P), vn = flat(lens), vl = flat(lse);
+  const Rows3 vt{static_cast<char*>(table->data), S > 1 ? table->stride[0] : 0, 0, S, 1, table->shape[1], 4};
+  if ((st = check_apart({&vo, &vl}, {&vc, &vr, &vp, &vt, &vn})) != MOBA_OK) return st;
   if ((st = check_scale(scale)) != MOBA_OK) return st;
   LatentShape d{};
   if ((st = decode_shape(S, table->shape[1], H, a.P, &d)) != MOBA_OK) return st;
   if (S == 0) return MOBA_OK;
   if (!workspace) return MOBA_ERR_NULL;
   if ((reinterpret_cast<uintptr_t>(workspace) & 15) != 0) return MOBA_ERR_LAYOUT;
-  if (workspace_bytes < decode_layout(d, S, static_cast<char*>(workspace), &a)) return MOBA_ERR_NO_MEMORY;
+  const size_t need = decode_layout(d, S, static_cast<char*>(workspace), &a);
+  if (workspace_bytes < need) return MOBA_ERR_NO_MEMORY;
+  const Rows3 ws = bytes_at(workspace, (int64_t)need);
+  if ((st = check_apart({&ws}, {&vc, &vr, &vp, &vt, &vn, &vo, &vl})) != MOBA_OK) return st;
   a.qc = reinterpret_cast<const __hip_bfloat16*>(vc.data); a.qc_ss = vc.st; a.qc_sh = vc.sh;
   a.qr = reinterpret_cast<const __hip_bfloat16*>(vr.data); a.qr_ss = vr.st; a.qr_sh = vr.sh;
   a.pages = pool;
