@@ -82,6 +82,45 @@ class Attention:
         return out, [t + U * x.abs() + 1e-30 for t, x in zip(tol, out)]
 
 
+    def out_spread(self):
+        """Variance of each result's error where every rounding to bf16 is an error of its own, at most U and
+        evenly spread (U^2 / 3): of the weights as operands and of the result."""
+        return U * U / 3 * (self.p ** 2 @ self.v ** 2 + self.out ** 2)
+
+    def gradient_spread(self, dout):
+        """The same of gradients(): P as the operand of dV; dS as the others', and in it Delta, whose error (of the
+        forward's weights and out) all of a row's keys share; the results' roundings."""
+        g = dout.double().transpose(0, 1)
+        dp = g @ self.v.transpose(1, 2)
+        ds = self.p * (dp - (g * self.out).sum(2, keepdim=True))
+        delta = (g * self.out).square().sum(2, keepdim=True) + (self.p * dp).square().sum(2, keepdim=True)
+        seen = (self.p @ self.k).square()  # (a row's error of Delta moves dq along its mean key)
+        dq = (ds ** 2 @ self.k ** 2 + delta * seen) * self.scale ** 2
+        dk = (ds ** 2 + self.p ** 2 * delta).transpose(1, 2) @ self.q ** 2 * self.scale ** 2
+        dv = (self.p ** 2).transpose(1, 2) @ g ** 2
+        want, _ = self.gradients(dout)
+        return [U * U / 3 * (v + x ** 2) for v, x in
+                zip((dq, dk[..., :128], dk[..., 128:].sum(0), dv), want)]
+
+
+# The 2-norm of a block's errors is held to this many times the square root of their variances' sum.  Thousands of
+# roundings that do not depend on each other stay close to 1 of it; a single one that outweighs all
+# others is at most sqrt(3).
+SPREAD = 2.0
+
+
+def worst_block(got, ref, var, block=256):
+    """Largest norm of errors over SPREAD times what their variances [.., n, D] ask, in each of the leading
+    dims and `block` rows (the last with what is left, if that is less than a quarter)."""
+    n = ref.shape[-2]
+    cut = [i for i in range(0, n, block) if i == 0 or n - i >= block // 4] + [n]
+    e, worst_ = (got.double() - ref).square().sum(-1), 0.0
+    for i, j in zip(cut, cut[1:]):
+        t = var[..., i:j, :].sum(-1).sum(-1)
+        worst_ = max(worst_, float((e[..., i:j].sum(-1) / t).max()))
+    return math.sqrt(worst_) / SPREAD
+
+
 def decode(qc, qr, rows, scale=SCALE):
     """One request: qc [H, 512], qr [H, 64], rows [n, 576] -> out, lse and their tolerances."""
     q = torch.cat([qc, qr], 1).double()

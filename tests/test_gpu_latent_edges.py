@@ -47,3 +47,41 @@ def test_decode_of_two_million_requests():
             o, l, to, tl = ref.decode(qc[at, 0], qr[at, 0], pages[page, :n])
             assert ref.worst(out[at, 0], o, to) <= 1.0, (n, page)
             assert ref.worst(lse[0, at], l, tl) <= 1.0, (n, page, "lse")
+
+
+def inputs(T, H, seed):
+    kv = randn(T, H, 256, seed=seed + 1)
+    return randn(T, H, 192, seed=seed), kv[..., :128], randn(T, 576, seed=seed + 2)[:, 512:], kv[..., 128:]
+
+
+# both sides of the backward in one launch; one after the other, with many heads, and with long sequences
+@pytest.mark.parametrize("lens,H", [((700, 64), 5), ((1023,), 10), ((2049, 65), 1), ((1100,), 110), ((4133, 70), 32),
+                                    ((8192,), 32)])
+def test_norms_of_errors(lens, H):
+    """Results and gradients, head by head in blocks of rows or keys (dkr summed over all heads): a tile left out anywhere
+    is far outside, and no number of heads hides it."""
+    T = sum(lens)
+    q, k, kr, v = inputs(T, H, seed=T)
+    cu = torch.tensor([0, *torch.tensor(lens).cumsum(0).tolist()], dtype=torch.int32, device=DEV)
+    dout = randn(T, H, 128, seed=T + 9)
+    out, lse = binding.latent_forward(q, k, kr, v, cu)
+    dq, dk, dkr, dv = binding.latent_backward(q, k, kr, v, cu, out, lse, dout)
+    at = 0
+    for n in lens:
+        s = slice(at, at + n)
+        at += n
+        sum_, var_ = 0.0, 0.0
+        for h in range(H):
+            one = slice(h, h + 1)
+            r = ref.Attention(q[s, one], k[s, one], kr[s], v[s, one])
+            want, _ = r.gradients(dout[s, one])
+            var = r.gradient_spread(dout[s, one])
+            sum_, var_ = sum_ + want[2], var_ + var[2]
+            pairs = [("out", out, r.out, r.out_spread())]
+            pairs += [(name, g, want[i], var[i]) for name, g, i in (("dq", dq, 0), ("dk", dk, 1), ("dv", dv, 3))]
+            for name, g, x, t in pairs:
+                w = ref.worst_block(g[s, one].transpose(0, 1), x, t)
+                assert w <= 1.0, (name, n, h, w)
+        # (each head's part has the variance of a rounded result in it, a little more than the sum's own)
+        w = ref.worst_block(dkr[s], sum_, var_ + ref.U ** 2 / 3 * sum_ ** 2)
+        assert w <= 1.0, ("dkr", n, w)
