@@ -420,7 +420,7 @@ size_t moba_cache_decode_workspace_bytes(int64_t S, int64_t W, int32_t Hq, int32
  * The R / 2 pairs are dims (i, i + R / 2) of the head's first R dims, or, interleaved, (2 i, 2 i + 1); dims
  * from R on are copied.  To turn the last dims of wider heads, pass views of them.
  *
- *   freqs   [R / 2] f64 contiguous: radians a position, scaled for longer contexts as the caller
+ *   freqs   [R / 2] f64 contiguous, finite: radians a position, scaled for longer contexts as the caller
  *           wants it.  Angles are formed in 64-bit integers (a fraction of a turn): exact to 2^-52 of a turn
  *           (or of the frequency's turns a position, where they are more than one) times the position
  *   pos     [T] i32 or i64 contiguous: the rows' positions; or NULL, with
@@ -441,8 +441,8 @@ typedef struct {
  * q [T, Hq, D], k [T, Hk, D] (with k_out, or both NULL) bf16 or f32 (the same), last dim contiguous, any
  * token and head stride, any D from 2 to 4096; q_out, k_out of the same shapes and dtype, may be q and k
  * themselves (with their strides), but share no memory with them otherwise, nor with what rot points to
- * (MOBA_ERR_LAYOUT).  One launch; products in fp32, rounded once.  Nothing is read back or allocated: calls
- * can be captured, and overlap on different streams.
+ * (MOBA_ERR_LAYOUT).  T < 2^31, Hq and Hk < 65536.  One launch (more past 2^31 threads); products in fp32,
+ * rounded once.  Nothing is read back or allocated: calls can be captured, and overlap on different streams.
  */
 moba_status moba_rope(const moba_tensor* q, const moba_tensor* k, const moba_rotation* rot,
                       moba_tensor* q_out, moba_tensor* k_out, hipStream_t stream);
@@ -460,7 +460,8 @@ moba_status moba_rope_backward(const moba_tensor* dq_out, const moba_tensor* dk_
  * expanded (prefill, training): the caller has projected c to each head's k and v.
  *   q      [T, H, 192] bf16: a head's 128 dims without position, then its 64 rotary ones
  *   k, v   [T, H, 128] bf16;  k_rope [T, 64] bf16: the rotary key, shared by all heads
- *   scores scale (<q[0:128], k> + <q[128:192], k_rope>), causal in each sequence
+ *   scores scale (<q[0:128], k> + <q[128:192], k_rope>), causal in each sequence, over the call's own tokens (what
+ *   a cache holds of a sequence is not attended)
  * absorbed (decode): the projections are folded into the query, which scores c itself.
  *   q_c    [S, H, 512], q_rope [S, H, 64] bf16
  *   scores scale (<q_c, c> + <q_rope, k_rope>);  out [S, H, 512] bf16 = sum of weights times c
@@ -470,7 +471,7 @@ moba_status moba_rope_backward(const moba_tensor* dq_out, const moba_tensor* dk_
  * elements).  scale is positive and finite (1 / sqrt(192) is usual).  cu_seqlens [S + 1] i32 contiguous
  * is in DEVICE memory, non-decreasing and within [0, T]: nothing is read back, and a padded batch keeps
  * its rows outside [cu_seqlens[0], cu_seqlens[S]) as they are, in all outputs.  T * H < 2^28 (backward: at
- * most 2^28 - 16).
+ * most 2^28 - 16), H < 65536, (T / 128 + S) * H < 2^23 - 8.
  * Nothing is allocated or kept between calls: calls can be captured into HIP graphs, and calls that share no
  * memory (workspaces included) may overlap on different streams.  None of the tensors a call writes may overlap
  * another of its tensors, nor may its workspace (as far as the call needs it): MOBA_ERR_LAYOUT.  Results do not depend on timing.
@@ -490,8 +491,7 @@ moba_status moba_latent_forward(const moba_tensor* q, const moba_tensor* k, cons
  * 192], dk, dv [T, H, 128], dk_rope [T, 64] (the sum over the heads, in their order) are overwritten.
  * Weights and score gradients enter the second products as bf16, all sums are fp32, no atomics.
  * workspace: moba_latent_backward_workspace_bytes of device memory, 16-byte aligned, uninitialised.
- * Inputs are finite: a value that is not may reach any gradient of its own sequence (no other's but
- * through nothing: sequences share no sums).
+ * Inputs are finite: a value that is not may reach any gradient of its own sequence, and no other's.
  */
 moba_status moba_latent_backward(const moba_tensor* q, const moba_tensor* k, const moba_tensor* k_rope,
                                  const moba_tensor* v, const moba_tensor* cu_seqlens, float scale,

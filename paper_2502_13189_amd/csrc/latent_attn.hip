@@ -12,9 +12,9 @@
 //   O^T (dims x queries) += V^T . P^T  4 dim tiles x 4 k-steps, V^T by transposed LDS reads
 // Queries and keys are cut at the same multiples of 32, so of a wave's halves of tiles one is masked, the
 // diagonal one; those before it are whole, those behind it are left out.
-// The weights enter the second product as bf16 (2^-9 of each, independent of each other: it adds
-// to the result about what its own rounding to bf16 does); all sums are fp32.
-// 16384 tokens, 32 heads: 2.24 to 2.34 ms, 1.18 to 1.23 PFLOP/s of the 1.23 to 1.39 that large matrix products reach here
+// The weights enter the second product as bf16 (at most 2^-8 of each, independent of each other: it adds
+// to the result about what its own rounding to bf16 does, 0.0020 of its 2-norm against 0.0015); all sums are fp32.
+// 16384 tokens, 32 heads: 2.26 to 2.36 ms, 1.16 to 1.22 PFLOP/s of the 1.23 to 1.39 that large matrix products reach here
 // (the chip's clock falls under either).
 #include "latent_tile.h"
 
@@ -125,9 +125,9 @@ __device__ __forceinline__ void pv_by_key(f32x16 (&o)[4], const char* vb, const 
 
 // Whether work-groups are ranked by the length of their chains, so that a chip that is filled a few times over ends
 // with short ones (but a head's work-groups then lie on all XCDs).  As latent_work has them and ranked, us: 8192
-// tokens, 10 heads 344, 227; 4 x 2000, 16 heads 117, 99; 1000 and 40 x 100, 16 heads 45, 32; 4096, 32 heads 189, 181; 8 x
-// 300, 128 heads 105, 100.  Below a work-group a CU there is no order (2048, 4 heads 45, 46), and sequences of a tile have
-// no chains (40 x 64, 32 heads 26, 28).
+// tokens, 10 heads 335, 217; 4 x 2000, 16 heads 117, 97; 1000 and 40 x 100, 16 heads 46, 32; 4096, 32 heads 188, 176; 8 x
+// 300, 128 heads 108, 104; 8 x 1000, 4 heads 33, 30.  Below a work-group a CU there is no order (2048, 4 heads 45, 46), and
+// sequences of a tile have no chains (40 x 64, 32 heads 26, 28).
 __device__ __forceinline__ bool by_rank(const LatentArgs& a, int64_t groups) {
   return a.S <= kLatRankedSeqs && groups > 256 && groups <= kLatRanked && a.T > (int64_t)kLatTile * a.S;
 }
@@ -325,8 +325,9 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void latent_forward_kernel(LatentA
 
 // Queries of a work-group: 256, which reads k and v half as often, where many long sequences' work fills the chip; else
 // 128, two work-groups on a CU, which leaves fewer waves without rows and the last ones alone for less long.  256 and
-// 128, us: 1 x 256 tokens, 32 heads 17.3, 12.6; 8 x 1000, 4 heads 37.2, 32.4; 4096, 8 heads 115, 89; 100 x 100, 32
-// heads 39, 30; 4096, 32 heads 206, 191; 2048, 128 heads 218, 212; 8192, 32 heads 628, 664.
+// 128 (ranked where by_rank says so), us: 1 x 256 tokens, 32 heads 16.5, 12.9; 8 x 1000, 4 heads 37.2, 30.0; 4096, 8
+// heads 111, 87; 100 x 100, 32 heads 140, 103; 4096, 32 heads 204, 176; 2048, 128 heads 208, 196; 8192, 32 heads 604, 609;
+// 16384, 32 heads 2278, 2358.
 hipError_t launch_latent_forward(const LatentArgs& a, hipStream_t st) {
   if (latent_places(a.T, a.S, kLatRows) * a.H <= kLatFew || a.T < kLatLong * (int64_t)a.S)
     latent_forward_kernel<4><<<latent_grid(a, 128), 256, 0, st>>>(a);

@@ -15,13 +15,16 @@
 //   P^T under the running max, through LDS as bf16, for all waves
 //   O^T (dims x heads) += U^T . P^T  wave w owns dims 128 w .. 128 w + 127
 // The running max is raised only when some weight of the step passes 2^8; the step's weights are then formed
-// again.  The weights enter the second product as bf16, all sums are fp32.
+// again.  The weights enter the second product as bf16 (at most 2^-8 of each, independent of each other: results are
+// off by up to 0.0021 of their 2-norm, by 0.0017 from their own rounding alone; all 24 bits of a weight would take the
+// second product three times over), all sums are fp32.
 //
-// 2^20 tokens, 128 heads: 334 us and the join 13, 3.6 TB/s and 870 TFLOP/s; 48 requests of 100 to 30000 tokens
-// (261732 in all), 128 heads: 124 and 12.  A step of M = 64 takes some 5000 cycles at the 2.0 GHz that the chip keeps
+// 2^20 tokens, 128 heads: 333 us (in a row of such calls 370, the clock falls) and the join 13, 3.6 TB/s and 880
+// TFLOP/s; 48 requests of 100 to 30000 tokens (261732 in all), 128 heads: 124 (136) and 12.  A step of M = 64 takes some 5000 cycles at the 2.0 GHz that the chip keeps
 // under this load: scores 2400 (1152 of products; the DMA's 18 instructions a wave go out beside them, and the path
 // from L2 to LDS, 33 bytes a cycle of a CU, needs 2200 for a step's rows), weights 650, values 1500 (1024), flag and
-// barriers 300.  A run's start, the chain lengths - table - rows - queries, takes 11 us.
+// barriers 300.  A run's start takes 11 us: lengths, table, rows, queries, next lengths and table one after the other (loads
+// return in order, so a length asked for behind the rows waits for them, and so on), then the queries' way into registers.
 //
 // Tried, whole calls: groups of 128 heads, a row read once for all, 7700 cycles a step of twice the work, but twice
 // the partials to write and join: 2^20 tokens 326 us against 345, the 48 requests 155 against 132, 128 of 1000 tokens
@@ -291,7 +294,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_decode_kernel(LatentDecode
     dma_wait();
     __syncthreads();
     // Into the accumulation registers, where the matrix cores read them as well as anywhere, as many as
-    // those hold (the others are full); a few at a time, which is all that fits on the way.
+    // those hold (the others are full).  One at a time: the pin behind a read waits for it, which for 64 heads
+    // takes about as long as a step, once a request and run.
     u32x4 qf[kHs][kNk];
 #pragma unroll
     for (int y = 0; y < kHs * kNk; y++) {

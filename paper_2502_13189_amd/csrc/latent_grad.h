@@ -25,7 +25,7 @@
 // that costs 2% and takes its rounding from where a row's largest weights stand.  (Relative 2-norm errors of dq, 1946
 // tokens: 0.0024 without, 0.0021 with the second term; 0.0017 is the rounding of dq alone.)  Delta is off by the
 // rounding of out, the more the fewer keys a row has: where it can be had without, it is.
-// 8192 tokens, 32 heads: delta 26 us, dq 1.02 to 1.08 ms (1.02 to 1.08 PFLOP/s), dkdv 1.32 to 1.40 ms (0.98 to 1.04),
+// 8192 tokens, 32 heads: delta 28 us, dq 0.97 to 0.99 ms (1.11 to 1.13 PFLOP/s), dkdv 1.25 to 1.28 ms (1.08 to 1.10),
 // dkr 17 us.
 #pragma once
 
